@@ -1,0 +1,57 @@
+// Shared by the device-tensor operators (include/toolspec_ops.h): pointer checks, device switching, element types.
+#pragma once
+#include <initializer_list>
+
+#include "../../include/toolspec_ops.h"
+#include "ts_device_utils.h"
+#include "ts_internal.h"
+
+typedef __bf16 ts_bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 ts_bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 ts_f16x8 __attribute__((ext_vector_type(8)));
+typedef float ts_f32x4 __attribute__((ext_vector_type(4)));
+
+// Every pointer that is not null has to be memory of one GPU, the stream's: what a kernel would fault on becomes an error here.
+// Returns that GPU in *device.
+ts_status ops_device(const char* call, std::initializer_list<const void*> pointers, ts_stream stream, int* device);
+
+// Makes `device` current for a launch and gives the caller its own back.
+struct DeviceGuard {
+  int back;
+  explicit DeviceGuard(int device) : back(-1) {
+    int now = -1;
+    if (hipGetDevice(&now) == hipSuccess && now != device && hipSetDevice(device) == hipSuccess) back = now;
+  }
+  ~DeviceGuard() { if (back >= 0) (void)hipSetDevice(back); }
+};
+
+inline bool ops_dtype_ok(int32_t dtype) { return dtype == TS_DTYPE_F32 || dtype == TS_DTYPE_BF16; }
+inline int ops_esz(int32_t dtype) { return dtype == TS_DTYPE_BF16 ? 2 : 4; }
+inline bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+// fp32 as a sum of bf16 terms: each is the rest so far rounded to nearest, so two carry 16 significant bits at least and
+// three all 24 (a rest below bf16's smallest subnormal, 2^-133, is lost); infinities and NaN stay in the first term.
+// One conversion instruction of gfx950 per pair of values.
+__device__ __forceinline__ ts_bf16x2 to_bf16x2(float a, float b) {
+  const ts_f32x2 v = {a, b};
+  return __builtin_convertvector(v, ts_bf16x2);
+}
+template <int N>
+__device__ __forceinline__ void split_bf16x2(float a, float b, ts_bf16x2 (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    t[i] = to_bf16x2(a, b);
+    if (i + 1 < N) {
+      const uint32_t w = __builtin_bit_cast(uint32_t, t[i]);
+      const float ra = a - __uint_as_float(w << 16), rb = b - __uint_as_float(w & 0xffff0000u);
+      a = i == 0 && !(fabsf(a) < 0x1.ffp127f) ? 0.f : ra;          // from here on the first term is infinite
+      b = i == 0 && !(fabsf(b) < 0x1.ffp127f) ? 0.f : rb;
+    }
+  }
+}
+
+// the weights of a model with 4-bit projections (ts_mx.hip), used by the passes of toolspec.h
+size_t mx_packed_bytes(int64_t n_out, int64_t n_in);
+void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, uint8_t* codes, uint8_t* scales);
+// tiles of 16 rows go to tile n_tile0 + i * n_tile_stride of `packed`
+void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride);

@@ -1,0 +1,613 @@
+// One layer's step over a paged cache: rows appended with the rotary embedding applied on the way, and attention of one
+// new token per sequence, split over the cache's length and joined.
+#include <math.h>
+
+#include "ts_ops.h"
+
+// ---------------------------------------------------------------------------------
+// append
+//
+// A workgroup takes the rows that share a page (a single row in a decoding step, up to 16 of a context) and a few
+// heads: the values are transposed within a page, so a page's 16 positions of a dimension are one 32-byte (fp32: 64)
+// piece, written whole.  The angle of position p and pair j is p theta^(-2 j / hd); as a number of turns it is formed and
+// reduced to [-1/2, 1/2] in 64 bits, so that far positions keep their phase, and sine and cosine are taken in fp32.
+// ---------------------------------------------------------------------------------
+constexpr int APPEND_THREADS = 256, APPEND_HEADS = 8;
+
+template <typename T> __device__ __forceinline__ float widen(T v) {
+  if constexpr (sizeof(T) == 2) return bf16_to_f32(v);
+  else return v;
+}
+// n consecutive elements, 16-byte accesses where the caller says so
+template <int N, typename T>
+__device__ __forceinline__ void load_n(const T* p, bool vec, float (&v)[N]) {
+  if (vec) {
+    alignas(16) uint32_t u[N * sizeof(T) / 4];
+    static_assert(N * sizeof(T) == 8 || N * sizeof(T) % 16 == 0, "whole vectors");
+    if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2*>(u) = *reinterpret_cast<const uint2*>(p);
+    else
+#pragma unroll
+      for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(u)[i] = reinterpret_cast<const uint4*>(p)[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+      else v[i] = __uint_as_float(u[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = widen(p[i]);
+  }
+}
+template <int N, typename T>
+__device__ __forceinline__ void store_n(T* p, bool vec, const float (&v)[N]) {
+  if (vec) {
+    alignas(16) uint32_t u[N * sizeof(T) / 4];
+    static_assert(N * sizeof(T) == 8 || N * sizeof(T) % 16 == 0, "whole vectors");
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if constexpr (sizeof(T) == 2) { if (!(i & 1)) u[i / 2] = (uint32_t)f32_to_bf16(v[i]) | (uint32_t)f32_to_bf16(v[i + 1]) << 16; }
+      else u[i] = __float_as_uint(v[i]);
+    }
+    if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(u);
+    else
+#pragma unroll
+      for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<uint4*>(u)[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) st_from_f32(p + i, v[i]);
+  }
+}
+
+struct AppendArgs {
+  ts_kv_append_args a;
+  double log2_theta;                     // rope_theta > 0
+  int vec_q, vec_k, vec_out;
+};
+
+// the last sequence whose first row is not behind `row`, -1 if none: 64 offsets at a time, one per lane
+__device__ __forceinline__ int seq_of_row(const int32_t* offsets, int n, int row) {
+  const int lane = threadIdx.x % 64;
+  int lo = 0, left = n;                  // offsets [lo, lo + left) are open; all before lo are <= row
+  for (;;) {
+    const int step = (left + 63) / 64;
+    const int i = lane * step;
+    const int c = __popcll(__ballot(i < left && offsets[lo + (i < left ? i : 0)] <= row));
+    if (c == 0) return lo - 1;
+    if (step == 1) return lo + c - 1;
+    lo += (c - 1) * step + 1;
+    left = min(step - 1, left - (c - 1) * step - 1);
+    if (left <= 0) return lo - 1;
+  }
+}
+
+// TI rows' element, TC cache's element
+template <typename TI, typename TC, int HD>
+__global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
+  constexpr int VE = HD >= 32 && sizeof(TI) == 2 && sizeof(TC) == 2 ? 8 : 4, HALF = HD / 2, PIECES = HALF / VE;
+  __shared__ float2 cs[16 * HALF];
+  const ts_kv_append_args& a = g.a;
+  const int row = blockIdx.x;
+  const int seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
+  if (seq < 0 || seq >= a.n_seqs) return;
+  const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.n_rows);
+  const int64_t pos = (int64_t)a.lengths[seq] + row - first;
+  if (pos < 0 || pos >= (int64_t)a.table_width * 16 || row >= end) return;
+  const int slot = (int)(pos & 15);
+  if (row != max(first, 0) && slot != 0) return;                     // the page's first new row takes this one along
+  const int cnt = min(16 - slot, end - row);
+  const int page = a.table[(int64_t)seq * a.table_stride + pos / 16];
+  if (page < 0 || page >= a.pages.n_pages) return;
+  const int tid = threadIdx.x, hkv = a.pages.n_kv_heads, hq = a.q ? a.n_q_heads : 0;
+  const int head0 = blockIdx.y * APPEND_HEADS, turned = hq + hkv, head1 = min(head0 + APPEND_HEADS, turned + hkv);
+
+  const bool turn = a.rope_theta > 0.f;
+  if (turn && head0 < turned) {
+    for (int i = tid; i < cnt * HALF; i += APPEND_THREADS) {
+      const int r = i / HALF, j = i % HALF;
+      const double f = exp2(g.log2_theta * (-2.0 * j / HD)) * 0.15915494309189535;       // turns per position
+      const double t = f * (double)(pos + r), rest = t - rint(t);
+      float s, c;
+      sincospif(2.f * (float)rest, &s, &c);
+      cs[i] = make_float2(c, s);
+    }
+    __syncthreads();
+  }
+
+  // queries and keys: pieces of VE pairs
+  const int rot1 = min(head1, turned);
+  for (int i = tid; i < (rot1 - head0) * cnt * PIECES; i += APPEND_THREADS) {
+    const int c = i % PIECES, r = i / PIECES % cnt, h = head0 + i / PIECES / cnt;
+    const bool is_q = h < hq;
+    const TI* src = is_q ? (const TI*)a.q + (int64_t)(row + r) * a.q_stride + h * HD : (const TI*)a.k + (int64_t)(row + r) * a.k_stride + (h - hq) * HD;
+    float x[VE], y[VE];
+    const bool vec = is_q ? g.vec_q : g.vec_k;
+    load_n<VE>(src + c * VE, vec, x);
+    load_n<VE>(src + HALF + c * VE, vec, y);
+    if (turn) {
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        const float2 w = cs[r * HALF + c * VE + e];
+        const float u = x[e] * w.x - y[e] * w.y;
+        y[e] = y[e] * w.x + x[e] * w.y;
+        x[e] = u;
+      }
+    }
+    if (is_q) {
+      TI* dst = (TI*)a.q_out + (int64_t)(row + r) * a.q_out_stride + h * HD;
+      store_n<VE>(dst + c * VE, g.vec_out, x);
+      store_n<VE>(dst + HALF + c * VE, g.vec_out, y);
+    } else {
+      TC* dst = (TC*)a.pages.k + (((int64_t)page * hkv + (h - hq)) * 16 + slot + r) * HD;
+      store_n<VE>(dst + c * VE, true, x);
+      store_n<VE>(dst + HALF + c * VE, true, y);
+    }
+  }
+
+  // values: a thread writes a dimension's positions
+  const int val0 = max(head0, turned);
+  for (int i = tid; i < (head1 - val0) * HD; i += APPEND_THREADS) {
+    const int h = val0 - turned + i / HD, d = i % HD;
+    const TI* src = (const TI*)a.v + (int64_t)row * a.v_stride + h * HD + d;
+    TC* dst = (TC*)a.pages.v + (((int64_t)page * hkv + h) * HD + d) * 16 + slot;
+    if (cnt == 16) {
+      float v[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[r] = widen(src[(int64_t)r * a.v_stride]);
+      store_n<16>(dst, true, v);
+    } else {
+      for (int r = 0; r < cnt; ++r) st_from_f32(dst + r, widen(src[(int64_t)r * a.v_stride]));
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// attention of one token
+//
+// out = sum_p w_p v_p with w the softmax of scale (q . k_p): one pass over the keys and values with a running maximum m
+// and sum l; what was accumulated is multiplied by 2^(m_old - m_new) when the maximum rises.  Bound by the bytes of the
+// cache: 2 head_dim elements per position and KV head, read once for all query heads of the group.
+//
+// Matrix instructions without any exchange between lanes: S^T = K Q^T puts the 16 query heads of a tile on the lanes
+// (lane l: head l % 16) and four keys in a lane's registers, and O^T = V^T P^T wants, as its second operand, eight
+// (fp32: one) consecutive keys of a head in a lane.  Which key is which row of K's tile is free, so tile t of a block of 32 keys
+// takes key 8 (m / 4) + 4 t + m % 4 as its row m: then the probabilities a lane has computed are, in place, the operand
+// it needs, and the matching values are 16 contiguous bytes of the transposed page.  Maximum and sum of a head lie in
+// four lanes (l, l + 16, l + 32, l + 48); nothing passes through the LDS before the waves of a workgroup are joined.
+// ---------------------------------------------------------------------------------
+constexpr int ATT_WAVES = 4, ATT_KB = 32;
+
+struct AttendArgs {
+  ts_kv_attend_args a;
+  float scale_log2;                      // scores enter 2^x
+  int group, tiles, chunk, splits;       // query heads per KV head, tiles of 16 of them, keys per workgroup, workgroups per sequence at most
+  float* part_o;                         // [n_seqs][n_q_heads][splits][head_dim], relative to 2^m
+  float* part_ml;                        // [n_seqs][n_q_heads][splits][2]
+};
+
+// positions seen by a sequence's token: [lo, hi), and where its chunks start (a block boundary)
+__device__ __forceinline__ void seen_range(const ts_kv_attend_args& a, int seq, int& lo, int& hi, int& base) {
+  const int64_t room = (int64_t)a.table_width * 16;
+  hi = max(0, min(a.lengths[seq], a.max_len));
+  const int len = hi;
+  if (hi > room) hi = (int)room;
+  lo = a.window > 0 && len > a.window ? len - a.window : 0;
+  base = lo & ~(ATT_KB - 1);
+}
+
+template <typename T, typename TQ, int HD>
+__global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int QP = BF && sizeof(TQ) == 4 ? 3 : 1;          // terms of a query
+  constexpr int PP = sizeof(TQ) == 4 ? 3 : 2;                // terms of a probability (bf16 caches)
+  constexpr int KC = BF ? HD / 32 : (HD + 15) / 16;          // 16-byte pieces of a key per lane
+  constexpr int DT = (HD + 15) / 16;                         // tiles of 16 dimensions
+  constexpr int OS = DT * 16 + 4;                            // floats of a head's row in the LDS
+  __shared__ float so[ATT_WAVES * 16 * OS];
+  __shared__ float sm[ATT_WAVES][16], sl[ATT_WAVES][16];
+  const ts_kv_attend_args& a = g.a;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 16, lg = lane / 16;
+  int id = blockIdx.x;
+  const int split = id % g.splits; id /= g.splits;
+  const int tile = id % g.tiles; id /= g.tiles;
+  const int hkv = a.pages.n_kv_heads, kvh = id % hkv, seq = id / hkv;
+  int lo, hi, base;
+  seen_range(a, seq, lo, hi, base);
+  const int k0 = base + split * g.chunk, k1 = min(hi, k0 + g.chunk);
+  if (split > 0 && k0 >= hi) return;                         // the join knows which splits there are
+  const int heads = min(16, g.group - tile * 16), head0 = kvh * g.group + tile * 16;
+
+  // the queries: lane (head n, group lg) holds the dimensions it multiplies with its keys' pieces
+  uint4 q[QP][KC];
+  {
+    const TQ* src = (const TQ*)a.q + (int64_t)seq * a.q_stride + (int64_t)(head0 + min(n, heads - 1)) * HD;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      constexpr int E = BF ? 8 : 4;
+      float x[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = (c * 4 + lg) * E + e;
+        x[e] = d < HD ? widen(src[d < HD ? d : 0]) : 0.f;
+      }
+      if constexpr (BF) {
+        uint32_t u[QP][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ts_bf16x2 t[QP];
+          split_bf16x2<QP>(x[2 * e], x[2 * e + 1], t);
+#pragma unroll
+          for (int p = 0; p < QP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, t[p]);
+        }
+#pragma unroll
+        for (int p = 0; p < QP; ++p) q[p][c] = make_uint4(u[p][0], u[p][1], u[p][2], u[p][3]);
+      } else {
+        q[0][c] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+      }
+    }
+  }
+
+  ts_f32x4 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                              // l: of this lane's keys only
+
+  const int32_t* table = a.table + (int64_t)seq * a.table_stride;
+  const char* kp = (const char*)a.pages.k;
+  const char* vp = (const char*)a.pages.v;
+  const int64_t head_bytes = (int64_t)16 * HD * sizeof(T), page_bytes = hkv * head_bytes;
+
+  for (int kb = k0 + wave * ATT_KB; kb < k1; kb += ATT_WAVES * ATT_KB) {
+    // the block's two pages; the second one may lie behind the last position
+    int pg[2];
+    pg[0] = table[kb / 16];
+    pg[1] = kb + 16 < hi ? table[kb / 16 + 1] : -1;
+    const bool ok0 = pg[0] >= 0 && pg[0] < a.pages.n_pages, ok1 = pg[1] >= 0 && pg[1] < a.pages.n_pages;
+    const int64_t off0 = (ok0 ? pg[0] : 0) * page_bytes + kvh * head_bytes, off1 = (ok1 ? pg[1] : ok0 ? pg[0] : 0) * page_bytes + kvh * head_bytes;
+
+    uint4 kf[2][KC], vf[BF ? 1 : 2][DT];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int key = BF ? 8 * (n / 4) + 4 * t + n % 4 : 16 * t + n;
+      const char* row = kp + (key < 16 ? off0 : off1) + (int64_t)(key % 16) * HD * sizeof(T);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int at = (c * 4 + lg) * 16;
+        if (HD * (int)sizeof(T) % 64 == 0 || at < HD * (int)sizeof(T)) kf[t][c] = *reinterpret_cast<const uint4*>(row + at);
+        else kf[t][c] = make_uint4(0, 0, 0, 0);
+      }
+    }
+    if constexpr (BF) {
+      const char* col = vp + (lg < 2 ? off0 : off1) + (lg & 1) * 16;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) vf[0][d] = *reinterpret_cast<const uint4*>(col + (d * 16 + n) * 32);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          if (HD % 16 == 0 || d * 16 + n < HD) vf[t][d] = *reinterpret_cast<const uint4*>(vp + (t ? off1 : off0) + (d * 16 + n) * 64 + lg * 16);
+          else vf[t][d] = make_uint4(0, 0, 0, 0);
+        }
+    }
+
+    ts_f32x4 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        if constexpr (BF) {
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p)
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, kf[t][c]), __builtin_bit_cast(ts_bf16x8, q[p][c]), s[t], 0, 0, 0);
+        } else {
+          const float* kx = reinterpret_cast<const float*>(&kf[t][c]);
+          const float* qx = reinterpret_cast<const float*>(&q[0][c]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], s[t], 0, 0, 0);
+        }
+      }
+    }
+    // this lane's keys: 8 lg + 4 t + r (fp32: 16 t + 4 lg + r) of the block
+    float x[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[4 * t + r] = s[t][r] * g.scale_log2;
+    const bool whole = kb >= lo && kb + ATT_KB <= k1 && ok0 && ok1;
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = BF ? 8 * lg + i : 16 * (i / 4) + 4 * lg + i % 4, at = kb + key;
+        const bool seen = at >= lo && at < k1 && (key < 16 ? ok0 : ok1);
+        x[i] = seen ? x[i] : -INFINITY;
+        // 0 times whatever the place holds is not 0
+        if constexpr (BF) {
+          const uint32_t keep = i & 1 ? 0x0000ffffu : 0xffff0000u;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&vf[0][d]) + i / 2;
+            *w = seen ? *w : *w & keep;
+          }
+        } else {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&vf[i / 4][d]) + i % 4;
+            *w = seen ? *w : 0u;
+          }
+        }
+      }
+    }
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    top = fmaxf(max_over_lane_groups(top), m);
+    if (__ballot(top > m)) {                                 // the sums so far move to the new reference
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= f;
+      m = top;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
+      l += x[i];
+    }
+    if constexpr (BF) {
+      uint32_t u[PP][4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        ts_bf16x2 t[PP];
+        split_bf16x2<PP>(x[2 * e], x[2 * e + 1], t);
+#pragma unroll
+        for (int p = 0; p < PP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, t[p]);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int p = PP - 1; p >= 0; --p)
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, vf[0][d]),
+                                                         __builtin_bit_cast(ts_bf16x8, make_uint4(u[p][0], u[p][1], u[p][2], u[p][3])), o[d], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const float* vx = reinterpret_cast<const float*>(&vf[t][d]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[r], x[4 * t + r], o[d], 0, 0, 0);
+        }
+    }
+  }
+
+  // the four waves' parts
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (lane < 16) { sm[wave][n] = m; sl[wave][n] = l; }
+#pragma unroll
+  for (int d = 0; d < DT; ++d) *reinterpret_cast<ts_f32x4*>(&so[(wave * 16 + n) * OS + d * 16 + lg * 4]) = o[d];
+  __syncthreads();
+  for (int i = tid; i < heads * HD; i += ATT_WAVES * 64) {
+    const int h = i / HD, d = i % HD;
+    float top = sm[0][h];
+#pragma unroll
+    for (int w = 1; w < ATT_WAVES; ++w) top = fmaxf(top, sm[w][h]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, val = 0.f;
+#pragma unroll
+    for (int w = 0; w < ATT_WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm[w][h] - ref);
+      sum += f * sl[w][h];
+      val += f * so[(w * 16 + h) * OS + d];
+    }
+    const int64_t row = (int64_t)seq * a.n_q_heads + head0 + h;
+    if (g.splits == 1) {
+      st_from_f32((TQ*)a.out + (int64_t)seq * a.out_stride + (int64_t)(head0 + h) * HD + d, sum == 0.f ? 0.f : val / sum);
+      if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+    } else {
+      g.part_o[(row * g.splits + split) * HD + d] = val;
+      if (d == 0) *reinterpret_cast<float2*>(g.part_ml + (row * g.splits + split) * 2) = make_float2(top, sum);
+    }
+  }
+}
+
+// The join of a sequence's splits: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A workgroup per (sequence, head);
+// HD lanes wide, the splits dealt to as many such rows of threads as fit.
+template <typename TQ, int HD>
+__global__ __launch_bounds__(256) void k_kv_attend_join(AttendArgs g) {
+  constexpr int ROWS = 256 / HD;
+  __shared__ float sv[256], ss[ROWS];
+  const ts_kv_attend_args& a = g.a;
+  const int64_t row = blockIdx.x;
+  const int seq = (int)(row / a.n_q_heads), h = (int)(row % a.n_q_heads), d = threadIdx.x % HD, r = threadIdx.x / HD;
+  int lo, hi, base;
+  seen_range(a, seq, lo, hi, base);
+  const int used = max(1, min(g.splits, (hi - base + g.chunk - 1) / g.chunk));
+  const float2* ml = reinterpret_cast<const float2*>(g.part_ml) + row * g.splits;
+  float top = -INFINITY;
+  for (int i = threadIdx.x % 64; i < used; i += 64) top = fmaxf(top, ml[i].x);
+  top = wave_max(top);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, val = 0.f;
+  for (int i = r; i < used; i += ROWS) {
+    const float2 p = ml[i];
+    const float f = __builtin_amdgcn_exp2f(p.x - ref);
+    sum += f * p.y;
+    val += f * g.part_o[(row * g.splits + i) * HD + d];
+  }
+  sv[threadIdx.x] = val;
+  if (d == 0) ss[r] = sum;
+  __syncthreads();
+  if (r) return;
+  sum = val = 0.f;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) { sum += ss[i]; val += sv[i * HD + d]; }
+  st_from_f32((TQ*)a.out + (int64_t)seq * a.out_stride + (int64_t)h * HD + d, sum == 0.f ? 0.f : val / sum);
+  if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------------
+static ts_status check_pages(const char* call, const ts_kv_pages& p, const int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lengths,
+                             int32_t n_seqs, int32_t dtype) {
+  if (!p.k || !p.v || !table || !lengths) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  if (!ops_dtype_ok(p.dtype) || !ops_dtype_ok(dtype)) return ts_fail(TS_ERR_INVALID_ARG, "%s: dtype must be TS_DTYPE_F32 or TS_DTYPE_BF16", call);
+  if (p.n_pages < 1 || p.n_kv_heads < 1 || p.n_kv_heads > 65536) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d pages of %d KV heads", call, p.n_pages, p.n_kv_heads);
+  const int hd = p.head_dim;
+  if (p.dtype == TS_DTYPE_BF16 ? hd != 64 && hd != 128 : hd != 8 && hd != 16 && hd != 32 && hd != 64 && hd != 128)
+    return ts_fail(TS_ERR_INVALID_ARG, "%s: head_dim %d (bf16: 64 or 128; fp32: a power of two in [8,128])", call, hd);
+  if (!aligned_to(p.k, 16) || !aligned_to(p.v, 16)) return ts_fail(TS_ERR_INVALID_ARG, "%s: pages must be 16-byte aligned", call);
+  if (n_seqs < 1 || n_seqs > (1 << 20)) return ts_fail(TS_ERR_INVALID_ARG, "%s: n_seqs %d outside [1, 2^20]", call, n_seqs);
+  if (table_width < 1 || table_stride < table_width) return ts_fail(TS_ERR_INVALID_ARG, "%s: page table of width %d, stride %lld", call, table_width, (long long)table_stride);
+  if (!aligned_to(table, 4) || !aligned_to(lengths, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned table or lengths", call);
+  return TS_OK;
+}
+
+template <typename TI, typename TC>
+static bool launch_append(const AppendArgs& g, int hd, dim3 grid, hipStream_t s) {
+  switch (hd) {
+    case 64: k_kv_append<TI, TC, 64><<<grid, APPEND_THREADS, 0, s>>>(g); return true;
+    case 128: k_kv_append<TI, TC, 128><<<grid, APPEND_THREADS, 0, s>>>(g); return true;
+  }
+  if constexpr (sizeof(TC) == 4) {
+    switch (hd) {
+      case 8: k_kv_append<TI, TC, 8><<<grid, APPEND_THREADS, 0, s>>>(g); return true;
+      case 16: k_kv_append<TI, TC, 16><<<grid, APPEND_THREADS, 0, s>>>(g); return true;
+      case 32: k_kv_append<TI, TC, 32><<<grid, APPEND_THREADS, 0, s>>>(g); return true;
+    }
+  }
+  return false;
+}
+
+extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream stream) {
+  if (!args) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: null argument");
+  const ts_kv_append_args& a = *args;
+  ts_status st = check_pages("ts_kv_append", a.pages, a.table, a.table_stride, a.table_width, a.lengths, a.n_seqs, a.dtype);
+  if (st) return st;
+  const int hd = a.pages.head_dim, esz = ops_esz(a.dtype);
+  if (a.n_rows < 0 || a.n_rows > (1 << 24)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: %d rows outside [0, 2^24]", a.n_rows);
+  if (!a.row_offsets || !aligned_to(a.row_offsets, 4)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: null or misaligned row_offsets");
+  if (!(a.rope_theta >= 0.f) || !(a.rope_theta < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: rope_theta %g must be zero or positive", a.rope_theta);
+  if ((a.q != nullptr) != (a.q_out != nullptr)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: q and q_out belong together");
+  if (a.q && (a.n_q_heads < 1 || a.n_q_heads > 65536)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: %d query heads", a.n_q_heads);
+  if (a.n_rows == 0) return TS_OK;
+  if (!a.k || !a.v) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: null argument");
+  const int64_t kv_row = (int64_t)a.pages.n_kv_heads * hd, q_row = (int64_t)a.n_q_heads * hd;
+  if (a.k_stride < kv_row || a.v_stride < kv_row || (a.q && (a.q_stride < q_row || a.q_out_stride < q_row)))
+    return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: a row stride is below its row");
+  if (!aligned_to(a.k, esz) || !aligned_to(a.v, esz) || !aligned_to(a.q, esz) || !aligned_to(a.q_out, esz))
+    return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: rows are not aligned to their type");
+  int dev;
+  if ((st = ops_device("ts_kv_append", {a.pages.k, a.pages.v, a.table, a.lengths, a.row_offsets, a.q, a.k, a.v, a.q_out}, stream, &dev))) return st;
+  DeviceGuard on(dev);
+  AppendArgs g{};
+  g.a = a;
+  g.log2_theta = a.rope_theta > 0.f ? log2((double)a.rope_theta) : 0.0;
+  g.vec_q = aligned_to(a.q, 16) && a.q_stride * esz % 16 == 0;
+  g.vec_k = aligned_to(a.k, 16) && a.k_stride * esz % 16 == 0;
+  g.vec_out = aligned_to(a.q_out, 16) && a.q_out_stride * esz % 16 == 0;
+  const int heads = (a.q ? a.n_q_heads : 0) + 2 * a.pages.n_kv_heads;
+  const dim3 grid(a.n_rows, (heads + APPEND_HEADS - 1) / APPEND_HEADS);
+  hipStream_t s = (hipStream_t)stream;
+  const bool in16 = a.dtype == TS_DTYPE_BF16, c16 = a.pages.dtype == TS_DTYPE_BF16;
+  in16 ? c16 ? launch_append<bf16_t, bf16_t>(g, hd, grid, s) : launch_append<bf16_t, float>(g, hd, grid, s)
+       : c16 ? launch_append<float, bf16_t>(g, hd, grid, s) : launch_append<float, float>(g, hd, grid, s);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+// How a call is cut: chunks of 128 keys or a multiple, so many that about four workgroups a CU are there for the longest
+// sequences; the number never falls when max_len grows.
+constexpr int ATT_GROUPS = 4 * 256;
+static void attend_cut(int64_t n_seqs, int hq, int hkv, int max_len, int window, int* chunk, int* splits) {
+  const int tiles = (hq / hkv + 15) / 16;
+  const int64_t span = window > 0 && window < max_len ? (int64_t)window + ATT_KB - 1 : max_len;
+  const int64_t unit = ATT_WAVES * ATT_KB, units = std::max<int64_t>(1, (span + unit - 1) / unit);
+  const int64_t want = std::max<int64_t>(1, ATT_GROUPS / (n_seqs * hkv * tiles));
+  const int64_t per = (units + want - 1) / want;             // units a chunk
+  *chunk = (int)(per * unit);
+  *splits = (int)((units + per - 1) / per);
+}
+static int64_t attend_splits_room(int64_t n_seqs, int hq, int hkv, int max_len, int window) {
+  const int tiles = (hq / hkv + 15) / 16;
+  const int64_t span = window > 0 && window < max_len ? (int64_t)window + ATT_KB - 1 : max_len;
+  const int64_t unit = ATT_WAVES * ATT_KB, units = std::max<int64_t>(1, (span + unit - 1) / unit);
+  return std::min(units, std::max<int64_t>(1, ATT_GROUPS / (n_seqs * hkv * tiles)));
+}
+
+static ts_status check_attend(const char* call, int32_t n_seqs, int32_t hq, int32_t hkv, int32_t max_len, int32_t window) {
+  if (n_seqs < 1 || n_seqs > (1 << 20)) return ts_fail(TS_ERR_INVALID_ARG, "%s: n_seqs %d outside [1, 2^20]", call, n_seqs);
+  if (hkv < 1 || hkv > 65536 || hq < 1 || hq > 65536 || hq % hkv) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d query heads over %d KV heads", call, hq, hkv);
+  if (max_len < 0 || max_len > (1 << 30)) return ts_fail(TS_ERR_INVALID_ARG, "%s: max_len %d outside [0, 2^30]", call, max_len);
+  if (window < 0) return ts_fail(TS_ERR_INVALID_ARG, "%s: window %d is negative", call, window);
+  const int64_t groups = (int64_t)n_seqs * hkv * ((hq / hkv + 15) / 16) * attend_splits_room(n_seqs, hq, hkv, max_len, window);
+  if (groups > 0x7fffffff || (int64_t)n_seqs * hq > 0x7fffffff) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d sequences of %d heads are too many for one call", call, n_seqs, hq);
+  return TS_OK;
+}
+
+extern "C" ts_status ts_kv_attend_workspace(int32_t n_seqs, int32_t hq, int32_t hkv, int32_t head_dim, int32_t max_len, int32_t window, uint64_t* bytes) {
+  if (!bytes) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend_workspace: null argument");
+  ts_status st = check_attend("ts_kv_attend_workspace", n_seqs, hq, hkv, max_len, window);
+  if (st) return st;
+  if (head_dim < 8 || head_dim > 128) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend_workspace: head_dim %d", head_dim);
+  const int64_t room = attend_splits_room(n_seqs, hq, hkv, max_len, window);
+  *bytes = room > 1 ? (uint64_t)n_seqs * hq * room * (head_dim + 2) * 4 : 0;
+  return TS_OK;
+}
+
+template <typename T, typename TQ, int HD>
+static void launch_attend(const AttendArgs& g, hipStream_t s) {
+  const ts_kv_attend_args& a = g.a;
+  k_kv_attend<T, TQ, HD><<<(uint32_t)((int64_t)a.n_seqs * a.pages.n_kv_heads * g.tiles * g.splits), ATT_WAVES * 64, 0, s>>>(g);
+  if (g.splits > 1) k_kv_attend_join<TQ, HD><<<(uint32_t)((int64_t)a.n_seqs * a.n_q_heads), 256, 0, s>>>(g);
+}
+template <typename TQ>
+static void launch_attend_q(const AttendArgs& g, hipStream_t s) {
+  const int hd = g.a.pages.head_dim;
+  if (g.a.pages.dtype == TS_DTYPE_BF16) {
+    if (hd == 64) launch_attend<bf16_t, TQ, 64>(g, s);
+    else launch_attend<bf16_t, TQ, 128>(g, s);
+  } else {
+    if (hd == 8) launch_attend<float, TQ, 8>(g, s);
+    else if (hd == 16) launch_attend<float, TQ, 16>(g, s);
+    else if (hd == 32) launch_attend<float, TQ, 32>(g, s);
+    else if (hd == 64) launch_attend<float, TQ, 64>(g, s);
+    else launch_attend<float, TQ, 128>(g, s);
+  }
+}
+
+extern "C" ts_status ts_kv_attend(const ts_kv_attend_args* args, ts_stream stream) {
+  if (!args) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: null argument");
+  const ts_kv_attend_args& a = *args;
+  ts_status st = check_pages("ts_kv_attend", a.pages, a.table, a.table_stride, a.table_width, a.lengths, a.n_seqs, a.dtype);
+  if (st) return st;
+  if ((st = check_attend("ts_kv_attend", a.n_seqs, a.n_q_heads, a.pages.n_kv_heads, a.max_len, a.window))) return st;
+  if (!a.q || !a.out) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: null argument");
+  const int64_t q_row = (int64_t)a.n_q_heads * a.pages.head_dim;
+  if (a.q_stride < q_row || a.out_stride < q_row) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: a row stride is below its row");
+  const int esz = ops_esz(a.dtype);
+  if (!aligned_to(a.q, esz) || !aligned_to(a.out, esz) || !aligned_to(a.lse, 4)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: rows are not aligned to their type");
+  if (!(fabsf(a.scale) < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: scale must be finite");
+  AttendArgs g{};
+  g.a = a;
+  attend_cut(a.n_seqs, a.n_q_heads, a.pages.n_kv_heads, a.max_len, a.window, &g.chunk, &g.splits);
+  if (g.splits > 1) {
+    uint64_t need = 0;
+    if ((st = ts_kv_attend_workspace(a.n_seqs, a.n_q_heads, a.pages.n_kv_heads, a.pages.head_dim, a.max_len, a.window, &need))) return st;
+    if (!a.workspace || a.workspace_bytes < need || !aligned_to(a.workspace, 16))
+      return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: needs a 16-byte aligned workspace of %llu bytes, got %llu", (unsigned long long)need, (unsigned long long)a.workspace_bytes);
+  }
+  int dev;
+  if ((st = ops_device("ts_kv_attend", {a.pages.k, a.pages.v, a.table, a.lengths, a.q, a.out, a.lse, g.splits > 1 ? a.workspace : nullptr}, stream, &dev))) return st;
+  DeviceGuard on(dev);
+  g.scale_log2 = a.scale * 1.4426950408889634f;
+  g.group = a.n_q_heads / a.pages.n_kv_heads;
+  g.tiles = (g.group + 15) / 16;
+  g.part_o = (float*)a.workspace;
+  g.part_ml = g.part_o + (int64_t)a.n_seqs * a.n_q_heads * g.splits * a.pages.head_dim;
+  if (a.dtype == TS_DTYPE_BF16) launch_attend_q<bf16_t>(g, (hipStream_t)stream);
+  else launch_attend_q<float>(g, (hipStream_t)stream);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}

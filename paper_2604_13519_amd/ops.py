@@ -1,0 +1,274 @@
+"""Binding of the device-tensor operators of libtoolspec_hip.so (include/toolspec_ops.h) for torch tensors.
+
+Function names mirror the header.  A call checks what the tensors themselves tell (types, shapes, devices, contiguity
+within a row), allocates outputs that it is not given, and enqueues on the current stream of the tensors' GPU; whatever
+is wrong raises before anything is enqueued.  The arithmetic is the library's: there is no fallback.
+"""
+import ctypes as C
+
+import numpy as np
+import torch
+
+from . import binding
+from .binding import TS_DTYPE_BF16, TS_DTYPE_F32, TS_PAGE_SIZE
+
+EXPORTS = ("ts_mx_quantize", "ts_mx_dequantize", "ts_mx_packed_bytes", "ts_mx_pack", "ts_mx_project", "ts_kv_layer_pages", "ts_kv_page_table",
+           "ts_kv_extend", "ts_kv_append", "ts_kv_attend", "ts_kv_attend_workspace")
+
+_DTYPES = {torch.float32: TS_DTYPE_F32, torch.bfloat16: TS_DTYPE_BF16}
+
+
+class ts_kv_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ts_kv_append_args(C.Structure):
+    _fields_ = [("pages", ts_kv_pages), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int32),
+                ("lengths", C.c_void_p), ("row_offsets", C.c_void_p),
+                ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("n_q_heads", C.c_int32), ("dtype", C.c_int32),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("k", C.c_void_p), ("k_stride", C.c_int64), ("v", C.c_void_p), ("v_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("q_out_stride", C.c_int64), ("rope_theta", C.c_float)]
+
+
+class ts_kv_attend_args(C.Structure):
+    _fields_ = [("pages", ts_kv_pages), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int32), ("lengths", C.c_void_p),
+                ("n_seqs", C.c_int32), ("max_len", C.c_int32), ("window", C.c_int32), ("n_q_heads", C.c_int32), ("dtype", C.c_int32),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64), ("lse", C.c_void_p), ("scale", C.c_float),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
+_lib = None
+
+
+def _load():
+    global _lib
+    lib = binding.load_library()
+    if _lib is not lib:
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        for name, args in {
+            "ts_mx_quantize": [p, i32, i64, i64, i64, p, p, p],
+            "ts_mx_dequantize": [p, p, i64, i64, p, i32, i64, p],
+            "ts_mx_packed_bytes": [i32, i32, C.POINTER(C.c_uint64)],
+            "ts_mx_pack": [p, p, i32, i32, p, p],
+            "ts_mx_project": [p, i32, i32, p, i32, i64, i64, p, i64, p],
+            "ts_kv_layer_pages": [p, i32, C.POINTER(ts_kv_pages)],
+            "ts_kv_page_table": [p, C.POINTER(i32), i32],
+            "ts_kv_extend": [p, i32, p],
+            "ts_kv_append": [C.POINTER(ts_kv_append_args), p],
+            "ts_kv_attend": [C.POINTER(ts_kv_attend_args), p],
+            "ts_kv_attend_workspace": [i32, i32, i32, i32, i32, i32, C.POINTER(C.c_uint64)],
+        }.items():
+            fn = getattr(lib, name)
+            fn.argtypes, fn.restype = args, i32
+        _lib = lib
+    return lib
+
+
+def _stream(t):
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _refuse(what, *args):
+    raise ValueError(what % args)
+
+
+def _rows(t, name, cols=None, dtype=None):
+    """A matrix whose rows are contiguous; the distance between rows is free."""
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        _refuse("%s: a matrix with contiguous rows is needed, got shape %s, strides %s", name, tuple(t.shape), t.stride())
+    if cols is not None and t.shape[1] != cols:
+        _refuse("%s: rows of %d values are needed, got %d", name, cols, t.shape[1])
+    if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+        raise TypeError("%s: %s is needed, got %s" % (name, dtype or "float32 or bfloat16", t.dtype))
+    if not t.is_cuda:
+        _refuse("%s is not on a GPU", name)
+    return t.data_ptr(), max(t.stride(0), t.shape[1])
+
+
+def _ints(t, name, n=None):
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 1 or (n is not None and t.shape[0] < n):
+        _refuse("%s: at least %s contiguous int32 on a GPU are needed, got %s %s", name, n, t.dtype, tuple(t.shape))
+    return t.data_ptr()
+
+
+def _bytes(t, name, shape=None):
+    if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+        _refuse("%s: a contiguous uint8 tensor%s on a GPU is needed, got %s %s", name, " of shape %s" % (shape,) if shape else "", t.dtype, tuple(t.shape))
+    return t.data_ptr()
+
+
+# ---- 4-bit microscaled values ------------------------------------------------------------
+def ts_mx_quantize(x, codes=None, scales=None):
+    """x [rows][cols] fp32 or bf16 -> (codes uint8 [rows][16 * blocks], scales uint8 [rows][blocks]), blocks = ceil(cols / 32)."""
+    lib = _load()
+    px, stride = _rows(x, "x")
+    rows, cols = x.shape
+    blocks = (cols + 31) // 32
+    if codes is None:
+        codes = torch.empty((rows, 16 * blocks), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device)
+    binding._check(lib.ts_mx_quantize(px, _DTYPES[x.dtype], rows, cols, stride, _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks)), _stream(x)))
+    return codes, scales
+
+
+def ts_mx_dequantize(codes, scales, cols, dtype=torch.float32, out=None):
+    """The values [rows][cols] that codes and scales stand for (exact in both types)."""
+    lib = _load()
+    rows, blocks = codes.shape[0], (cols + 31) // 32
+    pc, ps = _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks))
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    po, stride = _rows(out, "out", cols, dtype)
+    if out.shape[0] != rows:
+        _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
+    binding._check(lib.ts_mx_dequantize(pc, ps, rows, cols, po, _DTYPES[dtype], stride, _stream(codes)))
+    return out
+
+
+def ts_mx_packed_bytes(n_out, n_in):
+    n = C.c_uint64()
+    binding._check(_load().ts_mx_packed_bytes(n_out, n_in, C.byref(n)))
+    return n.value
+
+
+def ts_mx_pack(codes, scales, n_in, out=None):
+    """Weights [n_out][n_in], given as codes and scales, laid out for ts_mx_project: a uint8 tensor to keep."""
+    lib = _load()
+    n_out, blocks = codes.shape[0], (n_in + 31) // 32
+    pc, ps = _bytes(codes, "codes", (n_out, 16 * blocks)), _bytes(scales, "scales", (n_out, blocks))
+    n = ts_mx_packed_bytes(n_out, n_in)
+    if out is None:
+        out = torch.empty(n, dtype=torch.uint8, device=codes.device)
+    binding._check(lib.ts_mx_pack(pc, ps, n_out, n_in, _bytes(out, "out", (n,)), _stream(codes)))
+    return out
+
+
+def ts_mx_project(packed, n_out, x, out=None):
+    """x [rows][n_in] times the packed weights' transpose: [rows][n_out] in x's type."""
+    lib = _load()
+    px, xs = _rows(x, "x")
+    rows, n_in = x.shape
+    if n_in < 1 or n_out < 1 or _bytes(packed, "packed") and packed.numel() != ts_mx_packed_bytes(n_out, n_in):
+        _refuse("packed: not the weights of a [%d][%d] matrix", n_out, n_in)
+    if out is None:
+        out = torch.empty((rows, n_out), dtype=x.dtype, device=x.device)
+    po, os_ = _rows(out, "out", n_out, x.dtype)
+    if out.shape[0] != rows:
+        _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
+    binding._check(lib.ts_mx_project(packed.data_ptr(), n_out, n_in, px, _DTYPES[x.dtype], rows, xs, po, os_, _stream(x)))
+    return out
+
+
+# ---- one layer of a paged cache -----------------------------------------------------------
+def ts_kv_layer_pages(kv, layer):
+    """The pages of one layer of a library cache, to be given to ts_kv_append / ts_kv_attend as `k_pages` (with v_pages None)."""
+    p = ts_kv_pages()
+    binding._check(_load().ts_kv_layer_pages(kv, layer, C.byref(p)))
+    return p
+
+
+def ts_kv_page_table(kv, capacity_tokens):
+    """The cache's physical pages in order: numpy int32 [ceil(capacity_tokens / 16)], of the capacity it was allocated with."""
+    out = np.empty((capacity_tokens + TS_PAGE_SIZE - 1) // TS_PAGE_SIZE, np.int32)
+    binding._check(_load().ts_kv_page_table(kv, out.ctypes.data_as(C.POINTER(C.c_int32)), len(out)))
+    return out
+
+
+def ts_kv_extend(kv, n_pos, stream=None):
+    """Counts n_pos positions that were appended on `stream` (a torch stream; default: the current one) as committed."""
+    s = (stream or torch.cuda.current_stream()).cuda_stream
+    binding._check(_load().ts_kv_extend(kv, n_pos, s))
+
+
+def _pages(k_pages, v_pages):
+    if v_pages is None:
+        if not isinstance(k_pages, ts_kv_pages):
+            raise TypeError("v_pages is missing")
+        return k_pages
+    if k_pages.dim() != 4 or k_pages.shape[2] != TS_PAGE_SIZE or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not k_pages.is_cuda or not v_pages.is_cuda:
+        _refuse("k_pages: a contiguous [pages][heads][%d][head_dim] tensor on a GPU is needed, got %s", TS_PAGE_SIZE, tuple(k_pages.shape))
+    n, h, _, hd = k_pages.shape
+    if tuple(v_pages.shape) != (n, h, hd, TS_PAGE_SIZE):
+        _refuse("v_pages: shape %s is needed, got %s", (n, h, hd, TS_PAGE_SIZE), tuple(v_pages.shape))
+    if k_pages.dtype not in _DTYPES or v_pages.dtype != k_pages.dtype:
+        raise TypeError("pages: float32 or bfloat16 are needed, got %s and %s" % (k_pages.dtype, v_pages.dtype))
+    return ts_kv_pages(k_pages.data_ptr(), v_pages.data_ptr(), n, h, hd, _DTYPES[k_pages.dtype])
+
+
+def _table(t, n_seqs):
+    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.shape[0] < n_seqs or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1) \
+            or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        _refuse("table: int32 [%d][pages] on a GPU is needed, got %s %s", n_seqs, t.dtype, tuple(t.shape))
+    return t.data_ptr(), max(t.stride(0), t.shape[1]), t.shape[1]
+
+
+def ts_kv_append(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_theta, q_out=None):
+    """Rows of k and v ([rows][kv heads * head_dim]) into the cache at lengths[s], lengths[s] + 1, ... of their sequences, keys
+    rotated; with q ([rows][heads * head_dim]) the rotated queries, which are returned.  See the header."""
+    lib = _load()
+    pages = _pages(k_pages, v_pages)
+    n = row_offsets.shape[0] - 1
+    a = ts_kv_append_args()
+    a.pages = pages
+    a.table, a.table_stride, a.table_width = _table(table, n)
+    a.lengths, a.row_offsets = _ints(lengths, "lengths", n), _ints(row_offsets, "row_offsets", 2)
+    a.n_seqs, a.n_rows, a.dtype, a.rope_theta = n, k.shape[0], _DTYPES.get(k.dtype, -1), rope_theta
+    width = pages.n_kv_heads * pages.head_dim
+    a.k, a.k_stride = _rows(k, "k", width)
+    a.v, a.v_stride = _rows(v, "v", width, k.dtype)
+    if v.shape[0] != k.shape[0]:
+        _refuse("v: %d rows are needed, got %d", k.shape[0], v.shape[0])
+    if q is not None:
+        a.q, a.q_stride = _rows(q, "q", None, k.dtype)
+        if q.shape[0] != k.shape[0] or q.shape[1] < 1 or q.shape[1] % pages.head_dim:
+            _refuse("q: %d rows of a multiple of %d values are needed, got %s", k.shape[0], pages.head_dim, tuple(q.shape))
+        if q_out is None:
+            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        a.q_out, a.q_out_stride = _rows(q_out, "q_out", q.shape[1], k.dtype)
+        if q_out.shape[0] != k.shape[0]:
+            _refuse("q_out: %d rows are needed, got %d", k.shape[0], q_out.shape[0])
+        a.n_q_heads = q.shape[1] // pages.head_dim
+    elif q_out is not None:
+        _refuse("q_out without q")
+    binding._check(lib.ts_kv_append(C.byref(a), _stream(k)))
+    return q_out
+
+
+def ts_kv_attend_workspace(n_seqs, n_q_heads, n_kv_heads, head_dim, max_len, window=0, device="cuda"):
+    """A workspace tensor for ts_kv_attend calls of these sizes (None where they need none)."""
+    n = C.c_uint64()
+    binding._check(_load().ts_kv_attend_workspace(n_seqs, n_q_heads, n_kv_heads, head_dim, max_len, window, C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=None, workspace=None, out=None, lse=None):
+    """Attention of one token per sequence, q [n_seqs][heads * head_dim]: (out like q, lse fp32 [n_seqs][heads]).  scale None:
+    1 / sqrt(head_dim).  workspace: of ts_kv_attend_workspace; without one the call allocates it.  See the header."""
+    lib = _load()
+    pages = _pages(k_pages, v_pages)
+    n, hd = q.shape[0], pages.head_dim
+    a = ts_kv_attend_args()
+    a.pages = pages
+    a.q, a.q_stride = _rows(q, "q")
+    if n < 1 or q.shape[1] < 1 or q.shape[1] % hd:
+        _refuse("q: rows of a multiple of %d values are needed, got %s", hd, tuple(q.shape))
+    a.table, a.table_stride, a.table_width = _table(table, n)
+    a.lengths = _ints(lengths, "lengths", n)
+    heads = q.shape[1] // hd
+    a.n_seqs, a.max_len, a.window, a.n_q_heads, a.dtype = n, max_len, window, heads, _DTYPES[q.dtype]
+    if out is None:
+        out = torch.empty((n, heads * hd), dtype=q.dtype, device=q.device)
+    a.out, a.out_stride = _rows(out, "out", heads * hd, q.dtype)
+    if lse is None:
+        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+    if out.shape[0] != n or tuple(lse.shape) != (n, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
+        _refuse("out and lse: [%d][%d] and contiguous fp32 [%d][%d] are needed", n, heads * hd, n, heads)
+    a.lse = lse.data_ptr()
+    a.scale = hd ** -0.5 if scale is None else scale
+    if workspace is None:
+        workspace = ts_kv_attend_workspace(n, heads, pages.n_kv_heads, hd, max_len, window, q.device)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _bytes(workspace, "workspace"), workspace.numel()
+    binding._check(lib.ts_kv_attend(C.byref(a), _stream(q)))
+    return out, lse
