@@ -50,7 +50,7 @@ ts_status ts_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t 
 
 /* A weight matrix [n_out][n_in] laid out for the product, once: ts_mx_packed_bytes bytes,
  * 16-byte aligned, written by ts_mx_pack from codes and scales (which may be freed then).
- * Errors: as above; n_out and n_in in [1, 2^24]. */
+ * Errors: as above; n_out in [1, 2^24], n_in in [1, 2^22]. */
 ts_status ts_mx_packed_bytes(int32_t n_out, int32_t n_in, uint64_t* bytes);
 ts_status ts_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t n_out, int32_t n_in, void* packed, ts_stream stream);
 
@@ -59,7 +59,8 @@ ts_status ts_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t n_out,
  * that add up to them), the sums are fp32, y is rounded once.  The order of the sums depends on
  * the sizes only, never on the contents, the device's load or the other rows.
  * A row's result does not depend on the other rows' values.
- * Errors: INVALID_ARG as above (rows in [0, 2^22], strides at least the row). */
+ * Errors: INVALID_ARG as above (rows in [0, 2^22], strides at least the row,
+ * x_stride at most 2^22). */
 ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_in, const void* x, int32_t dtype, int64_t rows,
                         int64_t x_stride, void* y, int64_t y_stride, ts_stream stream);
 

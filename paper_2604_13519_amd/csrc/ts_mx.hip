@@ -3,6 +3,10 @@
 // A block of 32 values has a scale 2^e, e = floor(log2 max|x|) - 2, so that the largest lies in [4, 8) of the 4-bit
 // grid 0, 1/2, 1, 3/2, 2, 3, 4, 6.  e is read off the exponent field of the largest magnitude; dividing by a power of
 // two is exact, so the rounding of v_cvt_scalef32_pk_fp4_f32 (to nearest, ties to even, saturating) is the only one.
+#include <math.h>
+
+#include <algorithm>
+
 #include "ts_ops.h"
 
 // ---------------------------------------------------------------------------------
@@ -11,16 +15,17 @@
 constexpr int QT = 256, QU = 4;           // threads of a workgroup, pieces of eight values per thread
 
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]) {
-  if (vec && n >= 8) {
+__device__ __forceinline__ void values8(const T* p, int n, float (&v)[8]) {
+  if (n >= 8) {
     if constexpr (sizeof(T) == 2) {
-      const uint4 w = *reinterpret_cast<const uint4*>(p);
+      const uint4 w = load16(p);
       const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
     } else {
-      const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+      const ts_f32x4 a = __builtin_bit_cast(ts_f32x4, load16(p)), b = __builtin_bit_cast(ts_f32x4, load16(p + 4));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
     }
   } else {
 #pragma unroll
@@ -35,7 +40,7 @@ __device__ __forceinline__ void load8(const T* p, int n, bool vec, float (&v)[8]
 }
 
 template <typename T>
-__global__ __launch_bounds__(QT) void k_mx_quantize(const T* x, uint32_t rows, uint32_t cols, int64_t stride, bool vec,
+__global__ __launch_bounds__(QT) void k_mx_quantize(const T* x, uint32_t rows, uint32_t cols, int64_t stride,
                                                     uint8_t* codes, uint8_t* scales) {
   const uint32_t blocks = (cols + 31) / 32, row_pieces = blocks * 4;
   const uint64_t pieces = (uint64_t)rows * row_pieces;                     // < 2^32, see the launch
@@ -44,7 +49,7 @@ __global__ __launch_bounds__(QT) void k_mx_quantize(const T* x, uint32_t rows, u
   for (int u = 0; u < QU; ++u) {
     const uint64_t at = (uint64_t)blockIdx.x * (QT * QU) + u * QT + threadIdx.x;
     const uint32_t piece = (uint32_t)(at < pieces ? at : 0), r = piece / row_pieces, c = (piece - r * row_pieces) * 8;
-    load8(x + (int64_t)r * stride + c, (int)cols - (int)c, vec, v[u]);
+    values8(x + (int64_t)r * stride + c, (int)cols - (int)c, v[u]);
   }
 #pragma unroll
   for (int u = 0; u < QU; ++u) {
@@ -77,7 +82,7 @@ __device__ __forceinline__ float mx_scale(uint32_t s) {
 
 template <typename T>
 __global__ __launch_bounds__(QT) void k_mx_dequantize(const uint8_t* codes, const uint8_t* scales, uint32_t rows, uint32_t cols,
-                                                      T* x, int64_t stride, bool vec) {
+                                                      T* x, int64_t stride) {
   const uint32_t blocks = (cols + 31) / 32, row_pieces = blocks * 4;
   const uint64_t pieces = (uint64_t)rows * row_pieces;
   uint32_t w[QU], s[QU];
@@ -99,15 +104,15 @@ __global__ __launch_bounds__(QT) void k_mx_dequantize(const uint8_t* codes, cons
     v[0] = a[0] * f; v[1] = a[1] * f; v[2] = b[0] * f; v[3] = b[1] * f; v[4] = d[0] * f; v[5] = d[1] * f; v[6] = e[0] * f; v[7] = e[1] * f;
     T* p = x + (int64_t)r * stride + c;
     const int n = (int)cols - (int)c;
-    if (vec && n >= 8) {
+    if (n >= 8) {
       if constexpr (sizeof(T) == 2) {                                       // two significant bits: cutting is exact
         uint32_t o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(v[2 * i]) >> 16 | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
-        *reinterpret_cast<uint4*>(p) = make_uint4(o[0], o[1], o[2], o[3]);
+        store16(p, make_uint4(o[0], o[1], o[2], o[3]));
       } else {
-        reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        store16(p, __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3])));
+        store16(p + 4, __builtin_bit_cast(uint4, make_float4(v[4], v[5], v[6], v[7])));
       }
     } else {
 #pragma unroll
@@ -127,33 +132,32 @@ static uint32_t mx_groups(int64_t rows, int64_t cols) { return (uint32_t)((rows 
 void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t* codes, uint8_t* scales) {
   const int64_t blocks = (cols + 31) / 32, slab = mx_slab(cols);
   const int esz = ops_esz(dtype);
-  const bool vec = aligned_to(x, 16) && stride * esz % 16 == 0;
   for (int64_t r = 0; r < rows; r += slab) {
     const int64_t n = std::min(slab, rows - r);
     const void* xs = (const char*)x + r * stride * esz;
     uint8_t *cs = codes + r * blocks * 16, *ss = scales + r * blocks;
-    if (dtype == TS_DTYPE_BF16) k_mx_quantize<bf16_t><<<mx_groups(n, cols), QT, 0, s>>>((const bf16_t*)xs, (uint32_t)n, (uint32_t)cols, stride, vec, cs, ss);
-    else k_mx_quantize<float><<<mx_groups(n, cols), QT, 0, s>>>((const float*)xs, (uint32_t)n, (uint32_t)cols, stride, vec, cs, ss);
+    if (dtype == TS_DTYPE_BF16) k_mx_quantize<bf16_t><<<mx_groups(n, cols), QT, 0, s>>>((const bf16_t*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
+    else k_mx_quantize<float><<<mx_groups(n, cols), QT, 0, s>>>((const float*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
   }
 }
 
 static void launch_mx_dequantize(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, void* x, int32_t dtype, int64_t stride) {
   const int64_t blocks = (cols + 31) / 32, slab = mx_slab(cols);
   const int esz = ops_esz(dtype);
-  const bool vec = aligned_to(x, 16) && stride * esz % 16 == 0;
   for (int64_t r = 0; r < rows; r += slab) {
     const int64_t n = std::min(slab, rows - r);
     void* xs = (char*)x + r * stride * esz;
     const uint8_t *cs = codes + r * blocks * 16, *ss = scales + r * blocks;
-    if (dtype == TS_DTYPE_BF16) k_mx_dequantize<bf16_t><<<mx_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (bf16_t*)xs, stride, vec);
-    else k_mx_dequantize<float><<<mx_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (float*)xs, stride, vec);
+    if (dtype == TS_DTYPE_BF16) k_mx_dequantize<bf16_t><<<mx_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (bf16_t*)xs, stride);
+    else k_mx_dequantize<float><<<mx_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (float*)xs, stride);
   }
 }
 
 // ---------------------------------------------------------------------------------
 // weights laid out for the product: records of (16 rows, 128 columns), chunk after chunk of a row tile.  A record is
-// what one wave loads for one chunk, contiguous: 16 bytes of codes per lane (lane l: row l % 16, block l / 16 of the
-// chunk), then a scale byte per lane.  Rows and blocks beyond the matrix hold zeros.
+// what one wave loads for one chunk, contiguous: 16 bytes of codes per lane - lane l = 16 g + n: of row n, codes
+// 8 g .. + 7 of each of the chunk's four blocks, the operand of four matrix instructions - then the four scales of each
+// row.  Rows and blocks beyond the matrix hold zeros.
 // ---------------------------------------------------------------------------------
 constexpr int MX_REC = 1024 + 64;
 static int64_t mx_chunks(int64_t n_in) { return (n_in + 127) / 128; }
@@ -164,16 +168,19 @@ __global__ __launch_bounds__(256) void k_mx_pack(const uint8_t* codes, const uin
   const int64_t rec = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (rec >= records) return;
   const int lane = threadIdx.x % 64, tile = (int)(rec / chunks), c = (int)(rec % chunks);
-  const int n = tile * 16 + lane % 16, b = c * 4 + lane / 16, blocks = (n_in + 31) / 32;
-  uint4 w = make_uint4(0, 0, 0, 0);
-  uint8_t s = 127;
-  if (n < n_out && b < blocks) {
-    w = reinterpret_cast<const uint4*>(codes)[(int64_t)n * blocks + b];
-    s = scales[(int64_t)n * blocks + b];
+  const int n = tile * 16 + lane % 16, lg = lane / 16, blocks = (n_in + 31) / 32;
+  const int64_t row = (int64_t)min(n, n_out - 1) * blocks;
+  uint32_t w[4], s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = c * 4 + i;
+    const bool in = n < n_out && b < blocks;
+    w[i] = in ? reinterpret_cast<const uint32_t*>(codes)[(row + b) * 4 + lg] : 0;
+    s[i] = in ? scales[row + b] : 127;
   }
   uint8_t* p = packed + ((int64_t)(n_tile0 + tile * n_tile_stride) * chunks + c) * MX_REC;
-  reinterpret_cast<uint4*>(p)[lane] = w;
-  p[1024 + lane] = s;
+  reinterpret_cast<uint4*>(p)[lane] = make_uint4(w[0], w[1], w[2], w[3]);
+  if (lg == 0) reinterpret_cast<uint32_t*>(p + 1024)[lane] = s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24;
 }
 
 void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride) {
@@ -184,12 +191,9 @@ void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, 
 // ---------------------------------------------------------------------------------
 // the product
 //
-// A workgroup computes WR x RT row tiles by WC x CT column tiles (of 16) over all of K; KW groups of its waves take
-// every KW-th chunk of 128 inputs and are added up in the LDS at the end, in the order of the groups.  The weights go
-// from memory straight into the registers of the matrix instructions: a lane's 16 bytes are one block of one row, and
-// since a sum over k may be taken in any order as long as both operands agree on it, the four instructions of a chunk
-// take inputs 32 g + 8 i .. + 7 from lane group g.  The rows go through the LDS (16-byte pieces, their place in a row
-// of 256 bytes exclusive-or'ed with the row number: the 16 rows a quarter wave reads lie in different banks).
+// The weights go from memory straight into the registers of the matrix instructions; a pair of codes is widened with its
+// scale by one conversion instruction.  Two significant bits and eight of exponent fit bf16, so nothing is rounded.
+// (Models' rows are halves: see the range of the scales at their loading.)
 // ---------------------------------------------------------------------------------
 enum { MX_IN_BF16 = 0, MX_IN_F32 = 1, MX_IN_PLANES = 2 };   // rows: bf16; fp32 as three bf16 terms; a model's hi and lo halves
 enum { MX_OUT_ROWS = 0, MX_OUT_SWIGLU = 1 };
@@ -200,7 +204,6 @@ struct MxArgs {
   void* y; int64_t y_stride; size_t y_plane; int32_t y_f32;
   unsigned long long* sat;
   int rows, n_out, n_in, chunks;
-  int vec_x, vec_y;
 };
 
 template <int IN> struct MxIn { static constexpr int planes = IN == MX_IN_BF16 ? 1 : IN == MX_IN_F32 ? 3 : 2; };
@@ -211,9 +214,10 @@ __device__ __forceinline__ ts_f32x4 mx_mfma(uint4 w, uint4 x, ts_f32x4 acc) {
   else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, w), __builtin_bit_cast(ts_bf16x8, x), acc, 0, 0, 0);
 }
 
-// eight 4-bit codes -> eight halves or bf16 values times the scale (both exact: see the callers for the ranges)
+// eight 4-bit codes of block i of a chunk -> eight halves or bf16 values times its scale, of which the instruction reads the exponent
 template <int IN>
-__device__ __forceinline__ uint4 mx_widen(uint32_t w, float s) {
+__device__ __forceinline__ uint4 mx_widen(uint32_t w, uint32_t scales, int i) {
+  const float s = __uint_as_float((scales >> 8 * i & 255) << 23);
   uint4 o;
   if constexpr (IN == MX_IN_PLANES) {
     o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0));
@@ -228,210 +232,469 @@ __device__ __forceinline__ uint4 mx_widen(uint32_t w, float s) {
   }
   return o;
 }
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// one 16-byte piece (eight inputs) of a row as it comes from memory
+// eight inputs of a row as they come from memory
 template <int IN> struct MxRaw { uint4 a[IN == MX_IN_BF16 ? 1 : 2]; };
 
+template <int IN> struct MxElem { typedef bf16_t T; };
+template <> struct MxElem<MX_IN_F32> { typedef float T; };
+// Byte offset of element k of row r from row `row0`, within 32 bits (see the limit of the stride): added to a uniform
+// base by the load itself.  Rows past the last: the last again, never stored.  The empty asm keeps the compiler from
+// forming 64-bit lane addresses ahead of the loop, two registers and two additions a load.
 template <int IN>
-__device__ __forceinline__ MxRaw<IN> mx_fetch(const MxArgs& g, int r, int k) {
+__device__ __forceinline__ uint32_t mx_x_offset(const MxArgs& g, int row0, int r, int k) {
+  return ((uint32_t)(min(row0 + r, g.rows - 1) - row0) * (uint32_t)g.x_stride + k) * (uint32_t)sizeof(typename MxElem<IN>::T);
+}
+template <int IN>
+__device__ __forceinline__ MxRaw<IN> mx_fetch(const MxArgs& g, const char* base, uint32_t off) {
   MxRaw<IN> o;
+  asm("" : "+v"(off));
+  o.a[0] = load16(base + off);
+  if constexpr (IN == MX_IN_F32) o.a[1] = load16(base + off + 16);
+  if constexpr (IN == MX_IN_PLANES) o.a[1] = load16(base + g.x_plane * 2 + off);
+  return o;
+}
+__device__ __forceinline__ uint4 mx_fetch_w(const uint8_t* base, uint32_t off) {
+  asm("" : "+v"(off));
+  return *reinterpret_cast<const uint4*>(base + off);
+}
+__device__ __forceinline__ uint32_t mx_fetch_s(const uint8_t* base, uint32_t off) {
+  asm("" : "+v"(off));
+  return *reinterpret_cast<const uint32_t*>(base + 1024 + off);
+}
+// the first n of them, zeros behind (models' rows are whole chunks)
+template <int IN>
+__device__ __forceinline__ MxRaw<IN> mx_fetch_some(const char* base, uint32_t off, int n) {
+  const typename MxElem<IN>::T* p = (const typename MxElem<IN>::T*)(base + off);
+  MxRaw<IN> o;
+  if constexpr (IN != MX_IN_PLANES) {
+    constexpr int W = IN == MX_IN_BF16 ? 4 : 8;
+    uint32_t u[W];
 #pragma unroll
-  for (uint4& v : o.a) v = make_uint4(0, 0, 0, 0);
-  if (r >= g.rows || k >= g.n_in) return o;
-  if constexpr (IN == MX_IN_PLANES) {                        // n_in is a multiple of 128, rows are padded
-    const f16_t* p = (const f16_t*)g.x + (int64_t)r * g.x_stride + k;
-    o.a[0] = *reinterpret_cast<const uint4*>(p);
-    o.a[1] = *reinterpret_cast<const uint4*>(p + g.x_plane);
-  } else if constexpr (IN == MX_IN_BF16) {
-    const bf16_t* p = (const bf16_t*)g.x + (int64_t)r * g.x_stride + k;
-    if (g.vec_x && k + 8 <= g.n_in) o.a[0] = *reinterpret_cast<const uint4*>(p);
-    else {
-      uint32_t u[4] = {0, 0, 0, 0};
+    for (int i = 0; i < W; ++i) u[i] = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) if (k + i < g.n_in) u[i / 2] |= (uint32_t)p[i] << 16 * (i & 1);
-      o.a[0] = make_uint4(u[0], u[1], u[2], u[3]);
-    }
-  } else {
-    const float* p = (const float*)g.x + (int64_t)r * g.x_stride + k;
-    if (g.vec_x && k + 8 <= g.n_in) { o.a[0] = reinterpret_cast<const uint4*>(p)[0]; o.a[1] = reinterpret_cast<const uint4*>(p)[1]; }
-    else {
-      uint32_t u[8];
+    for (int i = 0; i < 8; ++i)
+      if (i < n) {
+        if constexpr (IN == MX_IN_BF16) u[i / 2] |= (uint32_t)p[i] << 16 * (i & 1);
+        else u[i] = __float_as_uint(p[i]);
+      }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = k + i < g.n_in ? __float_as_uint(p[i]) : 0;
-      o.a[0] = make_uint4(u[0], u[1], u[2], u[3]);
-      o.a[1] = make_uint4(u[4], u[5], u[6], u[7]);
-    }
+    for (int i = 0; i < W / 4; ++i) o.a[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
   }
   return o;
 }
 
-// into the LDS as one piece per plane, `plane` bytes apart
+// the planes that enter the matrix instructions
 template <int IN>
-__device__ __forceinline__ void mx_put(char* at, int plane, const MxRaw<IN>& v) {
+__device__ __forceinline__ void mx_planes(const MxRaw<IN>& v, uint4 (&o)[MxIn<IN>::planes]) {
   if constexpr (IN == MX_IN_F32) {
     const uint32_t u[8] = {v.a[0].x, v.a[0].y, v.a[0].z, v.a[0].w, v.a[1].x, v.a[1].y, v.a[1].z, v.a[1].w};
-    uint32_t o[3][4];
+    uint32_t t3[3][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       ts_bf16x2 t[3];
       split_bf16x2<3>(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]), t);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) o[p][i] = __builtin_bit_cast(uint32_t, t[p]);
+      for (int p = 0; p < 3; ++p) t3[p][i] = __builtin_bit_cast(uint32_t, t[p]);
     }
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *reinterpret_cast<uint4*>(at + p * plane) = make_uint4(o[p][0], o[p][1], o[p][2], o[p][3]);
+    for (int p = 0; p < 3; ++p) o[p] = make_uint4(t3[p][0], t3[p][1], t3[p][2], t3[p][3]);
   } else {
 #pragma unroll
-    for (int p = 0; p < MxIn<IN>::planes; ++p) *reinterpret_cast<uint4*>(at + p * plane) = v.a[p];
+    for (int p = 0; p < MxIn<IN>::planes; ++p) o[p] = v.a[p];
   }
 }
 
-template <int IN, int OUT, int RT, int CT, int WR, int WC, int KW>
-__global__ __launch_bounds__(WR * WC * KW * 64) void k_mx_project(MxArgs g) {
-  constexpr int NP = MxIn<IN>::planes, MT = WR * RT * 16, GT = WR * WC * 64, XU = MT * 16 / GT;
-  static_assert(XU * GT == MT * 16, "pieces of a chunk divide among the threads of a group");
-  constexpr int PLANE = MT * 256, LDS = NP * KW * PLANE, RED = (KW - 1) * WR * WC * CT * RT * 1024;
-  static_assert(LDS <= 160 * 1024 && RED <= 160 * 1024, "LDS of a CU");
-  __shared__ __align__(16) char smem[LDS > RED ? LDS : RED];
-  const int tid = threadIdx.x, kw = tid / GT, gt = tid % GT, lane = tid % 64, wave = gt / 64;
-  const int wr = wave / WC, wc = wave % WC, lm = lane % 16, lg = lane / 16;
-  const int row0 = blockIdx.y * MT, tile0 = (blockIdx.x * WC + wc) * CT, n_tiles = (g.n_out + 15) / 16;
-  char* xs = smem + kw * (NP * PLANE);
+// four neighbouring columns of one row
+__device__ __forceinline__ void mx_emit(const MxArgs& g, int row, int n, const ts_f32x4& v) {
+  if (row >= g.rows || n >= g.n_out) return;
+  if (g.y_f32) {
+    float* p = (float*)g.y + (int64_t)row * g.y_stride + n;
+    if (n + 4 <= g.n_out) store16(p, __builtin_bit_cast(uint4, v));
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (n + j < g.n_out) p[j] = v[j];
+  } else {
+    bf16_t* p = (bf16_t*)g.y + (int64_t)row * g.y_stride + n;
+    const uint32_t a = __builtin_bit_cast(uint32_t, to_bf16x2(v[0], v[1])), b = __builtin_bit_cast(uint32_t, to_bf16x2(v[2], v[3]));
+    if (n + 4 <= g.n_out) store8(p, make_uint2(a, b));
+    else
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (n + j < g.n_out) p[j] = (bf16_t)((j < 2 ? a : b) >> 16 * (j & 1));
+  }
+}
+// SwiGLU of four neighbouring features
+__device__ __forceinline__ void mx_emit_swiglu(const MxArgs& g, int row, int f, const ts_f32x4& gate, const ts_f32x4& up) {
+  if (row >= g.rows || 2 * f >= g.n_out) return;
+  float p[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) p[j] = gate[j] / (1.f + __expf(-gate[j])) * up[j];
+  st_act_planes4((f16_t*)g.y + (int64_t)row * g.y_stride + f, g.y_plane, p[0], p[1], p[2], p[3], g.sat);
+}
 
+// Few rows or few columns: KW waves share RT row tiles by CT column tiles (of 16), wave w takes chunks w, w + KW, ..., UC
+// of them per request and two requests in flight.  An input is used by one wave only, so a lane reads its pieces of its
+// rows itself: for instruction i of a chunk, 64 neighbouring bytes of each of 16 rows.  The waves' sums meet in the
+// LDS, added in their order.
+template <int IN, int OUT, int RT, int CT, int KW, int UC>
+__global__ __launch_bounds__(KW * 64) void k_mx_few(MxArgs g) {
+  typedef typename MxElem<IN>::T E;
+  constexpr int NP = MxIn<IN>::planes;
+  __shared__ __align__(16) ts_f32x4 red[KW][RT * CT][64];
+  const int kw = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, lm = lane % 16, lg = lane / 16;
+  const int row0 = blockIdx.y * (RT * 16), tile0 = blockIdx.x * CT, n_tiles = (g.n_out + 15) / 16;
   const uint8_t* wp[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) wp[c] = g.w + (int64_t)min(tile0 + c, n_tiles - 1) * g.chunks * MX_REC;
+  const char* xp = (const char*)((const E*)g.x + (int64_t)row0 * g.x_stride);
+  uint32_t xo[RT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) xo[r] = mx_x_offset<IN>(g, row0, r * 16 + lm, lg * 8);
+  ts_f32x4 acc[RT][CT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[r][c] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
 
-  ts_f32x4 acc[CT][RT];
+  struct Request { uint4 w[UC][CT]; uint32_t s[UC][CT]; MxRaw<IN> x[UC][RT][4]; };
+  const int full = g.n_in / 128;                             // chunks without an end in them
+  auto fetch = [&](Request& q, int c0) {
 #pragma unroll
-  for (int c = 0; c < CT; ++c)
+    for (int u = 0; u < UC; ++u) {
+      const int64_t cc = min(c0 + u * KW, full - 1);         // past the end: requested, not used
 #pragma unroll
-    for (int r = 0; r < RT; ++r) acc[c][r] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
-
-  uint4 wn[CT];
-  uint32_t sn[CT];
-  MxRaw<IN> xn[XU];
-  auto fetch = [&](int chunk) {
-    const int cc = min(chunk, g.chunks - 1);                              // past the end: loaded, never used
+      for (int c = 0; c < CT; ++c) { q.w[u][c] = mx_fetch_w(wp[c] + cc * MX_REC, lane * 16); q.s[u][c] = mx_fetch_s(wp[c] + cc * MX_REC, lm * 4); }
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      wn[c] = *reinterpret_cast<const uint4*>(wp[c] + (int64_t)cc * MX_REC + lane * 16);
-      sn[c] = wp[c][(int64_t)cc * MX_REC + 1024 + lane];
-    }
+      for (int r = 0; r < RT; ++r)
 #pragma unroll
-    for (int u = 0; u < XU; ++u) {
-      const int piece = gt + u * GT, r = piece / 16, k = chunk * 128 + (piece % 16) * 8;
-      xn[u] = mx_fetch<IN>(g, row0 + r, k);
+        for (int i = 0; i < 4; ++i) q.x[u][r][i] = mx_fetch<IN>(g, xp + (cc * 128 + i * 32) * (int)sizeof(E), xo[r]);
     }
   };
-  fetch(kw);
-  const int trips = (g.chunks + KW - 1) / KW;
-  for (int t = 0; t < trips; ++t) {
-    const int chunk = t * KW + kw;
+  auto multiply = [&](const uint4 (&w)[CT], const uint32_t (&s)[CT], const MxRaw<IN> (&x)[RT][4]) {
 #pragma unroll
-    for (int u = 0; u < XU; ++u) {
-      const int piece = gt + u * GT, r = piece / 16, q = piece % 16;
-      mx_put<IN>(xs + r * 256 + ((q ^ (r & 15)) * 16), PLANE, xn[u]);
-    }
-    uint4 w[CT];
-    float s[CT];
+    for (int i = 0; i < 4; ++i) {
+      uint4 wf[CT];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) { w[c] = wn[c]; s[c] = mx_scale(sn[c]); }
-    __syncthreads();
-    if (t + 1 < trips) fetch(chunk + KW);
-    if (chunk < g.chunks) {
+      for (int c = 0; c < CT; ++c) wf[c] = mx_widen<IN>(word(w[c], i), s[c], i);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint4 wf[CT];
+      for (int r = 0; r < RT; ++r) {
+        uint4 xf[NP];
+        mx_planes<IN>(x[r][i], xf);
 #pragma unroll
-        for (int c = 0; c < CT; ++c) wf[c] = mx_widen<IN>(i == 0 ? w[c].x : i == 1 ? w[c].y : i == 2 ? w[c].z : w[c].w, s[c]);
+        for (int p = NP - 1; p >= 0; --p)                    // the smaller terms first
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          const int row = (wr * RT + r) * 16 + lm;
-#pragma unroll
-          for (int p = 0; p < NP; ++p) {
-            const uint4 xf = *reinterpret_cast<const uint4*>(xs + p * PLANE + row * 256 + (((4 * lg + i) ^ lm) * 16));
-#pragma unroll
-            for (int c = 0; c < CT; ++c) acc[c][r] = mx_mfma<IN>(wf[c], xf, acc[c][r]);
-          }
-        }
+          for (int c = 0; c < CT; ++c) acc[r][c] = mx_mfma<IN>(wf[c], xf[p], acc[r][c]);
       }
     }
-    __syncthreads();
+  };
+  auto use = [&](const Request& q, int c0) {
+#pragma unroll
+    for (int u = 0; u < UC; ++u)
+      if (c0 + u * KW < full) multiply(q.w[u], q.s[u], q.x[u]);
+  };
+  const int trips = (full + KW * UC - 1) / (KW * UC);
+  if (full > 0) {
+    Request a, b;
+    fetch(a, kw);
+    for (int t = 0; t < trips; t += 2) {
+      fetch(b, (t + 1) * (KW * UC) + kw);
+      use(a, t * (KW * UC) + kw);
+      if (t + 1 >= trips) break;
+      fetch(a, (t + 2) * (KW * UC) + kw);
+      use(b, (t + 1) * (KW * UC) + kw);
+    }
+  }
+  if (IN != MX_IN_PLANES && full < g.chunks && kw == full % KW) {         // the last chunk ends early
+    uint4 w[CT];
+    uint32_t s[CT];
+    MxRaw<IN> x[RT][4];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) { w[c] = mx_fetch_w(wp[c] + (int64_t)full * MX_REC, lane * 16); s[c] = mx_fetch_s(wp[c] + (int64_t)full * MX_REC, lm * 4); }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[r][i] = mx_fetch_some<IN>(xp + ((int64_t)full * 128 + i * 32) * (int)sizeof(E), xo[r], g.n_in - (full * 128 + i * 32 + lg * 8));
+    multiply(w, s, x);
+  }
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) red[kw][r * CT + c][lane] = acc[r][c];
+  __syncthreads();
+  auto sum = [&](int t) {
+    ts_f32x4 v = red[0][t][lane];
+#pragma unroll
+    for (int o = 1; o < KW; ++o) v += red[o][t][lane];
+    return v;
+  };
+  constexpr int STEP = OUT == MX_OUT_SWIGLU ? 2 : 1;         // tiles alternate: gate and up of the same 16 features
+  for (int t = kw * STEP; t < RT * CT; t += KW * STEP) {
+    const int row = row0 + t / CT * 16 + lm, tile = tile0 + t % CT;
+    if constexpr (OUT == MX_OUT_SWIGLU) mx_emit_swiglu(g, row, tile * 8 + 4 * lg, sum(t), sum(t + 1));
+    else mx_emit(g, row, tile * 16 + 4 * lg, sum(t));
+  }
+}
+
+// More rows.  A workgroup computes RT row tiles by WC x CT column tiles (of T x T, T = 16 or 32) over all of K; KW
+// groups of its waves take every KW-th chunk and are added up in the LDS at the end, in the order of the groups.  The
+// rows go through the LDS (16-byte pieces, their place in a row of 256 bytes exclusive-or'ed with the row number: the
+// rows that a read of 16 lanes covers lie in different banks), in two buffers, one barrier a step; rows and weights are
+// requested a step ahead.
+template <int T> struct MxTile;
+template <> struct MxTile<16> { typedef ts_f32x4 Acc; };
+template <> struct MxTile<32> { typedef float Acc __attribute__((ext_vector_type(16))); };
+template <int IN, int T>
+__device__ __forceinline__ typename MxTile<T>::Acc mx_mfma_t(uint4 w, uint4 x, typename MxTile<T>::Acc acc) {
+  if constexpr (T == 16) return mx_mfma<IN>(w, x, acc);
+  else if constexpr (IN == MX_IN_PLANES) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(ts_f16x8, w), __builtin_bit_cast(ts_f16x8, x), acc, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ts_bf16x8, w), __builtin_bit_cast(ts_bf16x8, x), acc, 0, 0, 0);
+}
+
+constexpr int MX_AHEAD = 4;
+template <int IN, int OUT, int T, int RT, int CT, int WC, int KW>
+__global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
+  typedef typename MxTile<T>::Acc Acc;
+  typedef typename MxElem<IN>::T E;
+  constexpr int NP = MxIn<IN>::planes, MT = RT * T, GT = WC * 64, XU = MT * 16 / GT, AQ = T * T / 256;
+  constexpr int BL = T / 16, KS = 4 * BL;                    // 16-byte pieces of a record per lane, instructions of a chunk
+  static_assert(XU * GT == MT * 16, "pieces of a chunk divide among the threads of a group");
+  constexpr int PLANE = MT * 256, BUF = NP * KW * PLANE, RED = (KW - 1) * WC * CT * RT * AQ * 1024;
+  static_assert(2 * BUF <= 160 * 1024 && RED <= 160 * 1024, "LDS of a CU");
+  __shared__ __align__(16) char smem[2 * BUF > RED ? 2 * BUF : RED];
+  const int tid = threadIdx.x, kw = __builtin_amdgcn_readfirstlane(tid / GT), gt = tid % GT, lane = tid % 64;
+  const int wc = __builtin_amdgcn_readfirstlane(gt / 64), lm = lane % T, lg = lane / T;
+  const int row0 = blockIdx.y * MT, tile0 = (blockIdx.x * WC + wc) * CT, n_tiles = (g.n_out + 15) / 16;
+  char* xs = smem + kw * (NP * PLANE);
+
+  // Weights: instruction i of a chunk takes inputs (64 / T) 8 i + 8 lg .. + 7.  With T = 32 a lane's row lies in one of
+  // two records, and its inputs are those of lane groups lg and lg + 2 of the record.
+  const uint8_t* wp[CT];
+  uint32_t wo[CT], so[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int first = min((tile0 + c) * BL, n_tiles - 1);
+    const uint32_t second = lm >= 16 && first + 1 < n_tiles ? (uint32_t)g.chunks * MX_REC : 0;
+    wp[c] = g.w + (int64_t)first * g.chunks * MX_REC;
+    wo[c] = second + (lg * 16 + lm % 16) * 16;
+    so[c] = second + lm % 16 * 4;
+  }
+
+  Acc acc[RT][CT];
+#pragma unroll
+  for (int r = 0; r < RT; ++r)
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+      for (int q = 0; q < 4 * AQ; ++q) acc[r][c][q] = 0.f;
+
+  const char* xp = (const char*)((const E*)g.x + (int64_t)row0 * g.x_stride);
+  uint32_t xo[XU], xl[XU];
+#pragma unroll
+  for (int u = 0; u < XU; ++u) {
+    const int r = (gt + u * GT) / 16;
+    xo[u] = mx_x_offset<IN>(g, row0, r, gt % 16 * 8);
+    xl[u] = r * 256 + ((gt % 16) ^ (r & 15)) * 16;
+  }
+  auto put = [&](char* buf, const MxRaw<IN> (&x)[XU]) {
+#pragma unroll
+    for (int u = 0; u < XU; ++u) {
+      uint4 o[NP];
+      mx_planes<IN>(x[u], o);
+#pragma unroll
+      for (int p = 0; p < NP; ++p) *reinterpret_cast<uint4*>(buf + p * PLANE + xl[u]) = o[p];
+    }
+  };
+  struct Weights { uint4 w[CT][BL]; uint32_t s[CT]; };
+  auto fetch_w = [&](Weights& q, int64_t cc) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+#pragma unroll
+      for (int b = 0; b < BL; ++b) q.w[c][b] = mx_fetch_w(wp[c] + cc * MX_REC + b * 512, wo[c]);
+      q.s[c] = mx_fetch_s(wp[c] + cc * MX_REC, so[c]);
+    }
+  };
+  // Fragments of the rows are read MX_AHEAD before their products and the next step's weights are widened among them:
+  // left to itself the compiler reads each into the same registers right before its use and waits for the LDS every time.
+  auto multiply = [&](const char* buf, const Weights& q) {
+    constexpr int NF = KS * RT * NP, FD = MX_AHEAD;
+    auto frag = [&](int f) {                                 // instruction, row tile, term: the smaller terms first
+      const int i = f / (RT * NP), r = f / NP % RT, p = NP - 1 - f % NP;
+      return *reinterpret_cast<const uint4*>(buf + p * PLANE + (r * T + lm) * 256 + (((64 / T * i + lg) ^ (lm & 15)) * 16));
+    };
+    auto widen = [&](int c, int i) { return mx_widen<IN>(word(q.w[c][i % BL], i / BL), q.s[c], i / BL); };
+    uint4 xa[FD + 1], wf[2][CT];
+#pragma unroll
+    for (int f = 0; f < FD; ++f) xa[f] = frag(f);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) wf[0][c] = widen(c, 0);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      const int i = f / (RT * NP), r = f / NP % RT, at = f % (RT * NP);
+      if (f + FD < NF) xa[(f + FD) % (FD + 1)] = frag(f + FD);
+      if (i + 1 < KS) {
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+          if (c * (RT * NP) / CT == at) wf[(i + 1) & 1][c] = widen(c, i + 1);
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) acc[r][c] = mx_mfma_t<IN, T>(wf[i & 1][c], xa[f % (FD + 1)], acc[r][c]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  MxRaw<IN> xn[XU];
+  const int full = g.n_in / 128, trips = (full + KW - 1) / KW;            // chunks without an end in them
+  auto fetch = [&](Weights& q, int chunk) {
+    const int64_t cc = min(chunk, full - 1);                              // past the end: requested, not used
+#pragma unroll
+    for (int u = 0; u < XU; ++u) xn[u] = mx_fetch<IN>(g, xp + cc * (128 * (int)sizeof(E)), xo[u]);
+    fetch_w(q, cc);
+  };
+  auto step = [&](char* buf, const Weights& now, Weights& next, int t) {
+    put(buf, xn);
+    fetch(next, (t + 1) * KW + kw);
+    wait_lds();
+    if (KW == 1 || t * KW + kw < full) multiply(buf, now);
+  };
+  int t = 0;
+  if (full > 0) {
+    Weights a, b;
+    fetch(a, kw);
+    for (; t + 2 <= trips; t += 2) {
+      step(xs, a, b, t);
+      step(xs + BUF, b, a, t + 1);
+    }
+    if (t < trips) { step(xs, a, b, t); ++t; }
+  }
+  if (IN != MX_IN_PLANES && full < g.chunks) {               // the last chunk ends early
+    char* buf = xs + (t & 1) * BUF;
+    Weights q;
+    if (kw == 0) {
+#pragma unroll
+      for (int u = 0; u < XU; ++u) xn[u] = mx_fetch_some<IN>(xp + (int64_t)full * (128 * (int)sizeof(E)), xo[u], g.n_in - full * 128 - gt % 16 * 8);
+      put(buf, xn);
+      fetch_w(q, full);
+    }
+    wait_lds();
+    if (kw == 0) multiply(buf, q);
   }
 
   if constexpr (KW > 1) {                                  // the groups' sums, added in their order
     ts_f32x4* red = reinterpret_cast<ts_f32x4*>(smem);
-    constexpr int PER = WR * WC * CT * RT * 64;
+    constexpr int PER = WC * CT * RT * AQ * 64;
+    auto part = [&](int r, int c, int q) { return ((wc * RT + r) * CT + c) * AQ * 64 + q * 64 + lane; };
+    __syncthreads();
     if (kw > 0) {
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) red[(kw - 1) * PER + ((wave * CT + c) * RT + r) * 64 + lane] = acc[c][r];
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int q = 0; q < AQ; ++q) red[(kw - 1) * PER + part(r, c, q)] = ts_f32x4{acc[r][c][4 * q], acc[r][c][4 * q + 1], acc[r][c][4 * q + 2], acc[r][c][4 * q + 3]};
     }
     __syncthreads();
     if (kw > 0) return;
+#pragma unroll
     for (int o = 0; o < KW - 1; ++o)
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int r = 0; r < RT; ++r) acc[c][r] += red[o * PER + ((wave * CT + c) * RT + r) * 64 + lane];
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int q = 0; q < AQ; ++q) {
+            const ts_f32x4 v = red[o * PER + part(r, c, q)];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[r][c][4 * q + j] += v[j];
+          }
   }
-
-  // a lane holds columns 4 lg .. + 3 of each column tile, of row lm of each row tile
+  // a lane holds, of row lm of each row tile, columns 8 q + 4 lg .. + 3 of each column tile (T = 16: q = 0, four groups)
+  auto four = [](const Acc& a, int q) { return ts_f32x4{a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]}; };
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
-    const int row = row0 + (wr * RT + r) * 16 + lm;
-    if (row >= g.rows) continue;
-    if constexpr (OUT == MX_OUT_SWIGLU) {
+    const int row = row0 + r * T + lm;
+    if constexpr (OUT == MX_OUT_SWIGLU) {                    // tiles of 16 alternate: gate and up of the same features
+      if constexpr (T == 16) {
 #pragma unroll
-      for (int c = 0; c < CT; c += 2) {                    // tiles alternate: gate and up of the same 16 features
-        if (tile0 + c >= n_tiles) continue;
-        float v[4];
+        for (int c = 0; c < CT; c += 2) mx_emit_swiglu(g, row, (tile0 + c) * 8 + 4 * lg, acc[r][c], acc[r][c + 1]);
+      } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float gate = acc[c][r][j];
-          v[j] = gate / (1.f + __expf(-gate)) * acc[c + 1][r][j];
-        }
-        st_act_planes4((f16_t*)g.y + (int64_t)row * g.y_stride + (tile0 + c) * 8 + 4 * lg, g.y_plane, v[0], v[1], v[2], v[3], g.sat);
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) mx_emit_swiglu(g, row, (tile0 + c) * 16 + 8 * q + 4 * lg, four(acc[r][c], q), four(acc[r][c], q + 2));
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        const int n = (tile0 + c) * 16 + 4 * lg;
-        const ts_f32x4 v = acc[c][r];
-        if (n >= g.n_out) continue;
-        if (g.y_f32) {
-          float* p = (float*)g.y + (int64_t)row * g.y_stride + n;
-          if (g.vec_y && n + 4 <= g.n_out) *reinterpret_cast<ts_f32x4*>(p) = v;
-          else
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) if (n + j < g.n_out) p[j] = v[j];
-        } else {
-          bf16_t* p = (bf16_t*)g.y + (int64_t)row * g.y_stride + n;
-          const uint32_t a = __builtin_bit_cast(uint32_t, to_bf16x2(v[0], v[1])), b = __builtin_bit_cast(uint32_t, to_bf16x2(v[2], v[3]));
-          if (g.vec_y && n + 4 <= g.n_out) *reinterpret_cast<uint2*>(p) = make_uint2(a, b);
-          else
-#pragma unroll
-            for (int j = 0; j < 4; ++j) if (n + j < g.n_out) p[j] = (bf16_t)((j < 2 ? a : b) >> 16 * (j & 1));
-        }
-      }
+        for (int q = 0; q < AQ; ++q) mx_emit(g, row, (tile0 + c) * T + 8 * q + 4 * lg, four(acc[r][c], q));
     }
   }
 }
 
-template <int IN, int OUT, int RT, int CT, int WR, int WC, int KW>
+template <int IN, int OUT, int RT, int CT, int KW, int UC>
+static void mx_launch_few(hipStream_t s, const MxArgs& g) {
+  k_mx_few<IN, OUT, RT, CT, KW, UC><<<dim3((g.n_out + 16 * CT - 1) / (16 * CT), (g.rows + 16 * RT - 1) / (16 * RT)), KW * 64, 0, s>>>(g);
+}
+template <int IN, int OUT, int T, int RT, int CT, int WC, int KW>
 static void mx_launch(hipStream_t s, const MxArgs& g) {
-  constexpr int MT = WR * RT * 16, NT = WC * CT * 16;
-  k_mx_project<IN, OUT, RT, CT, WR, WC, KW><<<dim3((g.n_out + NT - 1) / NT, (g.rows + MT - 1) / MT), WR * WC * KW * 64, 0, s>>>(g);
+  constexpr int MT = RT * T, NT = WC * CT * T;
+  k_mx_rows<IN, OUT, T, RT, CT, WC, KW><<<dim3((g.n_out + NT - 1) / NT, (g.rows + MT - 1) / MT), WC * KW * 64, 0, s>>>(g);
+}
+
+// Which shape a call takes: the one whose rounds of workgroups (256 CUs) times the time of a round is least.  The times are
+// microseconds of one round at 4096 inputs, measured between events with a quarter of the CUs to all of them at work;
+// all shapes scale alike with the inputs.  For 2, 3, 4, 5 row tiles of 16 (more rows: blocks of 4 tiles):
+//   bf16 rows   32 columns  6.8   8.7  12.1  13.0     64 columns  7.9  10.0  12.8  14.7     128 columns 11.5  14.8  17.3  20.8
+//   fp32 rows               -                                    24.8  35.3  45.8  52                   35    47    61.6  73
+//   planes                  -                                    14.7  20.7  26.6  32                   20.5  28.5  36    43
+// 64 rows x 256 columns, T = 32: 30.5, 84, 55.  Shapes without LDS staging (shares of a round count, they are bound by
+// the rows' way through the caches): 16 rows x 16 columns 6.6, 11.2, 7.5; 32 x 32: -, 20.5, 12.5.
+// 65 rows x 4096 inputs, 28672 columns: 128 columns wide 22.3 us, 64 wide 29.8, 32 wide 47.4, 256 wide 31.6; 4096
+// columns: 32 wide 13.0, 64 wide 14.7, 128 wide 20.9.
+enum { MX_DIRECT, MX_DIRECT2, MX_N32, MX_N64, MX_N128, MX_N256 };
+struct MxPlan { int shape, rt; };
+template <int IN, int OUT>
+static MxPlan mx_plan(int rows, int n_out) {
+  static constexpr float round_us[3][3][4] = {{{6.8f, 8.7f, 12.1f, 13.0f}, {7.9f, 10.0f, 12.8f, 14.7f}, {11.5f, 14.8f, 17.3f, 20.8f}},
+                                              {{0, 0, 0, 0}, {24.8f, 35.3f, 45.8f, 52.f}, {35.f, 47.f, 61.6f, 73.f}},
+                                              {{0, 0, 0, 0}, {14.7f, 20.7f, 26.6f, 32.f}, {20.5f, 28.5f, 36.f, 43.f}}};
+  static constexpr float direct_us[3] = {6.6f, 11.2f, 7.5f}, direct2_us[3] = {1e9f, 20.5f, 12.5f}, wide_us[3] = {30.5f, 84.f, 55.f};
+  const int rt = rows > 80 ? 4 : std::max(2, (rows + 15) / 16);
+  auto groups = [&](int mt, int nt) { return (float)((rows + mt - 1) / mt) * (float)((n_out + nt - 1) / nt) / 256.f; };
+  MxPlan best{MX_N256, rt};
+  float least = ceilf(groups(64, 256)) * wide_us[IN];
+  auto offer = [&](int shape, float cost) { if (cost < least) { least = cost; best.shape = shape; } };
+  for (int w = IN == MX_IN_BF16 ? 0 : 1; w < 3; ++w)
+    if (OUT == MX_OUT_ROWS || w == 2) offer(MX_N32 + w, ceilf(groups(16 * rt, 32 << w)) * round_us[IN][w][rt - 2]);
+  if (OUT == MX_OUT_ROWS) offer(MX_DIRECT, std::max(1.f, groups(16, 16)) * direct_us[IN]);
+  if (IN != MX_IN_BF16) offer(MX_DIRECT2, std::max(1.f, groups(32, 32)) * direct2_us[IN]);
+  return best;
+}
+
+template <int IN, int OUT, int RT>
+static void mx_project_tiles(hipStream_t s, const MxArgs& g, int shape) {
+  constexpr int K64 = IN == MX_IN_BF16 ? 4 : IN == MX_IN_F32 ? 1 : 2, K128 = IN == MX_IN_BF16 ? 2 : 1;
+  if constexpr (OUT == MX_OUT_ROWS && IN == MX_IN_BF16) if (shape == MX_N32) return mx_launch<IN, OUT, 16, RT, 1, 2, 4>(s, g);
+  if constexpr (OUT == MX_OUT_ROWS) if (shape == MX_N64) return mx_launch<IN, OUT, 16, RT, 1, 4, K64>(s, g);
+  mx_launch<IN, OUT, 16, RT, 2, 4, K128>(s, g);
 }
 
 template <int IN, int OUT>
 static void mx_project(hipStream_t s, const MxArgs& g) {
-  if (g.rows <= 16) mx_launch<IN, OUT, 1, 2, 1, 1, 4>(s, g);
-  else if (g.rows <= 48) mx_launch<IN, OUT, 3, 2, 1, 2, 2>(s, g);
-  else if (g.rows <= 80) mx_launch<IN, OUT, 5, 2, 1, 2, 2>(s, g);
-  else mx_launch<IN, OUT, 4, 4, 2, 2, 1>(s, g);
+  if (g.rows <= 16) {
+    // one column tile a workgroup where that is one round at most: a row of 4096 inputs, 4096 columns 3.7 us (two tiles
+    // 4.2), 6144 columns 5.7 (4.7), 28672 columns 13.6 (12.0)
+    if constexpr (OUT == MX_OUT_ROWS) if (g.n_out <= 256 * 16) return mx_launch_few<IN, OUT, 1, 1, 8, 1>(s, g);
+    return mx_launch_few<IN, OUT, 1, 2, 8, 1>(s, g);
+  }
+  const MxPlan p = mx_plan<IN, OUT>(g.rows, g.n_out);
+  if constexpr (OUT == MX_OUT_ROWS) if (p.shape == MX_DIRECT) return mx_launch_few<IN, OUT, 1, 1, 8, 1>(s, g);
+  if constexpr (IN != MX_IN_BF16) if (p.shape == MX_DIRECT2) return mx_launch_few<IN, OUT, 2, 2, 8, 1>(s, g);
+  if (p.shape == MX_N256) return mx_launch<IN, OUT, 32, 2, 2, 4, 1>(s, g);
+  if (p.rt == 2) mx_project_tiles<IN, OUT, 2>(s, g, p.shape);
+  else if (p.rt == 3) mx_project_tiles<IN, OUT, 3>(s, g, p.shape);
+  else if (p.rt == 4) mx_project_tiles<IN, OUT, 4>(s, g, p.shape);
+  else mx_project_tiles<IN, OUT, 5>(s, g, p.shape);
 }
 
 // ---------------------------------------------------------------------------------
@@ -474,8 +737,8 @@ extern "C" ts_status ts_mx_dequantize(const uint8_t* codes, const uint8_t* scale
 }
 
 static ts_status mx_check_shape(const char* call, int32_t n_out, int32_t n_in) {
-  if (n_out < 1 || n_in < 1 || n_out > (1 << 24) || n_in > (1 << 24))
-    return ts_fail(TS_ERR_INVALID_ARG, "%s: a matrix of %d x %d (both must lie in [1, 2^24])", call, n_out, n_in);
+  if (n_out < 1 || n_in < 1 || n_out > (1 << 24) || n_in > (1 << 22))
+    return ts_fail(TS_ERR_INVALID_ARG, "%s: a matrix of %d x %d (at least 1 x 1, at most 2^24 x 2^22)", call, n_out, n_in);
   return TS_OK;
 }
 
@@ -508,6 +771,7 @@ extern "C" ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_
   if (rows < 0 || rows > (1 << 22)) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: %lld rows outside [0, 2^22]", (long long)rows);
   if (rows == 0) return TS_OK;
   if (!packed || !x || !y) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: null argument");
+  if (rows > 1 && x_stride > (1 << 22)) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: rows %lld values apart (at most 2^22)", (long long)x_stride);
   if (x_stride < n_in || y_stride < n_out)
     return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: row strides %lld, %lld below the rows of %d, %d", (long long)x_stride, (long long)y_stride, n_in, n_out);
   const int esz = ops_esz(dtype);
@@ -521,8 +785,6 @@ extern "C" ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_
   g.x = x; g.x_stride = x_stride;
   g.y = y; g.y_stride = y_stride; g.y_f32 = dtype == TS_DTYPE_F32;
   g.n_out = n_out; g.n_in = n_in; g.chunks = (int)mx_chunks(n_in);
-  g.vec_x = aligned_to(x, 16) && x_stride * esz % 16 == 0;
-  g.vec_y = aligned_to(y, 4 * esz) && y_stride % 4 == 0;
   g.rows = (int)rows;
   if (dtype == TS_DTYPE_BF16) mx_project<MX_IN_BF16, MX_OUT_ROWS>((hipStream_t)stream, g);
   else mx_project<MX_IN_F32, MX_OUT_ROWS>((hipStream_t)stream, g);

@@ -16,6 +16,7 @@ EXPORTS = ("ts_mx_quantize", "ts_mx_dequantize", "ts_mx_packed_bytes", "ts_mx_pa
            "ts_kv_extend", "ts_kv_append", "ts_kv_attend", "ts_kv_attend_workspace")
 
 _DTYPES = {torch.float32: TS_DTYPE_F32, torch.bfloat16: TS_DTYPE_BF16}
+_RECORD = 16 * 4 * 17                                      # bytes of packed weights per 16 rows and 128 columns
 
 
 class ts_kv_pages(C.Structure):
@@ -64,8 +65,11 @@ def _load():
     return lib
 
 
+_stream_of = torch._C._cuda_getCurrentRawStream           # the current stream's handle without a Python object around it
+
+
 def _stream(t):
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return _stream_of(t.get_device())
 
 
 def _refuse(what, *args):
@@ -73,16 +77,21 @@ def _refuse(what, *args):
 
 
 def _rows(t, name, cols=None, dtype=None):
-    """A matrix whose rows are contiguous; the distance between rows is free."""
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        _refuse("%s: a matrix with contiguous rows is needed, got shape %s, strides %s", name, tuple(t.shape), t.stride())
-    if cols is not None and t.shape[1] != cols:
-        _refuse("%s: rows of %d values are needed, got %d", name, cols, t.shape[1])
+    """A matrix whose rows are contiguous; the distance between rows is free.  (address, distance)"""
+    shape = t.shape
+    if len(shape) != 2:
+        _refuse("%s: a matrix with contiguous rows is needed, got shape %s", name, tuple(shape))
+    n, width = shape
+    dist, step = t.stride()
+    if (step != 1 and width > 1) or (dist < width and n > 1):
+        _refuse("%s: a matrix with contiguous rows is needed, got shape %s, strides %s", name, tuple(shape), t.stride())
+    if cols is not None and width != cols:
+        _refuse("%s: rows of %d values are needed, got %d", name, cols, width)
     if t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
         raise TypeError("%s: %s is needed, got %s" % (name, dtype or "float32 or bfloat16", t.dtype))
     if not t.is_cuda:
         _refuse("%s is not on a GPU", name)
-    return t.data_ptr(), max(t.stride(0), t.shape[1])
+    return t.data_ptr(), dist if dist > width else width
 
 
 def _ints(t, name, n=None):
@@ -105,9 +114,9 @@ def ts_mx_quantize(x, codes=None, scales=None):
     rows, cols = x.shape
     blocks = (cols + 31) // 32
     if codes is None:
-        codes = torch.empty((rows, 16 * blocks), dtype=torch.uint8, device=x.device)
+        codes = x.new_empty((rows, 16 * blocks), dtype=torch.uint8)
     if scales is None:
-        scales = torch.empty((rows, blocks), dtype=torch.uint8, device=x.device)
+        scales = x.new_empty((rows, blocks), dtype=torch.uint8)
     binding._check(lib.ts_mx_quantize(px, _DTYPES[x.dtype], rows, cols, stride, _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks)), _stream(x)))
     return codes, scales
 
@@ -118,7 +127,7 @@ def ts_mx_dequantize(codes, scales, cols, dtype=torch.float32, out=None):
     rows, blocks = codes.shape[0], (cols + 31) // 32
     pc, ps = _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks))
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+        out = codes.new_empty((rows, cols), dtype=dtype)
     po, stride = _rows(out, "out", cols, dtype)
     if out.shape[0] != rows:
         _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
@@ -149,14 +158,17 @@ def ts_mx_project(packed, n_out, x, out=None):
     lib = _load()
     px, xs = _rows(x, "x")
     rows, n_in = x.shape
-    if n_in < 1 or n_out < 1 or _bytes(packed, "packed") and packed.numel() != ts_mx_packed_bytes(n_out, n_in):
+    pw = _bytes(packed, "packed")
+    if n_in < 1 or n_out < 1 or packed.numel() != -(-n_out // 16) * -(-n_in // 128) * _RECORD:
         _refuse("packed: not the weights of a [%d][%d] matrix", n_out, n_in)
     if out is None:
-        out = torch.empty((rows, n_out), dtype=x.dtype, device=x.device)
-    po, os_ = _rows(out, "out", n_out, x.dtype)
-    if out.shape[0] != rows:
-        _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
-    binding._check(lib.ts_mx_project(packed.data_ptr(), n_out, n_in, px, _DTYPES[x.dtype], rows, xs, po, os_, _stream(x)))
+        out = x.new_empty((rows, n_out))
+        po, os_ = out.data_ptr(), n_out
+    else:
+        po, os_ = _rows(out, "out", n_out, x.dtype)
+        if out.shape[0] != rows:
+            _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
+    binding._check(lib.ts_mx_project(pw, n_out, n_in, px, _DTYPES[x.dtype], rows, xs, po, os_, _stream(x)))
     return out
 
 
@@ -258,10 +270,10 @@ def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=N
     heads = q.shape[1] // hd
     a.n_seqs, a.max_len, a.window, a.n_q_heads, a.dtype = n, max_len, window, heads, _DTYPES[q.dtype]
     if out is None:
-        out = torch.empty((n, heads * hd), dtype=q.dtype, device=q.device)
+        out = q.new_empty((n, heads * hd))
     a.out, a.out_stride = _rows(out, "out", heads * hd, q.dtype)
     if lse is None:
-        lse = torch.empty((n, heads), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((n, heads), dtype=torch.float32)
     if out.shape[0] != n or tuple(lse.shape) != (n, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
         _refuse("out and lse: [%d][%d] and contiguous fp32 [%d][%d] are needed", n, heads * hd, n, heads)
     a.lse = lse.data_ptr()
