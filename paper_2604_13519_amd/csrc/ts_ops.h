@@ -29,13 +29,16 @@ inline bool ops_dtype_ok(int32_t dtype) { return dtype == TS_DTYPE_F32 || dtype 
 inline int ops_esz(int32_t dtype) { return dtype == TS_DTYPE_BF16 ? 2 : 4; }
 inline bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
-// 16 and 8 bytes from or to the place of any element: the vector accesses of gfx950 need no more alignment than that
+// 16, 8 and 4 bytes from or to the place of any element: the vector accesses of gfx950 need no more alignment than that
 typedef uint32_t ts_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t ts_u32x2 __attribute__((ext_vector_type(2)));
 typedef ts_u32x4 ts_u32x4_any __attribute__((aligned(2)));
 typedef ts_u32x2 ts_u32x2_any __attribute__((aligned(2)));
 __device__ __forceinline__ uint4 load16(const void* p) { return __builtin_bit_cast(uint4, (ts_u32x4)*reinterpret_cast<const ts_u32x4_any*>(p)); }
 __device__ __forceinline__ uint2 load8(const void* p) { return __builtin_bit_cast(uint2, (ts_u32x2)*reinterpret_cast<const ts_u32x2_any*>(p)); }
+typedef uint32_t ts_u32_any __attribute__((aligned(2)));
+__device__ __forceinline__ uint32_t load4(const void* p) { return *reinterpret_cast<const ts_u32_any*>(p); }
+__device__ __forceinline__ void store4(void* p, uint32_t v) { *reinterpret_cast<ts_u32_any*>(p) = v; }
 __device__ __forceinline__ void store16(void* p, uint4 v) { *reinterpret_cast<ts_u32x4_any*>(p) = __builtin_bit_cast(ts_u32x4, v); }
 __device__ __forceinline__ void store8(void* p, uint2 v) { *reinterpret_cast<ts_u32x2_any*>(p) = __builtin_bit_cast(ts_u32x2, v); }
 

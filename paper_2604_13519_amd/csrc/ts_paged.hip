@@ -18,50 +18,60 @@ template <typename T> __device__ __forceinline__ float widen(T v) {
   if constexpr (sizeof(T) == 2) return bf16_to_f32(v);
   else return v;
 }
-// n consecutive elements, 16-byte accesses where the caller says so
+// N consecutive elements in vectors
 template <int N, typename T>
-__device__ __forceinline__ void load_n(const T* p, bool vec, float (&v)[N]) {
-  if (vec) {
-    alignas(16) uint32_t u[N * sizeof(T) / 4];
-    static_assert(N * sizeof(T) == 8 || N * sizeof(T) % 16 == 0, "whole vectors");
-    if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2*>(u) = *reinterpret_cast<const uint2*>(p);
-    else
+__device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
+  uint32_t u[N * sizeof(T) / 4];
+  if constexpr (N * sizeof(T) == 4) u[0] = load4(p);
+  else if constexpr (N * sizeof(T) == 8) { const uint2 w = load8(p); u[0] = w.x; u[1] = w.y; }
+  else
 #pragma unroll
-      for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(u)[i] = reinterpret_cast<const uint4*>(p)[i];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
-      else v[i] = __uint_as_float(u[i]);
+    for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) {
+      const uint4 w = load16((const char*)p + 16 * i);
+      u[4 * i] = w.x; u[4 * i + 1] = w.y; u[4 * i + 2] = w.z; u[4 * i + 3] = w.w;
     }
-  } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = widen(p[i]);
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+    else v[i] = __uint_as_float(u[i]);
   }
 }
 template <int N, typename T>
-__device__ __forceinline__ void store_n(T* p, bool vec, const float (&v)[N]) {
-  if (vec) {
-    alignas(16) uint32_t u[N * sizeof(T) / 4];
-    static_assert(N * sizeof(T) == 8 || N * sizeof(T) % 16 == 0, "whole vectors");
+__device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
+  uint32_t u[N * sizeof(T) / 4];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if constexpr (sizeof(T) == 2) { if (!(i & 1)) u[i / 2] = (uint32_t)f32_to_bf16(v[i]) | (uint32_t)f32_to_bf16(v[i + 1]) << 16; }
-      else u[i] = __float_as_uint(v[i]);
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(T) == 2) { if (!(i & 1)) u[i / 2] = __builtin_bit_cast(uint32_t, to_bf16x2(v[i], v[i + 1])); }
+    else u[i] = __float_as_uint(v[i]);
+  }
+  if constexpr (N * sizeof(T) == 4) store4(p, u[0]);
+  else if constexpr (N * sizeof(T) == 8) store8(p, make_uint2(u[0], u[1]));
+  else
+#pragma unroll
+    for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) store16((char*)p + 16 * i, make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]));
+}
+
+// those of positions p0 .. p0 + N - 1 that lie in [lo, hi), in as few pieces as there are
+template <int N, typename T>
+__device__ __forceinline__ void store_some(T* p, int p0, int lo, int hi, const float* v) {
+  if (lo <= p0 && p0 + N <= hi) {
+    if constexpr (N == 1) st_from_f32(p, v[0]);
+    else {
+      float w[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = v[i];
+      store_n<N>(p, w);
     }
-    if constexpr (N * sizeof(T) == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<uint2*>(u);
-    else
-#pragma unroll
-      for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) reinterpret_cast<uint4*>(p)[i] = reinterpret_cast<uint4*>(u)[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) st_from_f32(p + i, v[i]);
+  } else if constexpr (N > 1) {
+    if (lo < p0 + N / 2) store_some<N / 2>(p, p0, lo, hi, v);
+    if (hi > p0 + N / 2) store_some<N / 2>(p + N / 2, p0 + N / 2, lo, hi, v + N / 2);
   }
 }
 
 struct AppendArgs {
   ts_kv_append_args a;
   double log2_theta;                     // rope_theta > 0
-  int vec_q, vec_k, vec_out;
+  int window;                            // rows a workgroup looks for pages in
 };
 
 // the last sequence whose first row is not behind `row`, -1 if none: 64 offsets at a time, one per lane
@@ -80,83 +90,132 @@ __device__ __forceinline__ int seq_of_row(const int32_t* offsets, int n, int row
   }
 }
 
+// `cnt` rows from `row` on into slots `slot`, ... of a page, heads [head0, head1) of (queries, keys, values)
+struct AppendPage { int row, cnt, slot, page, head0, head1, hq, hkv; int64_t pos; };
+
+// Queries and keys, in pieces of VE pairs.  A thread requests all its pieces (more than four: in batches) before it stores
+// one - the stores may alias the loads for all the compiler knows - and the sines are worked out while they come.
+template <typename TI, typename TC, int HD>
+__device__ __forceinline__ void append_turned(const AppendArgs& g, const AppendPage& at, const double* freq, float2* cs) {
+  constexpr int VE = HD >= 32 && sizeof(TI) == 2 && sizeof(TC) == 2 ? 8 : 4, HALF = HD / 2, PIECES = HALF / VE, BATCH = 4;
+  const ts_kv_append_args& a = g.a;
+  const int tid = threadIdx.x, cnt = at.cnt, n = (min(at.head1, at.hq + at.hkv) - at.head0) * cnt * PIECES;
+  const int by_cnt = (65536 + cnt - 1) / cnt;                // divides what is below 16 * APPEND_HEADS by cnt
+  const bool turn = a.rope_theta > 0.f;
+  for (int i0 = 0; i0 < n; i0 += BATCH * APPEND_THREADS) {
+    float x[BATCH][VE], y[BATCH][VE];
+    int rr[BATCH], hh[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i0 + b * APPEND_THREADS >= n) break;
+      const int i = min(i0 + b * APPEND_THREADS + tid, n - 1), c = i % PIECES, hr = i / PIECES;
+      hh[b] = hr * by_cnt >> 16;
+      rr[b] = hr - hh[b] * cnt;
+      hh[b] += at.head0;
+      const int64_t row = at.row + rr[b];
+      const TI* src = hh[b] < at.hq ? (const TI*)a.q + row * a.q_stride + hh[b] * HD : (const TI*)a.k + row * a.k_stride + (hh[b] - at.hq) * HD;
+      load_n<VE>(src + c * VE, x[b]);
+      load_n<VE>(src + HALF + c * VE, y[b]);
+    }
+    if (turn && i0 == 0) {
+      for (int i = tid; i < cnt * HALF; i += APPEND_THREADS) {
+        const double t = freq[i % HALF] * (double)(at.pos + i / HALF), rest = t - rint(t);
+        float sn, c;
+        sincospif(2.f * (float)rest, &sn, &c);
+        cs[i] = make_float2(c, sn);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = i0 + b * APPEND_THREADS + tid, c = i % PIECES;
+      if (i >= n) continue;
+      if (turn) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const float2 w = cs[rr[b] * HALF + c * VE + e];
+          const float u = x[b][e] * w.x - y[b][e] * w.y;
+          y[b][e] = y[b][e] * w.x + x[b][e] * w.y;
+          x[b][e] = u;
+        }
+      }
+      if (hh[b] < at.hq) {
+        TI* dst = (TI*)a.q_out + (int64_t)(at.row + rr[b]) * a.q_out_stride + hh[b] * HD;
+        store_n<VE>(dst + c * VE, x[b]);
+        store_n<VE>(dst + HALF + c * VE, y[b]);
+      } else {
+        TC* dst = (TC*)a.pages.k + (((int64_t)at.page * at.hkv + (hh[b] - at.hq)) * 16 + at.slot + rr[b]) * HD;
+        store_n<VE>(dst + c * VE, x[b]);
+        store_n<VE>(dst + HALF + c * VE, y[b]);
+      }
+    }
+  }
+}
+
+template <typename TI, typename TC, int HD>
+__device__ __forceinline__ void append_values(const AppendArgs& g, const AppendPage& at) {
+  const ts_kv_append_args& a = g.a;
+  const int tid = threadIdx.x, cnt = at.cnt, slot = at.slot, row = at.row, page = at.page, hkv = at.hkv, turned = at.hq + at.hkv, head0 = at.head0, head1 = at.head1;
+  // values: a thread writes the positions of a dimension, of two for rows of bf16.  All rows are requested at once (what
+  // lies outside the new ones is the nearest of them, not stored); they go in vectors, cut at the ends.
+  constexpr int DV = 4 / sizeof(TI), SV = 16 / sizeof(TC);
+  const int val0 = max(head0, turned), end = slot + cnt;
+  for (int i = tid; i < (head1 - val0) * HD / DV; i += APPEND_THREADS) {
+    const int h = val0 - turned + i * DV / HD, d = i * DV % HD;
+    const TI* src = (const TI*)a.v + (int64_t)row * a.v_stride + h * HD + d;
+    TC* dst = (TC*)a.pages.v + (((int64_t)page * hkv + h) * HD + d) * 16;
+    if (cnt == 1) {
+      float w[DV];
+      load_n<DV>(src, w);
+#pragma unroll
+      for (int e = 0; e < DV; ++e) st_from_f32(dst + e * 16 + slot, w[e]);
+      continue;
+    }
+    float v[DV][16];
+#pragma unroll
+    for (int p = 0; p < 16; ++p) {
+      float w[DV];
+      load_n<DV>(src + (int64_t)min(max(p - slot, 0), cnt - 1) * a.v_stride, w);
+#pragma unroll
+      for (int e = 0; e < DV; ++e) v[e][p] = w[e];
+    }
+#pragma unroll
+    for (int p0 = 0; p0 < 16; p0 += SV)
+#pragma unroll
+      for (int e = 0; e < DV; ++e) store_some<SV>(dst + e * 16 + p0, p0, slot, end, &v[e][p0]);
+  }
+}
+
 // TI rows' element, TC cache's element
 template <typename TI, typename TC, int HD>
 __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
-  constexpr int VE = HD >= 32 && sizeof(TI) == 2 && sizeof(TC) == 2 ? 8 : 4, HALF = HD / 2, PIECES = HALF / VE;
+  constexpr int HALF = HD / 2;
   __shared__ float2 cs[16 * HALF];
+  __shared__ double freq[HALF];
   const ts_kv_append_args& a = g.a;
-  const int row = blockIdx.x;
-  const int seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
-  if (seq < 0 || seq >= a.n_seqs) return;
-  const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.n_rows);
-  const int64_t pos = (int64_t)a.lengths[seq] + row - first;
-  if (pos < 0 || pos >= (int64_t)a.table_width * 16 || row >= end) return;
-  const int slot = (int)(pos & 15);
-  if (row != max(first, 0) && slot != 0) return;                     // the page's first new row takes this one along
-  const int cnt = min(16 - slot, end - row);
-  const int page = a.table[(int64_t)seq * a.table_stride + pos / 16];
-  if (page < 0 || page >= a.pages.n_pages) return;
   const int tid = threadIdx.x, hkv = a.pages.n_kv_heads, hq = a.q ? a.n_q_heads : 0;
   const int head0 = blockIdx.y * APPEND_HEADS, turned = hq + hkv, head1 = min(head0 + APPEND_HEADS, turned + hkv);
+  const bool turn = a.rope_theta > 0.f && head0 < turned;
+  if (turn && tid < HALF) freq[tid] = exp2(g.log2_theta * (-2.0 * tid / HD)) * 0.15915494309189535;      // turns per position
 
-  const bool turn = a.rope_theta > 0.f;
-  if (turn && head0 < turned) {
-    for (int i = tid; i < cnt * HALF; i += APPEND_THREADS) {
-      const int r = i / HALF, j = i % HALF;
-      const double f = exp2(g.log2_theta * (-2.0 * j / HD)) * 0.15915494309189535;       // turns per position
-      const double t = f * (double)(pos + r), rest = t - rint(t);
-      float s, c;
-      sincospif(2.f * (float)rest, &s, &c);
-      cs[i] = make_float2(c, s);
-    }
-    __syncthreads();
-  }
-
-  // queries and keys: pieces of VE pairs
-  const int rot1 = min(head1, turned);
-  for (int i = tid; i < (rot1 - head0) * cnt * PIECES; i += APPEND_THREADS) {
-    const int c = i % PIECES, r = i / PIECES % cnt, h = head0 + i / PIECES / cnt;
-    const bool is_q = h < hq;
-    const TI* src = is_q ? (const TI*)a.q + (int64_t)(row + r) * a.q_stride + h * HD : (const TI*)a.k + (int64_t)(row + r) * a.k_stride + (h - hq) * HD;
-    float x[VE], y[VE];
-    const bool vec = is_q ? g.vec_q : g.vec_k;
-    load_n<VE>(src + c * VE, vec, x);
-    load_n<VE>(src + HALF + c * VE, vec, y);
-    if (turn) {
-#pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        const float2 w = cs[r * HALF + c * VE + e];
-        const float u = x[e] * w.x - y[e] * w.y;
-        y[e] = y[e] * w.x + x[e] * w.y;
-        x[e] = u;
-      }
-    }
-    if (is_q) {
-      TI* dst = (TI*)a.q_out + (int64_t)(row + r) * a.q_out_stride + h * HD;
-      store_n<VE>(dst + c * VE, g.vec_out, x);
-      store_n<VE>(dst + HALF + c * VE, g.vec_out, y);
-    } else {
-      TC* dst = (TC*)a.pages.k + (((int64_t)page * hkv + (h - hq)) * 16 + slot + r) * HD;
-      store_n<VE>(dst + c * VE, true, x);
-      store_n<VE>(dst + HALF + c * VE, true, y);
-    }
-  }
-
-  // values: a thread writes a dimension's positions
-  const int val0 = max(head0, turned);
-  for (int i = tid; i < (head1 - val0) * HD; i += APPEND_THREADS) {
-    const int h = val0 - turned + i / HD, d = i % HD;
-    const TI* src = (const TI*)a.v + (int64_t)row * a.v_stride + h * HD + d;
-    TC* dst = (TC*)a.pages.v + (((int64_t)page * hkv + h) * HD + d) * 16 + slot;
-    if (cnt == 16) {
-      float v[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) v[r] = widen(src[(int64_t)r * a.v_stride]);
-      store_n<16>(dst, true, v);
-    } else {
-      for (int r = 0; r < cnt; ++r) st_from_f32(dst + r, widen(src[(int64_t)r * a.v_stride]));
-    }
+  // The page's first new row takes the others along; a workgroup takes the pages whose first new row is in its window.
+  const int window1 = min((int)(blockIdx.x + 1) * g.window, a.n_rows);
+  for (int row = blockIdx.x * g.window, cnt; row < window1; row += cnt) {
+    cnt = 1;
+    const int seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
+    if (seq < 0 || seq >= a.n_seqs) continue;
+    const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.n_rows);
+    const int64_t pos = (int64_t)a.lengths[seq] + row - first;
+    if (pos < 0 || row >= end) continue;
+    const int slot = (int)(pos & 15);
+    cnt = min(16 - slot, end - row);
+    if ((row != max(first, 0) && slot != 0) || pos >= (int64_t)a.table_width * 16) continue;
+    const int page = a.table[(int64_t)seq * a.table_stride + pos / 16];
+    if (page < 0 || page >= a.pages.n_pages) continue;
+    const AppendPage at{row, cnt, slot, page, head0, head1, hq, hkv, pos};
+    __syncthreads();                                         // freq is there, the last page's cs no longer read
+    if (head0 < turned) append_turned<TI, TC, HD>(g, at, freq, cs);
+    if (head1 > turned) append_values<TI, TC, HD>(g, at);
   }
 }
 
@@ -195,7 +254,7 @@ __device__ __forceinline__ void seen_range(const ts_kv_attend_args& a, int seq, 
 }
 
 template <typename T, typename TQ, int HD>
-__global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
+__global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int QP = BF && sizeof(TQ) == 4 ? 3 : 1;          // terms of a query
   constexpr int PP = sizeof(TQ) == 4 ? 3 : 2;                // terms of a probability (bf16 caches)
@@ -206,10 +265,11 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
   __shared__ float sm[ATT_WAVES][16], sl[ATT_WAVES][16];
   const ts_kv_attend_args& a = g.a;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 16, lg = lane / 16;
+  // neighbours take the KV heads of the same positions: a page's heads lie side by side in memory and are read together
   int id = blockIdx.x;
-  const int split = id % g.splits; id /= g.splits;
+  const int hkv = a.pages.n_kv_heads, kvh = id % hkv; id /= hkv;
   const int tile = id % g.tiles; id /= g.tiles;
-  const int hkv = a.pages.n_kv_heads, kvh = id % hkv, seq = id / hkv;
+  const int split = id % g.splits, seq = id / g.splits;
   int lo, hi, base;
   seen_range(a, seq, lo, hi, base);
   const int k0 = base + split * g.chunk, k1 = min(hi, k0 + g.chunk);
@@ -256,40 +316,42 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
   const char* vp = (const char*)a.pages.v;
   const int64_t head_bytes = (int64_t)16 * HD * sizeof(T), page_bytes = hkv * head_bytes;
 
-  for (int kb = k0 + wave * ATT_KB; kb < k1; kb += ATT_WAVES * ATT_KB) {
-    // the block's two pages; the second one may lie behind the last position
-    int pg[2];
-    pg[0] = table[kb / 16];
-    pg[1] = kb + 16 < hi ? table[kb / 16 + 1] : -1;
-    const bool ok0 = pg[0] >= 0 && pg[0] < a.pages.n_pages, ok1 = pg[1] >= 0 && pg[1] < a.pages.n_pages;
-    const int64_t off0 = (ok0 ? pg[0] : 0) * page_bytes + kvh * head_bytes, off1 = (ok1 ? pg[1] : ok0 ? pg[0] : 0) * page_bytes + kvh * head_bytes;
-
-    uint4 kf[2][KC], vf[BF ? 1 : 2][DT];
+  // A block of 32 keys: its two pages, and what a lane holds of its keys and values.
+  struct Block { uint4 k[2][KC], v[BF ? 1 : 2][DT]; bool ok0, ok1; };
+  auto pages_of = [&](int kb) {                              // the second may lie behind the last position
+    return make_int2(kb < hi ? table[kb / 16] : -1, kb + 16 < hi ? table[kb / 16 + 1] : -1);
+  };
+  auto fetch = [&](Block& f, int2 pg) {                      // pages that do not exist: another is read, and masked
+    f.ok0 = pg.x >= 0 && pg.x < a.pages.n_pages;
+    f.ok1 = pg.y >= 0 && pg.y < a.pages.n_pages;
+    const int p0 = f.ok0 ? pg.x : 0, p1 = f.ok1 ? pg.y : p0;
+    const int64_t off0 = p0 * page_bytes + kvh * head_bytes, off1 = p1 * page_bytes + kvh * head_bytes;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int key = BF ? 8 * (n / 4) + 4 * t + n % 4 : 16 * t + n;
-      const char* row = kp + (key < 16 ? off0 : off1) + (int64_t)(key % 16) * HD * sizeof(T);
+      const char* row = kp + (key < 16 ? off0 : off1) + (key % 16) * HD * (int)sizeof(T);
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         const int at = (c * 4 + lg) * 16;
-        if (HD * (int)sizeof(T) % 64 == 0 || at < HD * (int)sizeof(T)) kf[t][c] = *reinterpret_cast<const uint4*>(row + at);
-        else kf[t][c] = make_uint4(0, 0, 0, 0);
+        if (HD * (int)sizeof(T) % 64 == 0 || at < HD * (int)sizeof(T)) f.k[t][c] = *reinterpret_cast<const uint4*>(row + at);
+        else f.k[t][c] = make_uint4(0, 0, 0, 0);
       }
     }
     if constexpr (BF) {
       const char* col = vp + (lg < 2 ? off0 : off1) + (lg & 1) * 16;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) vf[0][d] = *reinterpret_cast<const uint4*>(col + (d * 16 + n) * 32);
+      for (int d = 0; d < DT; ++d) f.v[0][d] = *reinterpret_cast<const uint4*>(col + (d * 16 + n) * 32);
     } else {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          if (HD % 16 == 0 || d * 16 + n < HD) vf[t][d] = *reinterpret_cast<const uint4*>(vp + (t ? off1 : off0) + (d * 16 + n) * 64 + lg * 16);
-          else vf[t][d] = make_uint4(0, 0, 0, 0);
+          if (HD % 16 == 0 || d * 16 + n < HD) f.v[t][d] = *reinterpret_cast<const uint4*>(vp + (t ? off1 : off0) + (d * 16 + n) * 64 + lg * 16);
+          else f.v[t][d] = make_uint4(0, 0, 0, 0);
         }
     }
-
+  };
+  auto use = [&](Block& f, int kb) {
     ts_f32x4 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -299,10 +361,9 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
         if constexpr (BF) {
 #pragma unroll
           for (int p = QP - 1; p >= 0; --p)
-            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, kf[t][c]), __builtin_bit_cast(ts_bf16x8, q[p][c]), s[t], 0, 0, 0);
+            s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, f.k[t][c]), __builtin_bit_cast(ts_bf16x8, q[p][c]), s[t], 0, 0, 0);
         } else {
-          const float* kx = reinterpret_cast<const float*>(&kf[t][c]);
-          const float* qx = reinterpret_cast<const float*>(&q[0][c]);
+          const ts_f32x4 kx = __builtin_bit_cast(ts_f32x4, f.k[t][c]), qx = __builtin_bit_cast(ts_f32x4, q[0][c]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], s[t], 0, 0, 0);
         }
@@ -314,26 +375,32 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) x[4 * t + r] = s[t][r] * g.scale_log2;
-    const bool whole = kb >= lo && kb + ATT_KB <= k1 && ok0 && ok1;
-    if (!whole) {
+    if (!(kb >= lo && kb + ATT_KB <= k1 && f.ok0 && f.ok1)) {
+      auto seen = [&](int i) {
+        const int key = BF ? 8 * lg + i : 16 * (i / 4) + 4 * lg + i % 4;
+        return kb + key >= lo && kb + key < k1 && (key < 16 ? f.ok0 : f.ok1);
+      };
+      uint32_t keep[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int key = BF ? 8 * lg + i : 16 * (i / 4) + 4 * lg + i % 4, at = kb + key;
-        const bool seen = at >= lo && at < k1 && (key < 16 ? ok0 : ok1);
-        x[i] = seen ? x[i] : -INFINITY;
-        // 0 times whatever the place holds is not 0
-        if constexpr (BF) {
-          const uint32_t keep = i & 1 ? 0x0000ffffu : 0xffff0000u;
+        const bool in = seen(i);
+        x[i] = in ? x[i] : -INFINITY;
+        keep[i] = in ? 0xffffffffu : 0;
+      }
+      // 0 times whatever an unseen place holds is not 0
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&vf[0][d]) + i / 2;
-            *w = seen ? *w : *w & keep;
-          }
+      for (int d = 0; d < DT; ++d) {
+        if constexpr (BF) {
+          uint4& v = f.v[0][d];
+          v.x &= (keep[0] & 0xffff) | (keep[1] & 0xffff0000u);
+          v.y &= (keep[2] & 0xffff) | (keep[3] & 0xffff0000u);
+          v.z &= (keep[4] & 0xffff) | (keep[5] & 0xffff0000u);
+          v.w &= (keep[6] & 0xffff) | (keep[7] & 0xffff0000u);
         } else {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&vf[i / 4][d]) + i % 4;
-            *w = seen ? *w : 0u;
+          for (int t = 0; t < 2; ++t) {
+            uint4& v = f.v[t][d];
+            v.x &= keep[4 * t]; v.y &= keep[4 * t + 1]; v.z &= keep[4 * t + 2]; v.w &= keep[4 * t + 3];
           }
         }
       }
@@ -341,10 +408,10 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
     float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
     top = fmaxf(max_over_lane_groups(top), m);
     if (__ballot(top > m)) {                                 // the sums so far move to the new reference
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
-      l *= f;
+      const float w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+      l *= w;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] *= f;
+      for (int d = 0; d < DT; ++d) o[d] *= w;
       m = top;
     }
     const float ref = m == -INFINITY ? 0.f : m;
@@ -363,20 +430,52 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
         for (int p = 0; p < PP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, t[p]);
       }
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int p = PP - 1; p >= 0; --p)
 #pragma unroll
-        for (int p = PP - 1; p >= 0; --p)
-          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, vf[0][d]),
+        for (int d = 0; d < DT; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, f.v[0][d]),
                                                          __builtin_bit_cast(ts_bf16x8, make_uint4(u[p][0], u[p][1], u[p][2], u[p][3])), o[d], 0, 0, 0);
     } else {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const float* vx = reinterpret_cast<const float*>(&vf[t][d]);
+        for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vx[r], x[4 * t + r], o[d], 0, 0, 0);
-        }
+          for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(ts_f32x4, f.v[t][d])[r], x[4 * t + r], o[d], 0, 0, 0);
+    }
+  };
+  // One block's keys and values are on their way while another is used, and the pages of the one after are known.  The
+  // request is made on every path - past the end for the last block again - because the waits count the loads behind
+  // the ones they wait for: with a path that requests nothing they would wait for the request as well.
+  constexpr int STEP = ATT_WAVES * ATT_KB;
+  const int kw = k0 + wave * ATT_KB;
+  if (kw + STEP >= k1) {
+    if (kw < k1) {
+      Block f;
+      fetch(f, pages_of(kw));
+      use(f, kw);
+    }
+  } else if constexpr (BF || HD < 128) {
+    const int last = kw + (k1 - 1 - kw) / STEP * STEP;
+    Block fa, fb;
+    fetch(fa, pages_of(kw));
+    int2 next = pages_of(kw + STEP);
+    for (int kb = kw; kb < k1; kb += 2 * STEP) {
+      fetch(fb, next);
+      next = pages_of(min(kb + 2 * STEP, last));
+      use(fa, kb);
+      if (kb + STEP >= k1) break;
+      fetch(fa, next);
+      next = pages_of(min(kb + 3 * STEP, last));
+      use(fb, kb + STEP);
+    }
+  } else {                                                   // 128 fp32 dimensions do not fit twice
+    int2 next = pages_of(kw);
+    for (int kb = kw; kb < k1; kb += STEP) {
+      Block f;
+      fetch(f, next);
+      next = pages_of(kb + STEP);
+      use(f, kb);
     }
   }
 
@@ -411,39 +510,65 @@ __global__ __launch_bounds__(ATT_WAVES * 64) void k_kv_attend(AttendArgs g) {
   }
 }
 
-// The join of a sequence's splits: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A workgroup per (sequence, head);
-// HD lanes wide, the splits dealt to as many such rows of threads as fit.
+// The join of a sequence's splits: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A workgroup per (sequence, head):
+// the weights of the splits first, into the LDS, then four dimensions a thread and the splits dealt to the 1024 / HD rows
+// of threads, so that a row's reads are few and all in flight at once.
+constexpr int ATT_SPLITS = 512;                              // at most, see attend_cut
 template <typename TQ, int HD>
 __global__ __launch_bounds__(256) void k_kv_attend_join(AttendArgs g) {
-  constexpr int ROWS = 256 / HD;
-  __shared__ float sv[256], ss[ROWS];
+  constexpr int COLS = HD / 4, ROWS = 256 / COLS;
+  __shared__ float sw[ATT_SPLITS];
+  __shared__ float4 sv[256];
+  __shared__ float red[2][4];
   const ts_kv_attend_args& a = g.a;
   const int64_t row = blockIdx.x;
-  const int seq = (int)(row / a.n_q_heads), h = (int)(row % a.n_q_heads), d = threadIdx.x % HD, r = threadIdx.x / HD;
+  const int seq = (int)(row / a.n_q_heads), h = (int)(row % a.n_q_heads), tid = threadIdx.x, wave = tid / 64;
   int lo, hi, base;
   seen_range(a, seq, lo, hi, base);
   const int used = max(1, min(g.splits, (hi - base + g.chunk - 1) / g.chunk));
   const float2* ml = reinterpret_cast<const float2*>(g.part_ml) + row * g.splits;
+  float2 p[ATT_SPLITS / 256];
   float top = -INFINITY;
-  for (int i = threadIdx.x % 64; i < used; i += 64) top = fmaxf(top, ml[i].x);
-  top = wave_max(top);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float sum = 0.f, val = 0.f;
-  for (int i = r; i < used; i += ROWS) {
-    const float2 p = ml[i];
-    const float f = __builtin_amdgcn_exp2f(p.x - ref);
-    sum += f * p.y;
-    val += f * g.part_o[(row * g.splits + i) * HD + d];
-  }
-  sv[threadIdx.x] = val;
-  if (d == 0) ss[r] = sum;
-  __syncthreads();
-  if (r) return;
-  sum = val = 0.f;
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) { sum += ss[i]; val += sv[i * HD + d]; }
-  st_from_f32((TQ*)a.out + (int64_t)seq * a.out_stride + (int64_t)h * HD + d, sum == 0.f ? 0.f : val / sum);
-  if (a.lse && d == 0) a.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+  for (int i = 0; i < ATT_SPLITS / 256; ++i) {
+    const int j = i * 256 + tid;
+    p[i] = j < used ? ml[j] : make_float2(-INFINITY, 0.f);
+    top = fmaxf(top, p[i].x);
+  }
+  top = wave_max(top);
+  if (tid % 64 == 0) red[0][wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < ATT_SPLITS / 256; ++i) {
+    const int j = i * 256 + tid;
+    const float f = __builtin_amdgcn_exp2f(p[i].x - ref);
+    if (j < used) { sw[j] = f; sum += f * p[i].y; }
+  }
+  sum = wave_sum(sum);
+  if (tid % 64 == 0) red[1][wave] = sum;
+  __syncthreads();
+  sum = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  const int d = tid % COLS, r = tid / COLS;
+  const float4* part = reinterpret_cast<const float4*>(g.part_o) + row * g.splits * COLS + d;
+  float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = r; i < used; i += ROWS) {
+    const float4 v = part[(int64_t)i * COLS];
+    const float f = sw[i];
+    val.x += f * v.x; val.y += f * v.y; val.z += f * v.z; val.w += f * v.w;
+  }
+  sv[tid] = val;
+  __syncthreads();
+  if (tid >= HD) return;
+  const float* sc = reinterpret_cast<const float*>(sv);
+  float out = 0.f;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) out += sc[i * HD + tid];
+  st_from_f32((TQ*)a.out + (int64_t)seq * a.out_stride + (int64_t)h * HD + tid, sum == 0.f ? 0.f : out / sum);
+  if (a.lse && tid == 0) a.lse[row] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
 }
 
 // ---------------------------------------------------------------------------------
@@ -504,11 +629,11 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   AppendArgs g{};
   g.a = a;
   g.log2_theta = a.rope_theta > 0.f ? log2((double)a.rope_theta) : 0.0;
-  g.vec_q = aligned_to(a.q, 16) && a.q_stride * esz % 16 == 0;
-  g.vec_k = aligned_to(a.k, 16) && a.k_stride * esz % 16 == 0;
-  g.vec_out = aligned_to(a.q_out, 16) && a.q_out_stride * esz % 16 == 0;
   const int heads = (a.q ? a.n_q_heads : 0) + 2 * a.pages.n_kv_heads;
-  const dim3 grid(a.n_rows, (heads + APPEND_HEADS - 1) / APPEND_HEADS);
+  // Single rows: a workgroup each.  Contexts: one for 16 rows, most of which its page's first row takes along anyway:
+  // @@APP@@
+  g.window = a.n_rows > 16 * (int64_t)a.n_seqs ? 16 : 1;
+  const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + APPEND_HEADS - 1) / APPEND_HEADS);
   hipStream_t s = (hipStream_t)stream;
   const bool in16 = a.dtype == TS_DTYPE_BF16, c16 = a.pages.dtype == TS_DTYPE_BF16;
   in16 ? c16 ? launch_append<bf16_t, bf16_t>(g, hd, grid, s) : launch_append<bf16_t, float>(g, hd, grid, s)
@@ -519,7 +644,7 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
 
 // How a call is cut: chunks of 128 keys or a multiple, so many that about four workgroups a CU are there for the longest
 // sequences; the number never falls when max_len grows.
-constexpr int ATT_GROUPS = 4 * 256;
+constexpr int ATT_GROUPS = 2 * 256;
 static void attend_cut(int64_t n_seqs, int hq, int hkv, int max_len, int window, int* chunk, int* splits) {
   const int tiles = (hq / hkv + 15) / 16;
   const int64_t span = window > 0 && window < max_len ? (int64_t)window + ATT_KB - 1 : max_len;
