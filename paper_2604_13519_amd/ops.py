@@ -94,14 +94,14 @@ def _rows(t, name, cols=None, dtype=None):
     return t.data_ptr(), dist if dist > width else width
 
 
-def _ints(t, name, n=None):
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or t.dim() != 1 or (n is not None and t.shape[0] < n):
+def _ints(t, name, n):
+    if t.dtype is not torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous() or t.shape[0] < n:
         _refuse("%s: at least %s contiguous int32 on a GPU are needed, got %s %s", name, n, t.dtype, tuple(t.shape))
     return t.data_ptr()
 
 
 def _bytes(t, name, shape=None):
-    if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or (shape is not None and tuple(t.shape) != shape):
+    if t.dtype is not torch.uint8 or not t.is_cuda or not t.is_contiguous() or (shape is not None and t.shape != shape):
         _refuse("%s: a contiguous uint8 tensor%s on a GPU is needed, got %s %s", name, " of shape %s" % (shape,) if shape else "", t.dtype, tuple(t.shape))
     return t.data_ptr()
 
@@ -117,7 +117,8 @@ def ts_mx_quantize(x, codes=None, scales=None):
         codes = x.new_empty((rows, 16 * blocks), dtype=torch.uint8)
     if scales is None:
         scales = x.new_empty((rows, blocks), dtype=torch.uint8)
-    binding._check(lib.ts_mx_quantize(px, _DTYPES[x.dtype], rows, cols, stride, _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks)), _stream(x)))
+    pc, ps = _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks))
+    binding._check(lib.ts_mx_quantize(px, _DTYPES[x.dtype], rows, cols, stride, pc, ps, _stream(x)))
     return codes, scales
 
 
@@ -198,21 +199,23 @@ def _pages(k_pages, v_pages):
         if not isinstance(k_pages, ts_kv_pages):
             raise TypeError("v_pages is missing")
         return k_pages
-    if k_pages.dim() != 4 or k_pages.shape[2] != TS_PAGE_SIZE or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not k_pages.is_cuda or not v_pages.is_cuda:
-        _refuse("k_pages: a contiguous [pages][heads][%d][head_dim] tensor on a GPU is needed, got %s", TS_PAGE_SIZE, tuple(k_pages.shape))
-    n, h, _, hd = k_pages.shape
-    if tuple(v_pages.shape) != (n, h, hd, TS_PAGE_SIZE):
+    ks = k_pages.shape
+    if len(ks) != 4 or ks[2] != TS_PAGE_SIZE or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not k_pages.is_cuda or not v_pages.is_cuda:
+        _refuse("k_pages: a contiguous [pages][heads][%d][head_dim] tensor on a GPU is needed, got %s", TS_PAGE_SIZE, tuple(ks))
+    n, h, _, hd = ks
+    if v_pages.shape != (n, h, hd, TS_PAGE_SIZE):
         _refuse("v_pages: shape %s is needed, got %s", (n, h, hd, TS_PAGE_SIZE), tuple(v_pages.shape))
-    if k_pages.dtype not in _DTYPES or v_pages.dtype != k_pages.dtype:
-        raise TypeError("pages: float32 or bfloat16 are needed, got %s and %s" % (k_pages.dtype, v_pages.dtype))
-    return ts_kv_pages(k_pages.data_ptr(), v_pages.data_ptr(), n, h, hd, _DTYPES[k_pages.dtype])
+    dtype = k_pages.dtype
+    if dtype not in _DTYPES or v_pages.dtype != dtype:
+        raise TypeError("pages: float32 or bfloat16 are needed, got %s and %s" % (dtype, v_pages.dtype))
+    return ts_kv_pages(k_pages.data_ptr(), v_pages.data_ptr(), n, h, hd, _DTYPES[dtype])
 
 
 def _table(t, n_seqs):
-    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 2 or t.shape[0] < n_seqs or t.shape[1] < 1 or (t.shape[1] > 1 and t.stride(1) != 1) \
-            or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        _refuse("table: int32 [%d][pages] on a GPU is needed, got %s %s", n_seqs, t.dtype, tuple(t.shape))
-    return t.data_ptr(), max(t.stride(0), t.shape[1]), t.shape[1]
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype is not torch.int32 or not t.is_cuda or shape[0] < n_seqs or shape[1] < 1 or (strides[1] != 1 and shape[1] > 1) or (strides[0] < shape[1] and shape[0] > 1):
+        _refuse("table: int32 [%d][pages] on a GPU is needed, got %s %s", n_seqs, t.dtype, tuple(shape))
+    return t.data_ptr(), strides[0] if strides[0] > shape[1] else shape[1], shape[1]
 
 
 def ts_kv_append(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_theta, q_out=None):
@@ -220,29 +223,30 @@ def ts_kv_append(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_th
     rotated; with q ([rows][heads * head_dim]) the rotated queries, which are returned.  See the header."""
     lib = _load()
     pages = _pages(k_pages, v_pages)
-    n = row_offsets.shape[0] - 1
-    a = ts_kv_append_args()
-    a.pages = pages
-    a.table, a.table_stride, a.table_width = _table(table, n)
-    a.lengths, a.row_offsets = _ints(lengths, "lengths", n), _ints(row_offsets, "row_offsets", 2)
-    a.n_seqs, a.n_rows, a.dtype, a.rope_theta = n, k.shape[0], _DTYPES.get(k.dtype, -1), rope_theta
-    width = pages.n_kv_heads * pages.head_dim
-    a.k, a.k_stride = _rows(k, "k", width)
-    a.v, a.v_stride = _rows(v, "v", width, k.dtype)
-    if v.shape[0] != k.shape[0]:
-        _refuse("v: %d rows are needed, got %d", k.shape[0], v.shape[0])
+    n, hd = row_offsets.shape[0] - 1, pages.head_dim
+    table, t_stride, t_width = _table(table, n)
+    width = pages.n_kv_heads * hd
+    pk, k_stride = _rows(k, "k", width)
+    dtype, rows = k.dtype, k.shape[0]
+    pv, v_stride = _rows(v, "v", width, dtype)
+    if v.shape[0] != rows:
+        _refuse("v: %d rows are needed, got %d", rows, v.shape[0])
+    pq, q_stride, po, o_stride, heads = None, 0, None, 0, 0
     if q is not None:
-        a.q, a.q_stride = _rows(q, "q", None, k.dtype)
-        if q.shape[0] != k.shape[0] or q.shape[1] < 1 or q.shape[1] % pages.head_dim:
-            _refuse("q: %d rows of a multiple of %d values are needed, got %s", k.shape[0], pages.head_dim, tuple(q.shape))
+        pq, q_stride = _rows(q, "q", None, dtype)
+        q_rows, q_width = q.shape
+        if q_rows != rows or q_width < 1 or q_width % hd:
+            _refuse("q: %d rows of a multiple of %d values are needed, got %s", rows, hd, tuple(q.shape))
         if q_out is None:
-            q_out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        a.q_out, a.q_out_stride = _rows(q_out, "q_out", q.shape[1], k.dtype)
-        if q_out.shape[0] != k.shape[0]:
-            _refuse("q_out: %d rows are needed, got %d", k.shape[0], q_out.shape[0])
-        a.n_q_heads = q.shape[1] // pages.head_dim
+            q_out = torch.zeros(q.shape, dtype=dtype, device=q.device)
+        po, o_stride = _rows(q_out, "q_out", q_width, dtype)
+        if q_out.shape[0] != rows:
+            _refuse("q_out: %d rows are needed, got %d", rows, q_out.shape[0])
+        heads = q_width // hd
     elif q_out is not None:
         _refuse("q_out without q")
+    a = ts_kv_append_args(pages, table, t_stride, t_width, _ints(lengths, "lengths", n), _ints(row_offsets, "row_offsets", 2), n, rows, heads, _DTYPES[dtype],
+                          pq, q_stride, pk, k_stride, pv, v_stride, po, o_stride, rope_theta)
     binding._check(lib.ts_kv_append(C.byref(a), _stream(k)))
     return q_out
 
@@ -259,28 +263,28 @@ def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=N
     1 / sqrt(head_dim).  workspace: of ts_kv_attend_workspace; without one the call allocates it.  See the header."""
     lib = _load()
     pages = _pages(k_pages, v_pages)
-    n, hd = q.shape[0], pages.head_dim
-    a = ts_kv_attend_args()
-    a.pages = pages
-    a.q, a.q_stride = _rows(q, "q")
-    if n < 1 or q.shape[1] < 1 or q.shape[1] % hd:
+    hd = pages.head_dim
+    pq, q_stride = _rows(q, "q")
+    n, width = q.shape
+    if n < 1 or width < 1 or width % hd:
         _refuse("q: rows of a multiple of %d values are needed, got %s", hd, tuple(q.shape))
-    a.table, a.table_stride, a.table_width = _table(table, n)
-    a.lengths = _ints(lengths, "lengths", n)
-    heads = q.shape[1] // hd
-    a.n_seqs, a.max_len, a.window, a.n_q_heads, a.dtype = n, max_len, window, heads, _DTYPES[q.dtype]
+    table, t_stride, t_width = _table(table, n)
+    heads, dtype = width // hd, q.dtype
     if out is None:
-        out = q.new_empty((n, heads * hd))
-    a.out, a.out_stride = _rows(out, "out", heads * hd, q.dtype)
+        out = q.new_empty((n, width))
+        po, o_stride = out.data_ptr(), width
+    else:
+        po, o_stride = _rows(out, "out", width, dtype)
     if lse is None:
         lse = q.new_empty((n, heads), dtype=torch.float32)
-    if out.shape[0] != n or tuple(lse.shape) != (n, heads) or lse.dtype != torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
-        _refuse("out and lse: [%d][%d] and contiguous fp32 [%d][%d] are needed", n, heads * hd, n, heads)
-    a.lse = lse.data_ptr()
-    a.scale = hd ** -0.5 if scale is None else scale
+    elif lse.shape != (n, heads) or lse.dtype is not torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
+        _refuse("lse: a contiguous fp32 [%d][%d] tensor on a GPU is needed, got %s %s", n, heads, lse.dtype, tuple(lse.shape))
+    if out.shape[0] != n:
+        _refuse("out: %d rows are needed, got %d", n, out.shape[0])
     if workspace is None:
         workspace = ts_kv_attend_workspace(n, heads, pages.n_kv_heads, hd, max_len, window, q.device)
-    if workspace is not None:
-        a.workspace, a.workspace_bytes = _bytes(workspace, "workspace"), workspace.numel()
+    ws, ws_bytes = (None, 0) if workspace is None else (_bytes(workspace, "workspace"), workspace.numel())
+    a = ts_kv_attend_args(pages, table, t_stride, t_width, _ints(lengths, "lengths", n), n, max_len, window, heads, _DTYPES[dtype], pq, q_stride, po, o_stride,
+                          lse.data_ptr(), hd ** -0.5 if scale is None else scale, ws, ws_bytes)
     binding._check(lib.ts_kv_attend(C.byref(a), _stream(q)))
     return out, lse
