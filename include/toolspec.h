@@ -21,7 +21,7 @@
  *  - Handles are not thread-safe.  One HIP stream per model; every call that
  *    returns data to the host has synchronised that stream before returning.
  *  - Matrices handed to ts_model_load are row-major [out][in] (y = x W^T),
- *    element type float (dtype 0) or bfloat16 bit patterns (dtype 1).  The
+ *    element type float (dtype 0) or bfloat16 bit patterns (dtypes 1 and 2).  The
  *    library copies and re-tiles them on the device; the caller may free its
  *    buffers as soon as ts_model_load returns.
  *
@@ -66,7 +66,7 @@ enum {
   TS_ERR_DEVICE       = -7  /* a HIP call failed                                   */
 };
 
-enum { TS_DTYPE_F32 = 0, TS_DTYPE_BF16 = 1 };
+enum { TS_DTYPE_F32 = 0, TS_DTYPE_BF16 = 1, TS_DTYPE_MX4 = 2 };
 enum { TS_MAX_NODES = 64, TS_PAGE_SIZE = 16 };
 
 /* Decoder shape: pre-norm blocks with RMSNorm, rotary embedding (pair (j, j+hd/2)
@@ -82,7 +82,15 @@ enum { TS_MAX_NODES = 64, TS_PAGE_SIZE = 16 };
  * significant bits; the rotated Q and the soft-max probabilities are single halves; bf16
  * K/V entries widen to half exactly (same subnormal caveat); soft-max is fp32, and the
  * residual stream and the logits stay fp32.  It needs d_model, n_q_heads*head_dim and d_ffn to be multiples of
- * 128 and head_dim 64 or 128.  TS_DTYPE_F32 computes in fp32. */
+ * 128 and head_dim 64 or 128.  TS_DTYPE_F32 computes in fp32.
+ * TS_DTYPE_MX4 is TS_DTYPE_BF16 (weights handed over as bf16 bit patterns, bf16 cache, the same
+ * numbers and limits) with wq, wk, wv, wo, wg, wu and wd held as 4-bit microscaled values: blocks
+ * of 32 along [in] share a power-of-two scale, rounded at load as ts_mx_quantize of
+ * toolspec_ops.h says; 17 bytes instead of 64 are read per block.  Values that are already of
+ * that form are kept exactly, so a model quantised elsewhere is handed over as the bf16 values its
+ * codes stand for, and a 4-bit model computes what the bf16 model of the rounded values computes,
+ * up to the order of fp32 sums.  A block that holds an infinity or NaN becomes NaN throughout.
+ * Embedding, lm_head and norm gains stay as in a bf16 model. */
 typedef struct {
   int32_t n_layers, d_model, n_q_heads, n_kv_heads, head_dim, d_ffn, vocab;
   float rope_theta, rms_eps;

@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libtoolspec_hip.so")
 TS_OK = 0
 TS_ERR_INVALID_ARG, TS_ERR_INVALID_TREE, TS_ERR_TOKEN_RANGE = -1, -2, -3
 TS_ERR_KV_CAPACITY, TS_ERR_STATE, TS_ERR_OOM, TS_ERR_DEVICE = -4, -5, -6, -7
-TS_DTYPE_F32, TS_DTYPE_BF16 = 0, 1
+TS_DTYPE_F32, TS_DTYPE_BF16, TS_DTYPE_MX4 = 0, 1, 2
 TS_MAX_NODES, TS_PAGE_SIZE = 64, 16
 TS_Q_OTHERS, TS_Q_TOOL_NAME, TS_Q_PARAM_NAME, TS_Q_PARAM_VALUE = 0, 1, 2, 3
 TS_DRAFT_NONE, TS_DRAFT_RETRIEVAL, TS_DRAFT_SCHEMA = 0, 1, 2

@@ -11,8 +11,7 @@
 #include <map>
 #include <new>
 
-#include "ts_internal.h"
-#include "ts_device_utils.h"
+#include "ts_ops.h"
 
 // ---------------------------------------------------------------------------------
 // errors
@@ -147,7 +146,7 @@ static ts_status check_config(const ts_model_config& c) {
     if (!is_pow2(c.head_dim) || c.head_dim < 8 || c.head_dim > 128)
       return ts_fail(TS_ERR_INVALID_ARG, "fp32 path: head_dim must be a power of two in [8,128]");
   } else {
-    return ts_fail(TS_ERR_INVALID_ARG, "dtype must be TS_DTYPE_F32 or TS_DTYPE_BF16");
+    return ts_fail(TS_ERR_INVALID_ARG, "dtype must be TS_DTYPE_F32, TS_DTYPE_BF16 or TS_DTYPE_MX4");
   }
   return TS_OK;
 }
@@ -257,9 +256,20 @@ static ts_status ensure_attn_partials(ts_model* m, size_t need) {       // need:
 // bf16: staged row-major, then re-tiled as IEEE half into dst at tile offset n_tile0 (stride
 //       n_tile_stride); m->range_flag collects weights that half cannot hold.
 // f32 : copied row-major to dst + row_off rows.
+// mx  : staged likewise, quantised to 4-bit microscaled values behind the staged matrix, and laid out from there.
 static ts_status upload_matrix(ts_model* m, const void* host, int N, int K, void* dst, void* staging, int n_tile0,
-                               int n_tile_stride, int f32_row_off) {
+                               int n_tile_stride, int f32_row_off, bool mx = false) {
   if (!host) return ts_fail(TS_ERR_INVALID_ARG, "null weight pointer");
+  if (mx) {
+    TS_HIP(copy_sync(m->stream, staging, host, (size_t)N * K * 2, hipMemcpyHostToDevice));
+    uint8_t* codes = (uint8_t*)staging + (size_t)N * K * 2;             // K is a multiple of 128: 16-byte aligned
+    uint8_t* scales = codes + (size_t)N * K / 2;
+    launch_mx_quantize(m->stream, staging, TS_DTYPE_BF16, N, K, K, codes, scales);
+    launch_mx_pack(m->stream, codes, scales, N, K, dst, n_tile0, n_tile_stride, m->range_flag);
+    TS_HIP(hipGetLastError());
+    TS_HIP(hipStreamSynchronize(m->stream));
+    return TS_OK;
+  }
   if (m->cfg.dtype == TS_DTYPE_BF16) {
     TS_HIP(copy_sync(m->stream, staging, host, (size_t)N * K * 2, hipMemcpyHostToDevice));
     launch_repack_tiles(m->stream, (const bf16_t*)staging, (f16_t*)dst, N, K, n_tile0, n_tile_stride, m->range_flag);
@@ -301,11 +311,13 @@ static ts_status model_load_impl(ts_model* m, const ts_weights* w) {
   if (bf) {
     size_t big = std::max((size_t)V * d, (size_t)F * d);
     big = std::max(big, (size_t)m->q_dim * d);
-    if ((st = dev_alloc_bytes(&staging, big * 2, false))) return st;
+    // 4-bit models: the codes and scales of a matrix behind it (the lm_head, the largest, has none)
+    if ((st = dev_alloc_bytes(&staging, big * 2 + (m->mx4 ? big / 2 + big / 32 : 0), false))) return st;
     if ((st = dev_alloc_bytes((void**)&m->range_flag, sizeof(int), true))) { dev_free(staging); return st; }
     if ((st = dev_alloc_bytes((void**)&m->sat_count, sizeof(unsigned long long), true))) { dev_free(staging); return st; }
   }
-  auto matrix_bytes = [&](int N, int K) { return (bf ? tiled_elems(N, K) : (size_t)N * K) * esz; };
+  const bool mx = m->mx4;                          // the layers' matrices; the lm_head is a half-precision one as in bf16 models
+  auto matrix_bytes = [&](int N, int K) { return mx ? mx_packed_bytes(N, K) : (bf ? tiled_elems(N, K) : (size_t)N * K) * esz; };
 
   // embedding stays row-major in the storage dtype (it is gathered, not multiplied)
   if ((st = dev_alloc_bytes(&m->embed, (size_t)V * d * esz, false))) { dev_free(staging); return st; }
@@ -313,7 +325,7 @@ static ts_status model_load_impl(ts_model* m, const ts_weights* w) {
     hipError_t e = copy_sync(m->stream, m->embed, w->embed, (size_t)V * d * esz, hipMemcpyHostToDevice);
     if (e != hipSuccess) { dev_free(staging); return ts_fail(TS_ERR_DEVICE, "embedding upload failed: %s", hipGetErrorString(e)); }
   }
-  st = dev_alloc_bytes(&m->lm_head, matrix_bytes(V, d), false);
+  st = dev_alloc_bytes(&m->lm_head, (bf ? tiled_elems(V, d) : (size_t)V * d) * esz, false);
   if (!st) st = upload_matrix(m, w->lm_head, V, d, m->lm_head, staging, 0, 1, 0);
   if (!st) st = upload_gain(m, w->norm_f, &m->norm_f);
 
@@ -330,14 +342,14 @@ static ts_status model_load_impl(ts_model* m, const ts_weights* w) {
     if ((st = dev_alloc_bytes(&L.wgu, matrix_bytes(2 * F, d), false))) break;
     if ((st = dev_alloc_bytes(&L.wd, matrix_bytes(d, F), false))) break;
     // fused QKV: rows [q | k | v]
-    if ((st = upload_matrix(m, w->wq[l], m->q_dim, d, L.wqkv, staging, 0, 1, 0))) break;
-    if ((st = upload_matrix(m, w->wk[l], m->kv_dim, d, L.wqkv, staging, m->q_dim / 16, 1, m->q_dim))) break;
-    if ((st = upload_matrix(m, w->wv[l], m->kv_dim, d, L.wqkv, staging, (m->q_dim + m->kv_dim) / 16, 1, m->q_dim + m->kv_dim))) break;
-    if ((st = upload_matrix(m, w->wo[l], d, m->q_dim, L.wo, staging, 0, 1, 0))) break;
+    if ((st = upload_matrix(m, w->wq[l], m->q_dim, d, L.wqkv, staging, 0, 1, 0, mx))) break;
+    if ((st = upload_matrix(m, w->wk[l], m->kv_dim, d, L.wqkv, staging, m->q_dim / 16, 1, m->q_dim, mx))) break;
+    if ((st = upload_matrix(m, w->wv[l], m->kv_dim, d, L.wqkv, staging, (m->q_dim + m->kv_dim) / 16, 1, m->q_dim + m->kv_dim, mx))) break;
+    if ((st = upload_matrix(m, w->wo[l], d, m->q_dim, L.wo, staging, 0, 1, 0, mx))) break;
     // fused gate/up: 16-row tiles alternate gate, up, gate, up, ...
     if (bf) {
-      if ((st = upload_matrix(m, w->wg[l], F, d, L.wgu, staging, 0, 2, 0))) break;
-      if ((st = upload_matrix(m, w->wu[l], F, d, L.wgu, staging, 1, 2, 0))) break;
+      if ((st = upload_matrix(m, w->wg[l], F, d, L.wgu, staging, 0, 2, 0, mx))) break;
+      if ((st = upload_matrix(m, w->wu[l], F, d, L.wgu, staging, 1, 2, 0, mx))) break;
     } else {
       gu_host.resize((size_t)2 * F * d);
       const float* g = (const float*)w->wg[l];
@@ -348,7 +360,7 @@ static ts_status model_load_impl(ts_model* m, const ts_weights* w) {
       }
       if ((st = upload_matrix(m, gu_host.data(), 2 * F, d, L.wgu, staging, 0, 1, 0))) break;
     }
-    if ((st = upload_matrix(m, w->wd[l], d, F, L.wd, staging, 0, 1, 0))) break;
+    if ((st = upload_matrix(m, w->wd[l], d, F, L.wd, staging, 0, 1, 0, mx))) break;
     if ((st = upload_gain(m, w->norm1[l], &L.norm1))) break;
     if ((st = upload_gain(m, w->norm2[l], &L.norm2))) break;
   }
@@ -379,11 +391,17 @@ extern "C" ts_status ts_model_free(ts_model* m) {
 extern "C" ts_status ts_model_load(const ts_model_config* cfg, const ts_weights* w, ts_model** out) {
   if (!cfg || !w || !out) return ts_fail(TS_ERR_INVALID_ARG, "ts_model_load: null argument");
   *out = nullptr;
+  // a 4-bit model is a bf16 model (storage of embedding, lm_head, norms and cache) whose layers' matrices are 4-bit
+  ts_model_config own = *cfg;
+  const bool mx4 = own.dtype == TS_DTYPE_MX4;
+  if (mx4) own.dtype = TS_DTYPE_BF16;
+  cfg = &own;
   ts_status st = check_config(*cfg);
   if (st) return st;
   ts_model* m = new (std::nothrow) ts_model();
   if (!m) return ts_fail(TS_ERR_OOM, "host allocation failed");
   m->cfg = *cfg;
+  m->mx4 = mx4;
   m->esz = cfg->dtype == TS_DTYPE_BF16 ? 2 : 4;
   m->q_dim = cfg->n_q_heads * cfg->head_dim;
   m->kv_dim = cfg->n_kv_heads * cfg->head_dim;
@@ -848,7 +866,11 @@ static ts_status verify_impl(ts_model* m, ts_kv* const* kvs, int n_seqs, const i
   int pending_parts = 0;          // split-K partials of the previous projection still to be added to H
   size_t pending_stride = 0;
   auto project = [&](const char* name, const void* X, const void* W, int N, int K, int* n_parts, size_t* stride) {
-    if (bf) {
+    if (m->mx4) {
+      ProfScope ps(m, name);
+      *n_parts = launch_mx_model(m, (const f16_t*)X, W, m->part, m->part_elems, R, N, K);
+      *stride = (size_t)R * N;
+    } else if (bf) {
       GemmPlan p = gemm_bf16_plan(m, R, N, K, 0);
       while (p.splits > 1 && (size_t)p.splits * R * N > m->part_elems) p.splits = K / gemm_bf16_chunk(p.shape) % (p.splits / 2) == 0 ? p.splits / 2 : 1;
       ProfScope ps(m, name);
@@ -875,7 +897,10 @@ static ts_status verify_impl(ts_model* m, ts_kv* const* kvs, int n_seqs, const i
     }
     project("gemm_o", m->Ab, L.wo, d, m->q_dim, &np, &ps);
     launch_norm(m, R, L.norm2, np, ps, false);
-    if (bf) {   // gate/up projection with the SwiGLU product in its epilogue
+    if (m->mx4) {
+      ProfScope psc(m, "gemm_gate_up");
+      launch_mx_model_swiglu(m, (const f16_t*)m->Xn, L.wgu, (f16_t*)m->Fb, R, F, d);
+    } else if (bf) {   // gate/up projection with the SwiGLU product in its epilogue
       const GemmPlan p = gemm_bf16_plan(m, R, 2 * F, d, 2);
       ProfScope psc(m, "gemm_gate_up");
       launch_gemm_bf16(m, (const f16_t*)m->Xn, (const f16_t*)L.wgu, nullptr, R, 2 * F, d, p, 2, nullptr, (f16_t*)m->Fb);
@@ -1096,7 +1121,7 @@ extern "C" ts_status ts_profile_plain_read(ts_model* m, int32_t launches, uint64
   if (m->cfg.dtype != TS_DTYPE_BF16 || !m->range_flag)
     return ts_fail(TS_ERR_INVALID_ARG, "ts_profile_plain_read: bf16 models only");
   (void)hipSetDevice(m->device);
-  const size_t bytes = (size_t)2 * m->cfg.d_ffn * m->cfg.d_model * 2;
+  const size_t bytes = m->mx4 ? mx_packed_bytes(2 * m->cfg.d_ffn, m->cfg.d_model) : (size_t)2 * m->cfg.d_ffn * m->cfg.d_model * 2;
   for (int i = 0; i < launches; ++i)
     launch_plain_read(m, m->layers[i % m->layers.size()].wgu, bytes, (uint32_t*)m->range_flag);
   TS_HIP(hipGetLastError());

@@ -120,7 +120,7 @@ struct ts_kv {
 };
 
 struct LayerW {
-  void* wqkv; void* wo; void* wgu; void* wd;   // device; bf16 models: MFMA-tiled IEEE half, f32: row-major [N][K]
+  void* wqkv; void* wo; void* wgu; void* wd;   // device; bf16 models: MFMA-tiled IEEE half, f32: row-major [N][K], 4-bit models: packed (ts_mx.hip)
   float* norm1; float* norm2;                  // device fp32
 };
 
@@ -129,6 +129,7 @@ struct ts_model {
   int device;
   hipStream_t stream;
   int esz;                      // bytes per stored element
+  bool mx4;                     // the layers' matrices are 4-bit microscaled ones (cfg.dtype is TS_DTYPE_BF16 then)
   int q_dim, kv_dim, qkv_dim;
   void* embed;                  // device [V][d] in storage dtype, row-major
   void* lm_head;                // device, tiled (bf16) or row-major (f32)
@@ -206,6 +207,10 @@ void gemm_rows_plan(const ts_model* m, int R, int N, int K, int mode, size_t max
 int gemm_rows_chunk(int cfg);
 void launch_gemm_rows_bf16(ts_model* m, const f16_t* X, const f16_t* Wt, float* out, int R, int N, int K, int mt, int cfg,
                            int splits, int mode, f16_t* act_out, float* logits);
+// projections of 4-bit models (ts_mx.hip): X in hi and lo halves; out: fp32 partial sums [split][R][N], as many splits as are
+// returned and fit out_elems / the SwiGLU product in hi and lo halves
+int launch_mx_model(ts_model* m, const f16_t* X, const void* W, float* out, size_t out_elems, int R, int N, int K);
+void launch_mx_model_swiglu(ts_model* m, const f16_t* X, const void* W, f16_t* act_out, int R, int F, int K);
 int attn_bf16_units(const ts_model* m, int n_seqs, const int* n_keys, int max_M, AttnUnit* units, int* seq_splits);
 int attn_bf16_max_units(const ts_model* m, int n_seqs);
 void launch_attn_bf16(ts_model* m, const RowMeta& rm, int n_units, int layer, int max_M);

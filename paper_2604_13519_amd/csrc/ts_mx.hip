@@ -127,7 +127,7 @@ __global__ __launch_bounds__(QT) void k_mx_dequantize(const uint8_t* codes, cons
 
 // rows of one launch: pieces within 32 bits
 static int64_t mx_slab(int64_t cols) { return ((int64_t)1 << 31) / ((cols + 31) / 32 * 4); }
-static uint32_t mx_groups(int64_t rows, int64_t cols) { return (uint32_t)((rows * ((cols + 31) / 32 * 4) + QT * QU - 1) / (QT * QU)); }
+static uint32_t mx_pieces_groups(int64_t rows, int64_t cols) { return (uint32_t)((rows * ((cols + 31) / 32 * 4) + QT * QU - 1) / (QT * QU)); }
 
 void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t* codes, uint8_t* scales) {
   const int64_t blocks = (cols + 31) / 32, slab = mx_slab(cols);
@@ -136,8 +136,8 @@ void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t row
     const int64_t n = std::min(slab, rows - r);
     const void* xs = (const char*)x + r * stride * esz;
     uint8_t *cs = codes + r * blocks * 16, *ss = scales + r * blocks;
-    if (dtype == TS_DTYPE_BF16) k_mx_quantize<bf16_t><<<mx_groups(n, cols), QT, 0, s>>>((const bf16_t*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
-    else k_mx_quantize<float><<<mx_groups(n, cols), QT, 0, s>>>((const float*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
+    if (dtype == TS_DTYPE_BF16) k_mx_quantize<bf16_t><<<mx_pieces_groups(n, cols), QT, 0, s>>>((const bf16_t*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
+    else k_mx_quantize<float><<<mx_pieces_groups(n, cols), QT, 0, s>>>((const float*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
   }
 }
 
@@ -148,8 +148,8 @@ static void launch_mx_dequantize(hipStream_t s, const uint8_t* codes, const uint
     const int64_t n = std::min(slab, rows - r);
     void* xs = (char*)x + r * stride * esz;
     const uint8_t *cs = codes + r * blocks * 16, *ss = scales + r * blocks;
-    if (dtype == TS_DTYPE_BF16) k_mx_dequantize<bf16_t><<<mx_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (bf16_t*)xs, stride);
-    else k_mx_dequantize<float><<<mx_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (float*)xs, stride);
+    if (dtype == TS_DTYPE_BF16) k_mx_dequantize<bf16_t><<<mx_pieces_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (bf16_t*)xs, stride);
+    else k_mx_dequantize<float><<<mx_pieces_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (float*)xs, stride);
   }
 }
 
@@ -164,7 +164,7 @@ static int64_t mx_chunks(int64_t n_in) { return (n_in + 127) / 128; }
 size_t mx_packed_bytes(int64_t n_out, int64_t n_in) { return (size_t)((n_out + 15) / 16) * mx_chunks(n_in) * MX_REC; }
 
 __global__ __launch_bounds__(256) void k_mx_pack(const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, uint8_t* packed,
-                                                 int n_tile0, int n_tile_stride, int chunks, int64_t records) {
+                                                 int n_tile0, int n_tile_stride, int chunks, int64_t records, int* range_flag) {
   const int64_t rec = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (rec >= records) return;
   const int lane = threadIdx.x % 64, tile = (int)(rec / chunks), c = (int)(rec % chunks);
@@ -180,12 +180,19 @@ __global__ __launch_bounds__(256) void k_mx_pack(const uint8_t* codes, const uin
   }
   uint8_t* p = packed + ((int64_t)(n_tile0 + tile * n_tile_stride) * chunks + c) * MX_REC;
   reinterpret_cast<uint4*>(p)[lane] = make_uint4(w[0], w[1], w[2], w[3]);
+  // a block's largest value is at least 4 times its scale (a code below that would not be of this scale): 4 * 2^14 is
+  // beyond half's largest number, 6 * 2^13 is not
+  if (range_flag && lg == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (s[i] > 127 + 13 && s[i] != 255) *range_flag = 1;
+  }
   if (lg == 0) reinterpret_cast<uint32_t*>(p + 1024)[lane] = s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24;
 }
 
-void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride) {
+void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride,
+                    int* range_flag) {
   const int64_t records = (int64_t)((n_out + 15) / 16) * mx_chunks(n_in);
-  k_mx_pack<<<(uint32_t)((records + 3) / 4), 256, 0, s>>>(codes, scales, n_out, n_in, (uint8_t*)packed, n_tile0, n_tile_stride, (int)mx_chunks(n_in), records);
+  k_mx_pack<<<(uint32_t)((records + 3) / 4), 256, 0, s>>>(codes, scales, n_out, n_in, (uint8_t*)packed, n_tile0, n_tile_stride, (int)mx_chunks(n_in), records, range_flag);
 }
 
 // ---------------------------------------------------------------------------------
@@ -204,6 +211,7 @@ struct MxArgs {
   void* y; int64_t y_stride; size_t y_plane; int32_t y_f32;
   unsigned long long* sat;
   int rows, n_out, n_in, chunks;
+  int per; size_t y_part;                                 // chunks of a split of K, elements between the splits' sums
 };
 
 template <int IN> struct MxIn { static constexpr int planes = IN == MX_IN_BF16 ? 1 : IN == MX_IN_F32 ? 3 : 2; };
@@ -310,7 +318,7 @@ __device__ __forceinline__ void mx_planes(const MxRaw<IN>& v, uint4 (&o)[MxIn<IN
 __device__ __forceinline__ void mx_emit(const MxArgs& g, int row, int n, const ts_f32x4& v) {
   if (row >= g.rows || n >= g.n_out) return;
   if (g.y_f32) {
-    float* p = (float*)g.y + (int64_t)row * g.y_stride + n;
+    float* p = (float*)g.y + blockIdx.z * g.y_part + (int64_t)row * g.y_stride + n;
     if (n + 4 <= g.n_out) store16(p, __builtin_bit_cast(uint4, v));
     else
 #pragma unroll
@@ -333,94 +341,71 @@ __device__ __forceinline__ void mx_emit_swiglu(const MxArgs& g, int row, int f, 
   st_act_planes4((f16_t*)g.y + (int64_t)row * g.y_stride + f, g.y_plane, p[0], p[1], p[2], p[3], g.sat);
 }
 
-// Few rows or few columns: KW waves share RT row tiles by CT column tiles (of 16), wave w takes chunks w, w + KW, ..., UC
-// of them per request and two requests in flight.  An input is used by one wave only, so a lane reads its pieces of its
-// rows itself: for instruction i of a chunk, 64 neighbouring bytes of each of 16 rows.  The waves' sums meet in the
-// LDS, added in their order.
-template <int IN, int OUT, int RT, int CT, int KW, int UC>
+// Few rows or few columns: KW waves share 16 rows by CT column tiles (of 16), wave w takes chunks w, w + KW, ..., one in use
+// and one on its way.  An input is used by one wave only, so a lane reads its pieces of its row itself: for
+// instruction i of a chunk, 64 neighbouring bytes of each of 16 rows.  The waves' sums meet in the LDS, added in their
+// order.
+template <int IN, int OUT, int CT, int KW>
 __global__ __launch_bounds__(KW * 64) void k_mx_few(MxArgs g) {
   typedef typename MxElem<IN>::T E;
   constexpr int NP = MxIn<IN>::planes;
-  __shared__ __align__(16) ts_f32x4 red[KW][RT * CT][64];
+  __shared__ __align__(16) ts_f32x4 red[KW][CT][64];
   const int kw = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, lm = lane % 16, lg = lane / 16;
-  const int row0 = blockIdx.y * (RT * 16), tile0 = blockIdx.x * CT, n_tiles = (g.n_out + 15) / 16;
+  const int row0 = blockIdx.y * 16, tile0 = blockIdx.x * CT, n_tiles = (g.n_out + 15) / 16;
   const uint8_t* wp[CT];
 #pragma unroll
   for (int c = 0; c < CT; ++c) wp[c] = g.w + (int64_t)min(tile0 + c, n_tiles - 1) * g.chunks * MX_REC;
   const char* xp = (const char*)((const E*)g.x + (int64_t)row0 * g.x_stride);
-  uint32_t xo[RT];
+  const uint32_t xo = mx_x_offset<IN>(g, row0, lm, lg * 8);
+  ts_f32x4 acc[CT];
 #pragma unroll
-  for (int r = 0; r < RT; ++r) xo[r] = mx_x_offset<IN>(g, row0, r * 16 + lm, lg * 8);
-  ts_f32x4 acc[RT][CT];
-#pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int c = 0; c < CT; ++c) acc[r][c] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int c = 0; c < CT; ++c) acc[c] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
 
-  struct Request { uint4 w[UC][CT]; uint32_t s[UC][CT]; MxRaw<IN> x[UC][RT][4]; };
-  const int full = g.n_in / 128;                             // chunks without an end in them
-  auto fetch = [&](Request& q, int c0) {
+  struct Chunk { uint4 w[CT]; uint32_t s[CT]; MxRaw<IN> x[4]; };
+  auto fetch_w = [&](Chunk& q, int64_t cc) {
 #pragma unroll
-    for (int u = 0; u < UC; ++u) {
-      const int64_t cc = min(c0 + u * KW, full - 1);         // past the end: requested, not used
-#pragma unroll
-      for (int c = 0; c < CT; ++c) { q.w[u][c] = mx_fetch_w(wp[c] + cc * MX_REC, lane * 16); q.s[u][c] = mx_fetch_s(wp[c] + cc * MX_REC, lm * 4); }
-#pragma unroll
-      for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q.x[u][r][i] = mx_fetch<IN>(g, xp + (cc * 128 + i * 32) * (int)sizeof(E), xo[r]);
-    }
+    for (int c = 0; c < CT; ++c) { q.w[c] = mx_fetch_w(wp[c] + cc * MX_REC, lane * 16); q.s[c] = mx_fetch_s(wp[c] + cc * MX_REC, lm * 4); }
   };
-  auto multiply = [&](const uint4 (&w)[CT], const uint32_t (&s)[CT], const MxRaw<IN> (&x)[RT][4]) {
+  const int full = g.n_in / 128;                             // chunks without an end in them
+  auto fetch = [&](Chunk& q, int chunk) {
+    const int64_t cc = min(chunk, full - 1);                 // past the end: requested, not used
+    fetch_w(q, cc);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.x[i] = mx_fetch<IN>(g, xp + (cc * 128 + i * 32) * (int)sizeof(E), xo);
+  };
+  auto multiply = [&](const Chunk& q) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint4 wf[CT];
+      uint4 xf[NP];
+      mx_planes<IN>(q.x[i], xf);
 #pragma unroll
-      for (int c = 0; c < CT; ++c) wf[c] = mx_widen<IN>(word(w[c], i), s[c], i);
+      for (int c = 0; c < CT; ++c) {
+        const uint4 wf = mx_widen<IN>(word(q.w[c], i), q.s[c], i);
 #pragma unroll
-      for (int r = 0; r < RT; ++r) {
-        uint4 xf[NP];
-        mx_planes<IN>(x[r][i], xf);
-#pragma unroll
-        for (int p = NP - 1; p >= 0; --p)                    // the smaller terms first
-#pragma unroll
-          for (int c = 0; c < CT; ++c) acc[r][c] = mx_mfma<IN>(wf[c], xf[p], acc[r][c]);
+        for (int p = NP - 1; p >= 0; --p) acc[c] = mx_mfma<IN>(wf, xf[p], acc[c]);      // the smaller terms first
       }
     }
   };
-  auto use = [&](const Request& q, int c0) {
-#pragma unroll
-    for (int u = 0; u < UC; ++u)
-      if (c0 + u * KW < full) multiply(q.w[u], q.s[u], q.x[u]);
-  };
-  const int trips = (full + KW * UC - 1) / (KW * UC);
-  if (full > 0) {
-    Request a, b;
+  if (kw < full) {
+    Chunk a, b;
     fetch(a, kw);
-    for (int t = 0; t < trips; t += 2) {
-      fetch(b, (t + 1) * (KW * UC) + kw);
-      use(a, t * (KW * UC) + kw);
-      if (t + 1 >= trips) break;
-      fetch(a, (t + 2) * (KW * UC) + kw);
-      use(b, (t + 1) * (KW * UC) + kw);
+    for (int c = kw; c < full; c += 2 * KW) {
+      fetch(b, c + KW);
+      multiply(a);
+      if (c + KW >= full) break;
+      fetch(a, c + 2 * KW);
+      multiply(b);
     }
   }
   if (IN != MX_IN_PLANES && full < g.chunks && kw == full % KW) {         // the last chunk ends early
-    uint4 w[CT];
-    uint32_t s[CT];
-    MxRaw<IN> x[RT][4];
+    Chunk q;
+    fetch_w(q, full);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) { w[c] = mx_fetch_w(wp[c] + (int64_t)full * MX_REC, lane * 16); s[c] = mx_fetch_s(wp[c] + (int64_t)full * MX_REC, lm * 4); }
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[r][i] = mx_fetch_some<IN>(xp + ((int64_t)full * 128 + i * 32) * (int)sizeof(E), xo[r], g.n_in - (full * 128 + i * 32 + lg * 8));
-    multiply(w, s, x);
+    for (int i = 0; i < 4; ++i) q.x[i] = mx_fetch_some<IN>(xp + ((int64_t)full * 128 + i * 32) * (int)sizeof(E), xo, g.n_in - (full * 128 + i * 32 + lg * 8));
+    multiply(q);
   }
 #pragma unroll
-  for (int r = 0; r < RT; ++r)
-#pragma unroll
-    for (int c = 0; c < CT; ++c) red[kw][r * CT + c][lane] = acc[r][c];
+  for (int c = 0; c < CT; ++c) red[kw][c][lane] = acc[c];
   __syncthreads();
   auto sum = [&](int t) {
     ts_f32x4 v = red[0][t][lane];
@@ -428,11 +413,10 @@ __global__ __launch_bounds__(KW * 64) void k_mx_few(MxArgs g) {
     for (int o = 1; o < KW; ++o) v += red[o][t][lane];
     return v;
   };
-  constexpr int STEP = OUT == MX_OUT_SWIGLU ? 2 : 1;         // tiles alternate: gate and up of the same 16 features
-  for (int t = kw * STEP; t < RT * CT; t += KW * STEP) {
-    const int row = row0 + t / CT * 16 + lm, tile = tile0 + t % CT;
-    if constexpr (OUT == MX_OUT_SWIGLU) mx_emit_swiglu(g, row, tile * 8 + 4 * lg, sum(t), sum(t + 1));
-    else mx_emit(g, row, tile * 16 + 4 * lg, sum(t));
+  if constexpr (OUT == MX_OUT_SWIGLU) {                      // tiles alternate: gate and up of the same 16 features
+    if (kw < CT / 2) mx_emit_swiglu(g, row0 + lm, (tile0 / 2 + kw) * 16 + 4 * lg, sum(2 * kw), sum(2 * kw + 1));
+  } else {
+    if (kw < CT) mx_emit(g, row0 + lm, (tile0 + kw) * 16 + 4 * lg, sum(kw));
   }
 }
 
@@ -466,6 +450,7 @@ __global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
   const int wc = __builtin_amdgcn_readfirstlane(gt / 64), lm = lane % T, lg = lane / T;
   const int row0 = blockIdx.y * MT, tile0 = (blockIdx.x * WC + wc) * CT, n_tiles = (g.n_out + 15) / 16;
   char* xs = smem + kw * (NP * PLANE);
+  const int chunk0 = blockIdx.z * g.per;
 
   // Weights: instruction i of a chunk takes inputs (64 / T) 8 i + 8 lg .. + 7.  With T = 32 a lane's row lies in one of
   // two records, and its inputs are those of lane groups lg and lg + 2 of the record.
@@ -475,7 +460,7 @@ __global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
   for (int c = 0; c < CT; ++c) {
     const int first = min((tile0 + c) * BL, n_tiles - 1);
     const uint32_t second = lm >= 16 && first + 1 < n_tiles ? (uint32_t)g.chunks * MX_REC : 0;
-    wp[c] = g.w + (int64_t)first * g.chunks * MX_REC;
+    wp[c] = g.w + ((int64_t)first * g.chunks + chunk0) * MX_REC;
     wo[c] = second + (lg * 16 + lm % 16) * 16;
     so[c] = second + lm % 16 * 4;
   }
@@ -488,7 +473,7 @@ __global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
 #pragma unroll
       for (int q = 0; q < 4 * AQ; ++q) acc[r][c][q] = 0.f;
 
-  const char* xp = (const char*)((const E*)g.x + (int64_t)row0 * g.x_stride);
+  const char* xp = (const char*)((const E*)g.x + (int64_t)row0 * g.x_stride + (int64_t)chunk0 * 128);
   uint32_t xo[XU], xl[XU];
 #pragma unroll
   for (int u = 0; u < XU; ++u) {
@@ -543,7 +528,7 @@ __global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
     }
   };
   MxRaw<IN> xn[XU];
-  const int full = g.n_in / 128, trips = (full + KW - 1) / KW;            // chunks without an end in them
+  const int full = min(g.n_in / 128 - chunk0, g.per), trips = (full + KW - 1) / KW;     // chunks without an end in them
   auto fetch = [&](Weights& q, int chunk) {
     const int64_t cc = min(chunk, full - 1);                              // past the end: requested, not used
 #pragma unroll
@@ -566,7 +551,7 @@ __global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
     }
     if (t < trips) { step(xs, a, b, t); ++t; }
   }
-  if (IN != MX_IN_PLANES && full < g.chunks) {               // the last chunk ends early
+  if (IN != MX_IN_PLANES && full < g.chunks) {               // the last chunk ends early (K is not split then)
     char* buf = xs + (t & 1) * BUF;
     Weights q;
     if (kw == 0) {
@@ -631,43 +616,73 @@ __global__ __launch_bounds__(WC * KW * 64) void k_mx_rows(MxArgs g) {
   }
 }
 
-template <int IN, int OUT, int RT, int CT, int KW, int UC>
+template <int IN, int OUT, int CT, int KW>
 static void mx_launch_few(hipStream_t s, const MxArgs& g) {
-  k_mx_few<IN, OUT, RT, CT, KW, UC><<<dim3((g.n_out + 16 * CT - 1) / (16 * CT), (g.rows + 16 * RT - 1) / (16 * RT)), KW * 64, 0, s>>>(g);
+  k_mx_few<IN, OUT, CT, KW><<<dim3((g.n_out + 16 * CT - 1) / (16 * CT), (g.rows + 15) / 16), KW * 64, 0, s>>>(g);
 }
 template <int IN, int OUT, int T, int RT, int CT, int WC, int KW>
 static void mx_launch(hipStream_t s, const MxArgs& g) {
   constexpr int MT = RT * T, NT = WC * CT * T;
-  k_mx_rows<IN, OUT, T, RT, CT, WC, KW><<<dim3((g.n_out + NT - 1) / NT, (g.rows + MT - 1) / MT), WC * KW * 64, 0, s>>>(g);
+  k_mx_rows<IN, OUT, T, RT, CT, WC, KW><<<dim3((g.n_out + NT - 1) / NT, (g.rows + MT - 1) / MT, (g.chunks + g.per - 1) / g.per), WC * KW * 64, 0, s>>>(g);
 }
 
 // Which shape a call takes: the one whose rounds of workgroups (256 CUs) times the time of a round is least.  The times are
-// microseconds of one round at 4096 inputs, measured between events with a quarter of the CUs to all of them at work;
-// all shapes scale alike with the inputs.  For 2, 3, 4, 5 row tiles of 16 (more rows: blocks of 4 tiles):
-//   bf16 rows   32 columns  6.8   8.7  12.1  13.0     64 columns  7.9  10.0  12.8  14.7     128 columns 11.5  14.8  17.3  20.8
-//   fp32 rows               -                                    24.8  35.3  45.8  52                   35    47    61.6  73
-//   planes                  -                                    14.7  20.7  26.6  32                   20.5  28.5  36    43
-// 64 rows x 256 columns, T = 32: 30.5, 84, 55.  Shapes without LDS staging (shares of a round count, they are bound by
-// the rows' way through the caches): 16 rows x 16 columns 6.6, 11.2, 7.5; 32 x 32: -, 20.5, 12.5.
+// microseconds of one round at 4096 inputs, measured between events with an eighth of the CUs to all of them at work; all
+// shapes scale alike with the inputs.  For 2, 3, 4, 5 row tiles of 16 (more rows: blocks of 4 tiles), columns a workgroup:
+//   bf16 rows   32:  6.8   8.7  12.1  13.0     64:  7.9  10.0  12.8  14.7     128: 11.5  14.8  17.3  20.8
+//   fp32 rows                                  64: 24.8  35.3  45.8  52       128: 35    47    61.6  73
+//   planes                                     64: 12.8  16.9  21.9  26.8     128: 23.1  29.5  37    44.2
+// 64 rows x 256 columns, T = 32: 30.5, 84, 52.6.  The shapes without LDS staging, 16 rows x 16 or 32 columns, are bound by
+// the rows' way through the caches: a round takes a time for r rows, more rounds one each (direct_us below).  One row of
+// 4096 inputs, 4096 columns: 3.8 and 4.3 us (32 columns staged 6.7); 28672 columns: 13.8 and 12.0 us, 128 columns staged 12.5;
+// 16 rows: 4096 columns 7.0, 7.3, 6.9 us, 28672 columns 36.3, 22.7, 13.1 us.
 // 65 rows x 4096 inputs, 28672 columns: 128 columns wide 22.3 us, 64 wide 29.8, 32 wide 47.4, 256 wide 31.6; 4096
 // columns: 32 wide 13.0, 64 wide 14.7, 128 wide 20.9.
 enum { MX_DIRECT, MX_DIRECT2, MX_N32, MX_N64, MX_N128, MX_N256 };
-struct MxPlan { int shape, rt; };
+struct MxPlan { int shape, rt; float rounds_us; };
+static constexpr float mx_round_us[3][3][4] = {{{6.8f, 8.7f, 12.1f, 13.0f}, {7.9f, 10.0f, 12.8f, 14.7f}, {11.5f, 14.8f, 17.3f, 20.8f}},
+                                               {{0, 0, 0, 0}, {24.8f, 35.3f, 45.8f, 52.f}, {35.f, 47.f, 61.6f, 73.f}},
+                                               {{0, 0, 0, 0}, {12.8f, 16.9f, 21.9f, 26.8f}, {23.1f, 29.5f, 37.f, 44.2f}}};
+static constexpr float mx_wide_us[3] = {30.5f, 84.f, 52.6f};
+static float mx_groups(int rows, int n_out, int mt, int nt) { return (float)((rows + mt - 1) / mt) * (float)((n_out + nt - 1) / nt); }
+static int mx_row_tiles(int rows) { return rows > 80 ? 4 : std::max(2, (rows + 15) / 16); }
+
 template <int IN, int OUT>
 static MxPlan mx_plan(int rows, int n_out) {
-  static constexpr float round_us[3][3][4] = {{{6.8f, 8.7f, 12.1f, 13.0f}, {7.9f, 10.0f, 12.8f, 14.7f}, {11.5f, 14.8f, 17.3f, 20.8f}},
-                                              {{0, 0, 0, 0}, {24.8f, 35.3f, 45.8f, 52.f}, {35.f, 47.f, 61.6f, 73.f}},
-                                              {{0, 0, 0, 0}, {14.7f, 20.7f, 26.6f, 32.f}, {20.5f, 28.5f, 36.f, 43.f}}};
-  static constexpr float direct_us[3] = {6.6f, 11.2f, 7.5f}, direct2_us[3] = {1e9f, 20.5f, 12.5f}, wide_us[3] = {30.5f, 84.f, 55.f};
-  const int rt = rows > 80 ? 4 : std::max(2, (rows + 15) / 16);
-  auto groups = [&](int mt, int nt) { return (float)((rows + mt - 1) / mt) * (float)((n_out + nt - 1) / nt) / 256.f; };
-  MxPlan best{MX_N256, rt};
-  float least = ceilf(groups(64, 256)) * wide_us[IN];
-  auto offer = [&](int shape, float cost) { if (cost < least) { least = cost; best.shape = shape; } };
+  // one round: [0] + [1] r, of several each: [2] + [3] r
+  static constexpr float direct_us[3][2][4] = {{{3.6f, 0.22f, 2.4f, 0.21f}, {4.0f, 0.2f, 2.8f, 0.2f}},
+                                               {{7.2f, 0.29f, 4.6f, 0.31f}, {7.6f, 0.25f, 5.6f, 0.28f}},
+                                               {{4.9f, 0.42f, 2.6f, 0.4f}, {5.0f, 0.42f, 3.7f, 0.42f}}};
+  const int rt = mx_row_tiles(rows);
+  const float r = (float)std::min(rows, 16);
+  auto share = [&](int mt, int nt) { return mx_groups(rows, n_out, mt, nt) / 256.f; };
+  MxPlan best{MX_N256, rt, ceilf(share(64, 256)) * mx_wide_us[IN]};
+  auto offer = [&](int shape, float cost) { if (cost < best.rounds_us) { best.rounds_us = cost; best.shape = shape; } };
   for (int w = IN == MX_IN_BF16 ? 0 : 1; w < 3; ++w)
-    if (OUT == MX_OUT_ROWS || w == 2) offer(MX_N32 + w, ceilf(groups(16 * rt, 32 << w)) * round_us[IN][w][rt - 2]);
-  if (OUT == MX_OUT_ROWS) offer(MX_DIRECT, std::max(1.f, groups(16, 16)) * direct_us[IN]);
-  if (IN != MX_IN_BF16) offer(MX_DIRECT2, std::max(1.f, groups(32, 32)) * direct2_us[IN]);
+    if (OUT == MX_OUT_ROWS || w == 2) offer(MX_N32 + w, ceilf(share(16 * rt, 32 << w)) * mx_round_us[IN][w][rt - 2]);
+  for (int w = OUT == MX_OUT_ROWS ? 0 : 1; w < 2; ++w) {
+    const float* us = direct_us[IN][w];
+    offer(MX_DIRECT + w, std::max(us[0] + us[1] * r, ceilf(share(16, 16 << w)) * (us[2] + us[3] * r)));
+  }
+  return best;
+}
+
+// Splits of K for a model's projection, whose sums the next kernel adds up: what a shape takes for its share of the
+// chunks, 2.5 us for starting and the sums' way to memory and back at 4 TB/s.  (65 rows x 14336 inputs, 4096 columns:
+// 128 columns in 1 split 147 us.)
+static MxPlan mx_plan_splits(int rows, int n_out, int chunks, int most, int* splits) {
+  const int rt = mx_row_tiles(rows);
+  MxPlan best{MX_N256, rt, 1e30f};
+  for (int s = 1; s <= most; ++s) {
+    const int per = (chunks + s - 1) / s;
+    if ((chunks + per - 1) / per != s) continue;
+    for (int w = 1; w <= 3; ++w) {
+      const float round = w < 3 ? mx_round_us[MX_IN_PLANES][w][rt - 2] : mx_wide_us[MX_IN_PLANES];
+      const float rounds = ceilf(mx_groups(rows, n_out, w < 3 ? 16 * rt : 64, 32 << w) * s / 256.f);
+      const float us = 2.5f + rounds * (round - 2.5f) * per / 32.f + (s > 1 ? s : 0) * (float)rows * n_out * 8 / 4e6f;
+      if (us < best.rounds_us) { best = MxPlan{MX_N32 + w, rt, us}; *splits = s; }
+    }
+  }
   return best;
 }
 
@@ -680,21 +695,48 @@ static void mx_project_tiles(hipStream_t s, const MxArgs& g, int shape) {
 }
 
 template <int IN, int OUT>
-static void mx_project(hipStream_t s, const MxArgs& g) {
-  if (g.rows <= 16) {
-    // one column tile a workgroup where that is one round at most: a row of 4096 inputs, 4096 columns 3.7 us (two tiles
-    // 4.2), 6144 columns 5.7 (4.7), 28672 columns 13.6 (12.0)
-    if constexpr (OUT == MX_OUT_ROWS) if (g.n_out <= 256 * 16) return mx_launch_few<IN, OUT, 1, 1, 8, 1>(s, g);
-    return mx_launch_few<IN, OUT, 1, 2, 8, 1>(s, g);
-  }
-  const MxPlan p = mx_plan<IN, OUT>(g.rows, g.n_out);
-  if constexpr (OUT == MX_OUT_ROWS) if (p.shape == MX_DIRECT) return mx_launch_few<IN, OUT, 1, 1, 8, 1>(s, g);
-  if constexpr (IN != MX_IN_BF16) if (p.shape == MX_DIRECT2) return mx_launch_few<IN, OUT, 2, 2, 8, 1>(s, g);
+static void mx_project_by(hipStream_t s, const MxArgs& g, const MxPlan& p) {
+  if constexpr (OUT == MX_OUT_ROWS) if (p.shape == MX_DIRECT) return mx_launch_few<IN, OUT, 1, 8>(s, g);
+  if (p.shape == MX_DIRECT2) return mx_launch_few<IN, OUT, 2, 8>(s, g);
   if (p.shape == MX_N256) return mx_launch<IN, OUT, 32, 2, 2, 4, 1>(s, g);
   if (p.rt == 2) mx_project_tiles<IN, OUT, 2>(s, g, p.shape);
   else if (p.rt == 3) mx_project_tiles<IN, OUT, 3>(s, g, p.shape);
   else if (p.rt == 4) mx_project_tiles<IN, OUT, 4>(s, g, p.shape);
   else mx_project_tiles<IN, OUT, 5>(s, g, p.shape);
+}
+
+template <int IN, int OUT>
+static void mx_project(hipStream_t s, const MxArgs& g) { mx_project_by<IN, OUT>(s, g, mx_plan<IN, OUT>(g.rows, g.n_out)); }
+
+// ---------------------------------------------------------------------------------
+// a model's projections
+// ---------------------------------------------------------------------------------
+static MxArgs mx_model_args(const ts_model* m, const f16_t* X, const void* W, int R, int N, int K) {
+  MxArgs g{};
+  g.w = (const uint8_t*)W;
+  g.x = X;
+  g.x_stride = act_ld(K);
+  g.x_plane = (size_t)(m->ws_rows + TS_MROWS_PER_BLOCK) * act_ld(K);
+  g.rows = R; g.n_out = N; g.n_in = K; g.chunks = g.per = (int)mx_chunks(K);
+  g.sat = m->sat_count;
+  return g;
+}
+int launch_mx_model(ts_model* m, const f16_t* X, const void* W, float* out, size_t out_elems, int R, int N, int K) {
+  MxArgs g = mx_model_args(m, X, W, R, N, K);
+  g.y = out; g.y_stride = N; g.y_f32 = 1;
+  int splits = 1;
+  const int most = (int)std::min<size_t>(16, out_elems / ((size_t)R * N));
+  MxPlan p = mx_plan_splits(R, N, g.chunks, std::max(most, 1), &splits);
+  if (const MxPlan one = mx_plan<MX_IN_PLANES, MX_OUT_ROWS>(R, N); 2.5f + (one.rounds_us - 2.5f) * g.chunks / 32.f < p.rounds_us) { p = one; splits = 1; }
+  g.per = (g.chunks + splits - 1) / splits;
+  g.y_part = (size_t)R * N;
+  mx_project_by<MX_IN_PLANES, MX_OUT_ROWS>(m->stream, g, p);
+  return splits;
+}
+void launch_mx_model_swiglu(ts_model* m, const f16_t* X, const void* W, f16_t* act_out, int R, int F, int K) {
+  MxArgs g = mx_model_args(m, X, W, R, 2 * F, K);
+  g.y = act_out; g.y_stride = act_ld(F); g.y_plane = (size_t)(m->ws_rows + TS_MROWS_PER_BLOCK) * act_ld(F);
+  mx_project<MX_IN_PLANES, MX_OUT_SWIGLU>(m->stream, g);
 }
 
 // ---------------------------------------------------------------------------------
@@ -758,7 +800,7 @@ extern "C" ts_status ts_mx_pack(const uint8_t* codes, const uint8_t* scales, int
   int dev;
   if ((st = ops_device("ts_mx_pack", {codes, scales, packed}, stream, &dev))) return st;
   DeviceGuard on(dev);
-  launch_mx_pack((hipStream_t)stream, codes, scales, n_out, n_in, packed, 0, 1);
+  launch_mx_pack((hipStream_t)stream, codes, scales, n_out, n_in, packed, 0, 1, nullptr);
   TS_HIP(hipGetLastError());
   return TS_OK;
 }
@@ -784,7 +826,7 @@ extern "C" ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_
   g.w = (const uint8_t*)packed;
   g.x = x; g.x_stride = x_stride;
   g.y = y; g.y_stride = y_stride; g.y_f32 = dtype == TS_DTYPE_F32;
-  g.n_out = n_out; g.n_in = n_in; g.chunks = (int)mx_chunks(n_in);
+  g.n_out = n_out; g.n_in = n_in; g.chunks = g.per = (int)mx_chunks(n_in);
   g.rows = (int)rows;
   if (dtype == TS_DTYPE_BF16) mx_project<MX_IN_BF16, MX_OUT_ROWS>((hipStream_t)stream, g);
   else mx_project<MX_IN_F32, MX_OUT_ROWS>((hipStream_t)stream, g);

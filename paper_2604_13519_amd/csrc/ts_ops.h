@@ -69,5 +69,7 @@ __device__ __forceinline__ void split_bf16x2(float a, float b, ts_bf16x2 (&t)[N]
 // the weights of a model with 4-bit projections (ts_mx.hip), used by the passes of toolspec.h
 size_t mx_packed_bytes(int64_t n_out, int64_t n_in);
 void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, uint8_t* codes, uint8_t* scales);
-// tiles of 16 rows go to tile n_tile0 + i * n_tile_stride of `packed`
-void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride);
+// tiles of 16 rows go to tile n_tile0 + i * n_tile_stride of `packed`; range_flag (may be null) is set where a value would not
+// fit IEEE half
+void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride,
+                    int* range_flag);
