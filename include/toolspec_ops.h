@@ -59,7 +59,7 @@ ts_status ts_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t n_out,
  * that add up to them), the sums are fp32, y is rounded once.  The order of the sums depends on
  * the sizes only, never on the contents, the device's load or the other rows.
  * A row's result does not depend on the other rows' values.
- * Errors: INVALID_ARG as above (rows in [0, 2^22], strides at least the row,
+ * Errors: INVALID_ARG as above (rows in [0, 2^19], strides at least the row,
  * x_stride at most 2^22). */
 ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_in, const void* x, int32_t dtype, int64_t rows,
                         int64_t x_stride, void* y, int64_t y_stride, ts_stream stream);
@@ -94,7 +94,7 @@ ts_status ts_kv_extend(ts_kv* kv, int32_t n_pos, ts_stream stream);
  *   row_offsets : [n_seqs + 1], non-decreasing;  lengths : [n_seqs]
  *   q, k, v     : rows of n_q_heads resp. n_kv_heads heads of head_dim, in `dtype`, with their
  *                 own strides (slices of one projection's rows will do); q and q_out may be null
- * Errors: INVALID_ARG (also n_seqs in [1, 2^20], n_rows in [0, 2^24]), DEVICE. */
+ * Errors: INVALID_ARG (also n_seqs in [1, 2^20], n_rows in [0, 2^23]), DEVICE. */
 typedef struct {
   ts_kv_pages pages;
   const int32_t* table; int64_t table_stride; int32_t table_width;
@@ -122,7 +122,8 @@ ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream stream);
  *   workspace: ts_kv_attend_workspace bytes for the same sizes, 16-byte aligned, contents irrelevant
  *              (null where that is 0)
  * Errors: INVALID_ARG (also n_q_heads not a multiple of n_kv_heads, n_seqs in [1, 2^20], max_len in
- * [0, 2^30], window < 0, scale not finite, workspace too small), DEVICE. */
+ * [0, 2^30], window < 0, scale not finite, workspace too small, n_seqs * n_q_heads or the
+ * workgroups beyond 2^24), DEVICE. */
 typedef struct {
   ts_kv_pages pages;
   const int32_t* table; int64_t table_stride; int32_t table_width;

@@ -810,7 +810,7 @@ extern "C" ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_
   ts_status st = mx_check_shape("ts_mx_project", n_out, n_in);
   if (st) return st;
   if (!ops_dtype_ok(dtype)) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: dtype must be TS_DTYPE_F32 or TS_DTYPE_BF16");
-  if (rows < 0 || rows > (1 << 22)) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: %lld rows outside [0, 2^22]", (long long)rows);
+  if (rows < 0 || rows > (1 << 19)) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: %lld rows outside [0, 2^19]", (long long)rows);
   if (rows == 0) return TS_OK;
   if (!packed || !x || !y) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: null argument");
   if (rows > 1 && x_stride > (1 << 22)) return ts_fail(TS_ERR_INVALID_ARG, "ts_mx_project: rows %lld values apart (at most 2^22)", (long long)x_stride);

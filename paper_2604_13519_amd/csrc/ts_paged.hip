@@ -611,7 +611,7 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   ts_status st = check_pages("ts_kv_append", a.pages, a.table, a.table_stride, a.table_width, a.lengths, a.n_seqs, a.dtype);
   if (st) return st;
   const int hd = a.pages.head_dim, esz = ops_esz(a.dtype);
-  if (a.n_rows < 0 || a.n_rows > (1 << 24)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: %d rows outside [0, 2^24]", a.n_rows);
+  if (a.n_rows < 0 || a.n_rows > (1 << 23)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: %d rows outside [0, 2^23]", a.n_rows);
   if (!a.row_offsets || !aligned_to(a.row_offsets, 4)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: null or misaligned row_offsets");
   if (!(a.rope_theta >= 0.f) || !(a.rope_theta < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: rope_theta %g must be zero or positive", a.rope_theta);
   if ((a.q != nullptr) != (a.q_out != nullptr)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_append: q and q_out belong together");
@@ -667,7 +667,8 @@ static ts_status check_attend(const char* call, int32_t n_seqs, int32_t hq, int3
   if (max_len < 0 || max_len > (1 << 30)) return ts_fail(TS_ERR_INVALID_ARG, "%s: max_len %d outside [0, 2^30]", call, max_len);
   if (window < 0) return ts_fail(TS_ERR_INVALID_ARG, "%s: window %d is negative", call, window);
   const int64_t groups = (int64_t)n_seqs * hkv * ((hq / hkv + 15) / 16) * attend_splits_room(n_seqs, hq, hkv, max_len, window);
-  if (groups > 0x7fffffff || (int64_t)n_seqs * hq > 0x7fffffff) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d sequences of %d heads are too many for one call", call, n_seqs, hq);
+  constexpr int64_t kMost = (1 << 24) - 1;                   // workgroups of 256 whose threads a launch can count
+  if (groups > kMost || (int64_t)n_seqs * hq > kMost) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d sequences of %d heads are too many for one call", call, n_seqs, hq);
   return TS_OK;
 }
 

@@ -63,7 +63,7 @@ def test_pack_and_project_refusals(lib):
     p = lib.ts_mx_project
     refused(p(P, 16, 32, P, 3, 1, 32, P, 16, None), "dtype")
     refused(p(P, 16, 32, P, 1, -1, 32, P, 16, None), "rows")
-    refused(p(P, 16, 32, P, 1, (1 << 22) + 1, 32, P, 16, None), "rows")
+    refused(p(P, 16, 32, P, 1, (1 << 19) + 1, 32, P, 16, None), "rows")
     refused(p(P, 16, 32, P, 1, 1, 31, P, 16, None), "strides")
     refused(p(P, 16, 32, P, 1, 1, 32, P, 15, None), "strides")
     refused(p(P, 16, 32, P, 1, 2, (1 << 22) + 1, P, 16, None), "apart")
@@ -109,7 +109,7 @@ SHARED = [(dict(pages_k=None), "null"), (dict(pages_v=None), "null"), (dict(tabl
 
 
 @pytest.mark.parametrize("kw,word", SHARED + [
-    (dict(n_rows=-1), "rows"), (dict(n_rows=(1 << 24) + 1), "rows"), (dict(row_offsets=None), "row_offsets"), (dict(row_offsets=P + 2), "row_offsets"),
+    (dict(n_rows=-1), "rows"), (dict(n_rows=(1 << 23) + 1), "rows"), (dict(row_offsets=None), "row_offsets"), (dict(row_offsets=P + 2), "row_offsets"),
     (dict(rope_theta=-1.0), "rope_theta"), (dict(rope_theta=float("inf")), "rope_theta"), (dict(rope_theta=float("nan")), "rope_theta"),
     (dict(q=None), "belong together"), (dict(q_out=None), "belong together"), (dict(n_q_heads=0), "query heads"), (dict(k=None), "null"), (dict(v=None), "null"),
     (dict(k_stride=127), "stride"), (dict(v_stride=1), "stride"), (dict(q_out_stride=0), "stride"), (dict(k=P + 1), "aligned"), (dict(v=P + 1), "aligned")])
@@ -121,7 +121,7 @@ def test_append_refusals(lib, kw, word):
     (dict(n_q_heads=3), "query heads"), (dict(n_q_heads=0), "query heads"), (dict(max_len=-1), "max_len"), (dict(max_len=(1 << 30) + 1), "max_len"),
     (dict(window=-1), "window"), (dict(scale=float("inf")), "scale"), (dict(scale=float("nan")), "scale"), (dict(q=None), "null"), (dict(out=None), "null"),
     (dict(out_stride=100), "stride"), (dict(lse=P + 2), "aligned"), (dict(max_len=100000), "workspace"), (dict(max_len=100000, workspace=P, workspace_bytes=1024), "workspace"),
-    (dict(max_len=100000, workspace=P + 4, workspace_bytes=1 << 30), "workspace"), (dict(n_seqs=1 << 20, n_q_heads=65536), "too many")])
+    (dict(max_len=100000, workspace=P + 4, workspace_bytes=1 << 30), "workspace"), (dict(n_seqs=1 << 20, n_q_heads=65536), "too many"), (dict(n_seqs=1 << 20, n_q_heads=32), "too many")])
 def test_attend_refusals(lib, kw, word):
     refused(lib.ts_kv_attend(C.byref(attend_args(**kw)), None), word)
 
