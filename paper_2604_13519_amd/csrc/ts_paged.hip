@@ -11,6 +11,9 @@
 // heads: the values are transposed within a page, so a page's 16 positions of a dimension are one 32-byte (fp32: 64)
 // piece, written whole.  The angle of position p and pair j is p theta^(-2 j / hd); as a number of turns it is formed and
 // reduced to [-1/2, 1/2] in 64 bits, so that far positions keep their phase, and sine and cosine are taken in fp32.
+//
+// Bound by the start of a launch for a step's rows (one row, 8 + 32 heads of 128: 3.9 us, of which starting a launch is 2 to 3) and by HBM
+// for contexts: 2040 rows of 8 + 64 heads move 80 MB (as counted) in 20 us, 4 TB/s; 2048 rows on whole pages 4.8 TB/s.
 // ---------------------------------------------------------------------------------
 constexpr int APPEND_THREADS = 256, APPEND_HEADS = 8;
 
@@ -232,6 +235,9 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
 // takes key 8 (m / 4) + 4 t + m % 4 as its row m: then the probabilities a lane has computed are, in place, the operand
 // it needs, and the matching values are 16 contiguous bytes of the transposed page.  Maximum and sum of a head lie in
 // four lanes (l, l + 16, l + 32, l + 48); nothing passes through the LDS before the waves of a workgroup are joined.
+//
+// bf16, 8 KV heads of 128: 8 sequences of up to 32768 tokens, 64 query heads (728 MB, as counted): 136 us, 5.4 TB/s, a kernel
+// that only reads the same bytes takes 123; one sequence of 8192, 32 query heads (34 MB): 9.0 us and 3.5 of the join.
 // ---------------------------------------------------------------------------------
 constexpr int ATT_WAVES = 4, ATT_KB = 32;
 
@@ -512,7 +518,8 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
 
 // The join of a sequence's splits: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A workgroup per (sequence, head):
 // the weights of the splits first, into the LDS, then four dimensions a thread and the splits dealt to the 1024 / HD rows
-// of threads, so that a row's reads are few and all in flight at once.
+// of threads, so that a row's reads are few and all in flight at once.  A launch of its own, 3.5 us: joining in the last
+// workgroup to end needs the parts written through to memory by every workgroup, and one sequence of 8192 took 62 us so, not 12.5.
 constexpr int ATT_SPLITS = 512;                              // at most, see attend_cut
 template <typename TQ, int HD>
 __global__ __launch_bounds__(256) void k_kv_attend_join(AttendArgs g) {
@@ -630,9 +637,13 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   g.a = a;
   g.log2_theta = a.rope_theta > 0.f ? log2((double)a.rope_theta) : 0.0;
   const int heads = (a.q ? a.n_q_heads : 0) + 2 * a.pages.n_kv_heads;
-  // Single rows: a workgroup each.  Contexts: one for 16 rows, most of which its page's first row takes along anyway:
-  // @@APP@@
-  g.window = a.n_rows > 16 * (int64_t)a.n_seqs ? 16 : 1;
+  // A workgroup's window, from the rows a sequence has on average: pages of one window are written one after the other, but
+  // the more windows, the more workgroups only find that another takes their rows along.  bf16, 8 KV heads of 128, 32 query
+  // heads, microseconds at windows 1 / 2 / 4 / 8 / 16: 512 sequences of 1 row 15 / 16 / 18 / 28 / 46, of 2 rows 29 / 20 / 23 / 26
+  // / 44; 64 of 8 rows 20 / 15 / 13 / 17 / 19, of 20 rows 24 / 18 / 17 / 15 / 18; 1 of 128 rows 7.4 / 6.8 / 5.4 / 5.4 / 7.7,
+  // of 512 rows 17.5 / 13.9 / 9.0 / 6.9 / 8.1, of 2048 rows 55 / 38 / 22 / 14.5 / 11.3.
+  const int each = a.n_rows / a.n_seqs;
+  g.window = each < 2 ? 1 : each < 8 ? 2 : each < 512 ? 4 : each < 2048 ? 8 : 16;
   const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + APPEND_HEADS - 1) / APPEND_HEADS);
   hipStream_t s = (hipStream_t)stream;
   const bool in16 = a.dtype == TS_DTYPE_BF16, c16 = a.pages.dtype == TS_DTYPE_BF16;
@@ -642,8 +653,10 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   return TS_OK;
 }
 
-// How a call is cut: chunks of 128 keys or a multiple, so many that about four workgroups a CU are there for the longest
-// sequences; the number never falls when max_len grows.
+// How a call is cut: chunks of 128 keys or a multiple, so many that the longest sequences give two workgroups a CU, what is
+// resident at once; the number never falls when max_len grows.  bf16, 8 KV heads of 128, 4 query heads each: one sequence of
+// 8192 keys in chunks of 128 12.5 us, of 256 14.0; 8 of 4096 in chunks of 1024 21.3, of 512 23.4; 64 of 2048 whole 70.9, in
+// two 80; 8 of up to 32768 in chunks of 4096 145, of 1024 the same.
 constexpr int ATT_GROUPS = 2 * 256;
 static void attend_cut(int64_t n_seqs, int hq, int hkv, int max_len, int window, int* chunk, int* splits) {
   const int tiles = (hq / hkv + 15) / 16;
