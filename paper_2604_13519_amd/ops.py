@@ -3,6 +3,8 @@
 Function names mirror the header.  A call checks what the tensors themselves tell (types, shapes, devices, contiguity
 within a row), allocates outputs that it is not given, and enqueues on the current stream of the tensors' GPU; whatever
 is wrong raises before anything is enqueued.  The arithmetic is the library's: there is no fallback.
+
+Import this module (or torch) before the library is loaded: it then runs on torch's HIP runtime, and not on one of its own.
 """
 import ctypes as C
 
@@ -45,6 +47,11 @@ def _load():
     global _lib
     lib = binding.load_library()
     if _lib is not lib:
+        with open("/proc/self/maps") as maps:
+            runtimes = {line.split()[-1] for line in maps if "libamdhip64" in line}
+        if len(runtimes) > 1:                              # torch's and the system's: neither knows the other's memory and streams
+            raise RuntimeError("the library was loaded before torch, and each uses a HIP runtime of its own (%s): import torch, or this module, before "
+                               "binding.load_library" % ", ".join(sorted(runtimes)))
         p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
         for name, args in {
             "ts_mx_quantize": [p, i32, i64, i64, i64, p, p, p],

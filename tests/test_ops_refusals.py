@@ -3,6 +3,8 @@ never reach a kernel), the exports, and the sizes the host computes."""
 import ctypes as C
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -159,3 +161,11 @@ def test_tensors_are_looked_at(lib):
         ops.ts_mx_dequantize(torch.zeros((4, 32), dtype=torch.uint8), torch.zeros((4, 2), dtype=torch.uint8), 64)
     with pytest.raises(ValueError, match="k_pages"):
         ops.ts_kv_attend(torch.zeros((3, 2, 16, 64)), torch.zeros((3, 2, 64, 16)), torch.zeros((1, 3), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros((1, 128)), 40)
+
+
+def test_a_library_on_another_hip_runtime_than_torch_is_refused(lib):
+    code = "from paper_2604_13519_amd import binding as B\nB.load_library()\nfrom paper_2604_13519_amd import ops\ntry: ops.ts_mx_packed_bytes(16, 128)\nexcept RuntimeError as e: print(e)"
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    with open("/proc/self/maps") as maps:                  # here torch came first: one runtime
+        assert len({line.split()[-1] for line in maps if "libamdhip64" in line}) == 1
+    assert r.returncode == 0 and "before torch" in r.stdout, (r.stdout, r.stderr)
