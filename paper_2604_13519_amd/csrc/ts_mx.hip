@@ -431,8 +431,9 @@ __global__ __launch_bounds__(KW * 64) void k_mx_few(MxArgs g) {
 // and weights are requested a step ahead.
 // bf16 rows, 4096 inputs: 2048 rows x 14336 columns 200 us, 1.2 PFLOP/s, what the library's product of bf16 matrices of these
 // sizes takes (199); the matrix pipes are busy 65 % of the time, the rest is issuing the widening of the codes, the
-// reads of the LDS and the barrier.  65 rows x 28672 columns 22 - 24 us: its 67 MB need 12 at a copy's rate; 42 % busy, each step waits
-// for its rows.
+// reads of the LDS and the barrier.  65 rows x 28672 columns 22 - 25 us: its 67 MB need 12 at a copy's rate, its
+// 65 rows 13 at the library's rate, the 80 it multiplies 16.  Rows or weights requested two or three steps ahead are no
+// faster (25 - 26 us), nor are waves of 64 columns, which read half as much from the LDS (28 us with KW 2, 36 with 4).
 template <int T> struct MxTile;
 template <> struct MxTile<16> { typedef ts_f32x4 Acc; };
 template <> struct MxTile<32> { typedef float Acc __attribute__((ext_vector_type(16))); };
