@@ -194,8 +194,13 @@ __global__ __launch_bounds__(256) void k_mx_pack(const uint8_t* codes, const uin
 
 void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, int n_out, int n_in, void* packed, int n_tile0, int n_tile_stride,
                     int* range_flag) {
-  const int64_t records = (int64_t)((n_out + 15) / 16) * mx_chunks(n_in);
-  k_mx_pack<<<(uint32_t)((records + 3) / 4), 256, 0, s>>>(codes, scales, n_out, n_in, (uint8_t*)packed, n_tile0, n_tile_stride, (int)mx_chunks(n_in), records, range_flag);
+  const int64_t chunks = mx_chunks(n_in), blocks = (n_in + 31) / 32, slab = ((int64_t)1 << 25) / chunks * 16;     // rows: threads within 32 bits
+  for (int64_t r = 0; r < n_out; r += slab) {
+    const int n = (int)std::min(slab, n_out - r);
+    const int64_t records = (n + 15) / 16 * chunks;
+    k_mx_pack<<<(uint32_t)((records + 3) / 4), 256, 0, s>>>(codes + r * blocks * 16, scales + r * blocks, n, n_in, (uint8_t*)packed, n_tile0 + (int)(r / 16) * n_tile_stride,
+                                                            n_tile_stride, (int)chunks, records, range_flag);
+  }
 }
 
 // ---------------------------------------------------------------------------------

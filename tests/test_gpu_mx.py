@@ -236,6 +236,27 @@ def test_on_another_stream_and_captured():
         assert torch.equal(codes, c) and torch.equal(scales, e)
 
 
+def test_pack_more_records_than_one_launch_counts():
+    n_out, n_in = (1 << 24) - 24, 4224                      # 33 records a row tile: 2^25 records end inside the matrix
+    blocks = n_in // 32
+    if torch.cuda.mem_get_info()[0] < (100 << 30):
+        pytest.skip("100 GB of device memory are needed")
+    codes = torch.zeros((n_out, 16 * blocks), dtype=torch.uint8, device="cuda")
+    scales = torch.full((n_out, blocks), 127, dtype=torch.uint8, device="cuda")
+    edge = (1 << 25) // 33 * 16
+    spans = [(0, 48), (edge - 32, edge + 32), (n_out - 40, n_out)]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for lo, hi in spans:
+        codes[lo:hi] = torch.randint(0, 256, (hi - lo, 16 * blocks), dtype=torch.uint8, device="cuda", generator=gen)
+        scales[lo:hi] = torch.randint(0, 255, (hi - lo, blocks), dtype=torch.uint8, device="cuda", generator=gen)
+    packed = ops.ts_mx_pack(codes, scales, n_in).view(-1, 33, 1088)
+    for lo, hi in spans:
+        want = ops.ts_mx_pack(codes[lo:hi].contiguous(), scales[lo:hi].contiguous(), n_in).view(-1, 33, 1088)
+        assert lo % 16 == 0 and torch.equal(packed[lo // 16:lo // 16 + want.shape[0]], want)
+    del codes, scales, packed
+    torch.cuda.empty_cache()
+
+
 def test_pointers_of_the_host_are_refused():
     lib = ops._load()
     x = torch.zeros((4, 64), device="cuda")
