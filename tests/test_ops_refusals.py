@@ -169,3 +169,18 @@ def test_a_library_on_another_hip_runtime_than_torch_is_refused(lib):
     with open("/proc/self/maps") as maps:                  # here torch came first: one runtime
         assert len({line.split()[-1] for line in maps if "libamdhip64" in line}) == 1
     assert r.returncode == 0 and "before torch" in r.stdout, (r.stdout, r.stderr)
+
+
+@pytest.mark.parametrize("cls,pack", [(ops.ts_kv_append_args, ops._pack_append), (ops.ts_kv_attend_args, ops._pack_attend)])
+def test_packed_arguments_are_the_structure(cls, pack):
+    values = []
+
+    def fill(part):
+        for name, kind in part._fields_:
+            if issubclass(kind, C.Structure):
+                fill(getattr(part, name))
+            else:
+                values.append(0.5 + len(values) if kind is C.c_float else 3 + 1000 * len(values))
+                setattr(part, name, values[-1])
+        return part
+    assert bytes(fill(cls())) == pack(*values)
