@@ -653,25 +653,33 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   return TS_OK;
 }
 
-// How a call is cut: chunks of 128 keys or a multiple, so many that the longest sequences give two workgroups a CU, what is
-// resident at once; the number never falls when max_len grows.  bf16, 8 KV heads of 128, 4 query heads each: one sequence of
-// 8192 keys in chunks of 128 12.5 us, of 256 14.0; 8 of 4096 in chunks of 1024 21.3, of 512 23.4; 64 of 2048 whole 70.9, in
-// two 80; 8 of up to 32768 in chunks of 4096 145, of 1024 the same.
-constexpr int ATT_GROUPS = 2 * 256;
-static void attend_cut(int64_t n_seqs, int hq, int hkv, int max_len, int window, int* chunk, int* splits) {
-  const int tiles = (hq / hkv + 15) / 16;
+// How a call is cut.  The longest sequences give a workgroup a CU: two a CU, in shorter chunks, are slower (bf16, 8 KV heads of
+// 128, 4 query heads each, microseconds: 8 sequences of 2048 keys 18.1, one a CU 16.8; of 32768 191 and 183; ragged ones, up to
+// 32768, 134 and 117; 16 ragged ones up to 2048 20.5 and 18.9), and so is less than one (8 ragged up to 2048: 16.8, not 12.7).
+// Only where they leave chunks of 128 keys, two a CU are as fast or faster: 8 of 1024 10.0 and 10.5, one of 8192 12.5 and 14.0.
+// A sequence of few keys is not cut, whose join (3.1) takes longer than what it saves, 1.05 per 128 keys of 256 bytes: 256 keys
+// whole 6.2, cut 7.5; 384 7.3 and 7.6; 512 8.4 and 7.4; of 128 bytes 512 keys 5.8 and 7.1, 1024 7.9 and 7.0; of 512 bytes 256 keys
+// 10.9 and 9.5.
+constexpr int ATT_CUS = 256;
+static int64_t attend_units(int max_len, int window) {       // of 128 keys, in the longest sequence
   const int64_t span = window > 0 && window < max_len ? (int64_t)window + ATT_KB - 1 : max_len;
-  const int64_t unit = ATT_WAVES * ATT_KB, units = std::max<int64_t>(1, (span + unit - 1) / unit);
-  const int64_t want = std::max<int64_t>(1, ATT_GROUPS / (n_seqs * hkv * tiles));
-  const int64_t per = (units + want - 1) / want;             // units a chunk
-  *chunk = (int)(per * unit);
+  return std::max<int64_t>(1, (span + ATT_WAVES * ATT_KB - 1) / (ATT_WAVES * ATT_KB));
+}
+static int64_t attend_whole(int64_t n_seqs, int hq, int hkv) { return n_seqs * hkv * ((hq / hkv + 15) / 16); }
+static void attend_cut(int64_t n_seqs, int hq, int hkv, int key_bytes, int max_len, int window, int* chunk, int* splits) {
+  const int64_t whole = attend_whole(n_seqs, hq, hkv), units = attend_units(max_len, window);
+  int64_t per = 1;                                           // units a chunk
+  if (units <= (key_bytes <= 128 ? 4 : key_bytes <= 256 ? 3 : 1)) per = units;
+  else if (units * whole > 2 * ATT_CUS) {
+    const int64_t want = std::max<int64_t>(1, ATT_CUS / whole);
+    per = (units + want - 1) / want;
+  }
+  *chunk = (int)(per * ATT_WAVES * ATT_KB);
   *splits = (int)((units + per - 1) / per);
 }
+// the most splits that this max_len or a smaller one gets
 static int64_t attend_splits_room(int64_t n_seqs, int hq, int hkv, int max_len, int window) {
-  const int tiles = (hq / hkv + 15) / 16;
-  const int64_t span = window > 0 && window < max_len ? (int64_t)window + ATT_KB - 1 : max_len;
-  const int64_t unit = ATT_WAVES * ATT_KB, units = std::max<int64_t>(1, (span + unit - 1) / unit);
-  return std::min(units, std::max<int64_t>(1, ATT_GROUPS / (n_seqs * hkv * tiles)));
+  return std::min(attend_units(max_len, window), std::max<int64_t>(1, 2 * ATT_CUS / attend_whole(n_seqs, hq, hkv)));
 }
 
 static ts_status check_attend(const char* call, int32_t n_seqs, int32_t hq, int32_t hkv, int32_t max_len, int32_t window) {
@@ -679,7 +687,7 @@ static ts_status check_attend(const char* call, int32_t n_seqs, int32_t hq, int3
   if (hkv < 1 || hkv > 65536 || hq < 1 || hq > 65536 || hq % hkv) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d query heads over %d KV heads", call, hq, hkv);
   if (max_len < 0 || max_len > (1 << 30)) return ts_fail(TS_ERR_INVALID_ARG, "%s: max_len %d outside [0, 2^30]", call, max_len);
   if (window < 0) return ts_fail(TS_ERR_INVALID_ARG, "%s: window %d is negative", call, window);
-  const int64_t groups = (int64_t)n_seqs * hkv * ((hq / hkv + 15) / 16) * attend_splits_room(n_seqs, hq, hkv, max_len, window);
+  const int64_t groups = attend_whole(n_seqs, hq, hkv) * attend_splits_room(n_seqs, hq, hkv, max_len, window);
   constexpr int64_t kMost = (1 << 24) - 1;                   // workgroups of 256 whose threads a launch can count
   if (groups > kMost || (int64_t)n_seqs * hq > kMost) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d sequences of %d heads are too many for one call", call, n_seqs, hq);
   return TS_OK;
@@ -730,7 +738,7 @@ extern "C" ts_status ts_kv_attend(const ts_kv_attend_args* args, ts_stream strea
   if (!(fabsf(a.scale) < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_attend: scale must be finite");
   AttendArgs g{};
   g.a = a;
-  attend_cut(a.n_seqs, a.n_q_heads, a.pages.n_kv_heads, a.max_len, a.window, &g.chunk, &g.splits);
+  attend_cut(a.n_seqs, a.n_q_heads, a.pages.n_kv_heads, a.pages.head_dim * ops_esz(a.pages.dtype), a.max_len, a.window, &g.chunk, &g.splits);
   if (g.splits > 1) {
     uint64_t need = 0;
     if ((st = ts_kv_attend_workspace(a.n_seqs, a.n_q_heads, a.pages.n_kv_heads, a.pages.head_dim, a.max_len, a.window, &need))) return st;
