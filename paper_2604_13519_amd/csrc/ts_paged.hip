@@ -236,8 +236,8 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
 // it needs, and the matching values are 16 contiguous bytes of the transposed page.  Maximum and sum of a head lie in
 // four lanes (l, l + 16, l + 32, l + 48); nothing passes through the LDS before the waves of a workgroup are joined.
 //
-// bf16, 8 KV heads of 128: 8 sequences of up to 32768 tokens, 64 query heads (728 MB, as counted): 136 us, 5.4 TB/s, a kernel
-// that only reads the same bytes takes 123; one sequence of 8192, 32 query heads (34 MB): 9.0 us and 3.5 of the join.
+// bf16, 8 KV heads of 128: 8 sequences of up to 32768 tokens, 64 query heads (727 MB, as counted): 125.5 us, 5.8 TB/s, a kernel
+// that only reads the same bytes takes 123; one sequence of 8192, 32 query heads (34 MB): 8.9 us and 3.1 of the join.
 // ---------------------------------------------------------------------------------
 constexpr int ATT_WAVES = 4, ATT_KB = 32;
 
@@ -450,7 +450,8 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
           for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(ts_f32x4, f.v[t][d])[r], x[4 * t + r], o[d], 0, 0, 0);
     }
   };
-  // One block's keys and values are on their way while another is used, and the pages of the one after are known.  The
+  // One block's keys and values are on their way while another is used (two or three were no faster: 8 sequences of 8192 tokens
+  // 45.0, 46.0 and 47.4 us), and the pages of the one after are known.  The
   // request is made on every path - past the end for the last block again - because the waits count the loads behind
   // the ones they wait for: with a path that requests nothing they would wait for the request as well.
   constexpr int STEP = ATT_WAVES * ATT_KB;
@@ -518,7 +519,7 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
 
 // The join of a sequence's splits: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A workgroup per (sequence, head):
 // the weights of the splits first, into the LDS, then four dimensions a thread and the splits dealt to the 1024 / HD rows
-// of threads, so that a row's reads are few and all in flight at once.  A launch of its own, 3.5 us: joining in the last
+// of threads, so that a row's reads are few and all in flight at once.  A launch of its own, 3.1 us: joining in the last
 // workgroup to end needs the parts written through to memory by every workgroup, and one sequence of 8192 took 62 us so, not 12.5.
 constexpr int ATT_SPLITS = 512;                              // at most, see attend_cut
 template <typename TQ, int HD>
@@ -643,7 +644,7 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   // / 44; 64 of 8 rows 20 / 15 / 13 / 17 / 19, of 20 rows 24 / 18 / 17 / 15 / 18; 1 of 128 rows 7.4 / 6.8 / 5.4 / 5.4 / 7.7,
   // of 512 rows 17.5 / 13.9 / 9.0 / 6.9 / 8.1, of 2048 rows 55 / 38 / 22 / 14.5 / 11.3.
   const int each = a.n_rows / a.n_seqs;
-  g.window = each < 2 ? 1 : each < 8 ? 2 : each < 512 ? 4 : each < 2048 ? 8 : 16;
+  g.window = each < 2 ? 1 : each < 8 ? 2 : each < 256 ? 4 : each < 1024 ? 8 : 16;
   const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + APPEND_HEADS - 1) / APPEND_HEADS);
   hipStream_t s = (hipStream_t)stream;
   const bool in16 = a.dtype == TS_DTYPE_BF16, c16 = a.pages.dtype == TS_DTYPE_BF16;
