@@ -15,7 +15,7 @@
 // Bound by the start of a launch for a step's rows (one row, 8 + 32 heads of 128: 3.9 us, of which starting a launch is 2 to 3) and by HBM
 // for contexts: 2040 rows of 8 + 64 heads move 80 MB (as counted) in 20 us, 4 TB/s; 2048 rows on whole pages 4.8 TB/s.
 // ---------------------------------------------------------------------------------
-constexpr int APPEND_THREADS = 256, APPEND_HEADS = 8;
+constexpr int APPEND_THREADS = 256, APPEND_HEADS = 32;     // heads of a workgroup at most
 
 template <typename T> __device__ __forceinline__ float widen(T v) {
   if constexpr (sizeof(T) == 2) return bf16_to_f32(v);
@@ -74,7 +74,7 @@ __device__ __forceinline__ void store_some(T* p, int p0, int lo, int hi, const f
 struct AppendArgs {
   ts_kv_append_args a;
   double log2_theta;                     // rope_theta > 0
-  int window;                            // rows a workgroup looks for pages in
+  int window, heads;                     // of a workgroup: rows it looks for pages in, heads
 };
 
 // the last sequence whose first row is not behind `row`, -1 if none: 64 offsets at a time, one per lane
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
   __shared__ double freq[HALF];
   const ts_kv_append_args& a = g.a;
   const int tid = threadIdx.x, hkv = a.pages.n_kv_heads, hq = a.q ? a.n_q_heads : 0;
-  const int head0 = blockIdx.y * APPEND_HEADS, turned = hq + hkv, head1 = min(head0 + APPEND_HEADS, turned + hkv);
+  const int head0 = blockIdx.y * g.heads, turned = hq + hkv, head1 = min(head0 + g.heads, turned + hkv);
   const bool turn = a.rope_theta > 0.f && head0 < turned;
   if (turn && tid < HALF) freq[tid] = exp2(g.log2_theta * (-2.0 * tid / HD)) * 0.15915494309189535;      // turns per position
 
@@ -645,7 +645,11 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   // of 512 rows 17.5 / 13.9 / 9.0 / 6.9 / 8.1, of 2048 rows 55 / 38 / 22 / 14.5 / 11.3.
   const int each = a.n_rows / a.n_seqs;
   g.window = each < 2 ? 1 : each < 8 ? 2 : each < 256 ? 4 : each < 1024 ? 8 : 16;
-  const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + APPEND_HEADS - 1) / APPEND_HEADS);
+  // Its heads: many sequences with a few rows each are many pages with little on them, and where a page's rows go and their
+  // sines are the work: 8 / 32 heads, 64 sequences of 1 row 4.8 / 5.3 us, 128 5.8 / 6.0, 256 9.2 / 7.6, 1024 29 / 20; 64 of 4
+  // rows 9.7 / 10.3, 128 17 / 14, 512 43 / 32; contexts 2040 rows of 5 21 / 23, 2048 of 1 12 / 18.
+  g.heads = a.n_seqs >= 128 && each < 16 ? APPEND_HEADS : 8;
+  const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + g.heads - 1) / g.heads);
   hipStream_t s = (hipStream_t)stream;
   const bool in16 = a.dtype == TS_DTYPE_BF16, c16 = a.pages.dtype == TS_DTYPE_BF16;
   in16 ? c16 ? launch_append<bf16_t, bf16_t>(g, hd, grid, s) : launch_append<bf16_t, float>(g, hd, grid, s)

@@ -319,6 +319,20 @@ def test_append_many_sequences():
         check_append([int(x) for x in rng.integers(0, 20, n)], new, 1, 1, 64, torch.bfloat16, torch.bfloat16, 1e4, seed=n, pad=1)
 
 
+@pytest.mark.parametrize("dtype,rdtype", TYPES)
+@pytest.mark.parametrize("most", [2, 6, 14, 30])
+def test_append_many_sequences_of_many_heads(dtype, rdtype, most):
+    rng = np.random.default_rng(most)
+    for n, hq, hkv in ((127, 5, 2), (130, 31, 5)):
+        new = [int(x) for x in rng.integers(most // 2, most + 1, n)]
+        check_append([int(x) for x in rng.integers(0, 20, n)], new, hq, hkv, 64, dtype, rdtype, 1e4, seed=n + most, pad=1)
+
+
+@pytest.mark.parametrize("new", [[300], [9, 700, 0, 260], [1100, 1030]])
+def test_append_long_contexts(new):
+    check_append([5 + 7 * i for i in range(len(new))], new, 3, 1, 64, torch.bfloat16, torch.bfloat16, 1e6, seed=len(new), pad=2)
+
+
 def test_append_far_positions_keep_their_phase():
     """Positions up to 2^27 on one page each: the table points them all at a few pages."""
     hd, width = 64, (1 << 27) // 16 + 1
