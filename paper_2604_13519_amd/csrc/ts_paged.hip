@@ -272,9 +272,15 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
   const ts_kv_attend_args& a = g.a;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 16, lg = lane / 16;
   // neighbours take the KV heads of the same positions: a page's heads lie side by side in memory and are read together
-  int id = blockIdx.x;
+  int id = blockIdx.x, tile = 0;
+  // Tiles of the same keys are 8 apart (fewer at the end), on one XCD, whose cache serves all but the first: 8 sequences of 8192,
+  // 64 heads over one KV head 19.7 us, as neighbours 27.3.
+  if (g.tiles > 1) {
+    const int u0 = id / (8 * g.tiles) * 8, width = min(8, (int)(gridDim.x / g.tiles) - u0), in = id - u0 * g.tiles;
+    tile = in / width;
+    id = u0 + in % width;
+  }
   const int hkv = a.pages.n_kv_heads, kvh = id % hkv; id /= hkv;
-  const int tile = id % g.tiles; id /= g.tiles;
   const int split = id % g.splits, seq = id / g.splits;
   int lo, hi, base;
   seen_range(a, seq, lo, hi, base);
