@@ -641,8 +641,10 @@ static void mx_launch(hipStream_t s, const MxArgs& g) {
 }
 
 // Which shape a call takes: the one whose rounds of workgroups (256 CUs) times the time of a round is least.  The times are
-// microseconds of one round at 4096 inputs, measured between events with an eighth of the CUs to all of them at work; all
-// shapes scale alike with the inputs.  For 2, 3, 4, 5 row tiles of 16 (more rows: blocks of 4 tiles), columns a workgroup:
+// microseconds of one round at 4096 inputs, measured between events with an eighth of the CUs to all of them at work; what is
+// beyond a start of 2.2 (direct) or 2.6 scales with the inputs.  Several blocks of fewer rows are offered as well as one: 64 rows
+// x 14336 inputs, 4096 columns: two blocks of 32 rows 17.9 us, one of 64 on half the CUs 30.8; 128 fp32 rows, 6144 columns 36.7, 45.6.
+// For 2, 3, 4, 5 row tiles of 16, columns a workgroup:
 //   bf16 rows   32:  6.8   8.7  12.1  13.0     64:  7.9  10.0  12.8  14.7     128: 11.5  14.8  17.3  20.8
 //   fp32 rows                                  64: 24.8  35.3  45.8  52       128: 35    47    61.6  73
 //   planes                                     64: 12.8  16.9  21.9  26.8     128: 23.1  29.5  37    44.2
@@ -653,30 +655,40 @@ static void mx_launch(hipStream_t s, const MxArgs& g) {
 // 65 rows x 4096 inputs, 28672 columns: 128 columns wide 22.3 us, 64 wide 29.8, 32 wide 47.4, 256 wide 31.6; 4096
 // columns: 32 wide 13.0, 64 wide 14.7, 128 wide 20.9.
 enum { MX_DIRECT, MX_DIRECT2, MX_N32, MX_N64, MX_N128, MX_N256 };
-struct MxPlan { int shape, rt; float rounds_us; };
+struct MxPlan { int shape, rt; float us; };
 static constexpr float mx_round_us[3][3][4] = {{{6.8f, 8.7f, 12.1f, 13.0f}, {7.9f, 10.0f, 12.8f, 14.7f}, {11.5f, 14.8f, 17.3f, 20.8f}},
                                                {{0, 0, 0, 0}, {24.8f, 35.3f, 45.8f, 52.f}, {35.f, 47.f, 61.6f, 73.f}},
                                                {{0, 0, 0, 0}, {12.8f, 16.9f, 21.9f, 26.8f}, {23.1f, 29.5f, 37.f, 44.2f}}};
 static constexpr float mx_wide_us[3] = {30.5f, 84.f, 52.6f};
 static float mx_groups(int rows, int n_out, int mt, int nt) { return (float)((rows + mt - 1) / mt) * (float)((n_out + nt - 1) / nt); }
-static int mx_row_tiles(int rows) { return rows > 80 ? 4 : std::max(2, (rows + 15) / 16); }
+static int mx_row_tiles(int rows) { return std::clamp((rows + 15) / 16, 2, 5); }       // at most, of 16
+// Several blocks of planes hold their times only in blocks of 64 rows, or up to three smaller ones: 520 rows x 4096 inputs, 4096
+// columns in blocks of 48 or 80 53 us, not 48 and 42, 64 rows by 256 columns 43; 132 rows, 28672 columns, two blocks of 80 rows
+// 76 us, three of 48 68, of 64 91.
+template <int IN> static bool mx_blocks_hold(int rows, int rt) {
+  return IN != MX_IN_PLANES || rt == 4 || (rt == 5 ? rows <= 80 : rows <= 48 * rt);
+}
 
 template <int IN, int OUT>
-static MxPlan mx_plan(int rows, int n_out) {
+static MxPlan mx_plan(int rows, int n_out, int chunks) {
   // one round: [0] + [1] r, of several each: [2] + [3] r
   static constexpr float direct_us[3][2][4] = {{{3.6f, 0.22f, 2.4f, 0.21f}, {4.0f, 0.2f, 2.8f, 0.2f}},
                                                {{7.2f, 0.29f, 4.6f, 0.31f}, {7.6f, 0.25f, 5.6f, 0.28f}},
                                                {{4.9f, 0.42f, 2.6f, 0.4f}, {5.0f, 0.42f, 3.7f, 0.42f}}};
-  const int rt = mx_row_tiles(rows);
+  const int rts = mx_row_tiles(rows);
   const float r = (float)std::min(rows, 16);
   auto share = [&](int mt, int nt) { return mx_groups(rows, n_out, mt, nt) / 256.f; };
-  MxPlan best{MX_N256, rt, ceilf(share(64, 256)) * mx_wide_us[IN]};
-  auto offer = [&](int shape, float cost) { if (cost < best.rounds_us) { best.rounds_us = cost; best.shape = shape; } };
+  auto scaled = [&](float start, float us) { return start + (us - start) * (float)chunks / 32.f; };
+  MxPlan best{MX_N256, 0, scaled(2.6f, ceilf(share(64, 256)) * mx_wide_us[IN])};
+  auto offer = [&](int shape, int rt, float cost) { if (cost < best.us) best = MxPlan{shape, rt, cost}; };
   for (int w = IN == MX_IN_BF16 ? 0 : 1; w < 3; ++w)
-    if (OUT == MX_OUT_ROWS || w == 2) offer(MX_N32 + w, ceilf(share(16 * rt, 32 << w)) * mx_round_us[IN][w][rt - 2]);
+    if (OUT == MX_OUT_ROWS || w == 2)
+      for (int rt = rts; rt >= 2; --rt)
+        if (mx_blocks_hold<IN>(rows, rt)) offer(MX_N32 + w, rt, scaled(2.6f, ceilf(share(16 * rt, 32 << w)) * mx_round_us[IN][w][rt - 2]));
   for (int w = OUT == MX_OUT_ROWS ? 0 : 1; w < 2; ++w) {
     const float* us = direct_us[IN][w];
-    offer(MX_DIRECT + w, std::max(us[0] + us[1] * r, ceilf(share(16, 16 << w)) * (us[2] + us[3] * r)));
+    const float rounds = share(16, 16 << w);                 // past two they run into each other
+    offer(MX_DIRECT + w, 0, scaled(2.2f, std::max(us[0] + us[1] * r, (rounds > 2.f ? rounds : ceilf(rounds)) * (us[2] + us[3] * r))));
   }
   return best;
 }
@@ -685,17 +697,19 @@ static MxPlan mx_plan(int rows, int n_out) {
 // chunks, 2.5 us for starting and the sums' way to memory and back at 4 TB/s.  (65 rows x 14336 inputs, 4096 columns:
 // 128 columns in 1 split 147 us, as chosen here 28.)
 static MxPlan mx_plan_splits(int rows, int n_out, int chunks, int most, int* splits) {
-  const int rt = mx_row_tiles(rows);
-  MxPlan best{MX_N256, rt, 1e30f};
+  const int rts = mx_row_tiles(rows);
+  MxPlan best{MX_N256, 0, 1e30f};
   for (int s = 1; s <= most; ++s) {
     const int per = (chunks + s - 1) / s;
     if ((chunks + per - 1) / per != s) continue;
-    for (int w = 1; w <= 3; ++w) {
-      const float round = w < 3 ? mx_round_us[MX_IN_PLANES][w][rt - 2] : mx_wide_us[MX_IN_PLANES];
-      const float rounds = ceilf(mx_groups(rows, n_out, w < 3 ? 16 * rt : 64, 32 << w) * s / 256.f);
-      const float us = 2.5f + rounds * (round - 2.5f) * per / 32.f + (s > 1 ? s : 0) * (float)rows * n_out * 8 / 4e6f;
-      if (us < best.rounds_us) { best = MxPlan{MX_N32 + w, rt, us}; *splits = s; }
-    }
+    for (int w = 1; w <= 3; ++w)
+      for (int rt = rts; rt >= (w < 3 ? 2 : rts); --rt) {
+        if (w < 3 && !mx_blocks_hold<MX_IN_PLANES>(rows, rt)) continue;
+        const float round = w < 3 ? mx_round_us[MX_IN_PLANES][w][rt - 2] : mx_wide_us[MX_IN_PLANES];
+        const float rounds = ceilf(mx_groups(rows, n_out, w < 3 ? 16 * rt : 64, 32 << w) * s / 256.f);
+        const float us = 2.5f + rounds * (round - 2.5f) * per / 32.f + (s > 1 ? s : 0) * (float)rows * n_out * 8 / 4e6f;
+        if (us < best.us) { best = MxPlan{MX_N32 + w, rt, us}; *splits = s; }
+      }
   }
   return best;
 }
@@ -720,7 +734,7 @@ static void mx_project_by(hipStream_t s, const MxArgs& g, const MxPlan& p) {
 }
 
 template <int IN, int OUT>
-static void mx_project(hipStream_t s, const MxArgs& g) { mx_project_by<IN, OUT>(s, g, mx_plan<IN, OUT>(g.rows, g.n_out)); }
+static void mx_project(hipStream_t s, const MxArgs& g) { mx_project_by<IN, OUT>(s, g, mx_plan<IN, OUT>(g.rows, g.n_out, g.chunks)); }
 
 // ---------------------------------------------------------------------------------
 // a model's projections
@@ -741,7 +755,7 @@ int launch_mx_model(ts_model* m, const f16_t* X, const void* W, float* out, size
   int splits = 1;
   const int most = (int)std::min<size_t>(16, out_elems / ((size_t)R * N));
   MxPlan p = mx_plan_splits(R, N, g.chunks, std::max(most, 1), &splits);
-  if (const MxPlan one = mx_plan<MX_IN_PLANES, MX_OUT_ROWS>(R, N); 2.5f + (one.rounds_us - 2.5f) * g.chunks / 32.f < p.rounds_us) { p = one; splits = 1; }
+  if (const MxPlan one = mx_plan<MX_IN_PLANES, MX_OUT_ROWS>(R, N, g.chunks); one.us < p.us) { p = one; splits = 1; }
   g.per = (g.chunks + splits - 1) / splits;
   g.y_part = (size_t)R * N;
   mx_project_by<MX_IN_PLANES, MX_OUT_ROWS>(m->stream, g, p);
