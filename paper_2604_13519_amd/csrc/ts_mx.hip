@@ -6,33 +6,36 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ts_ops.h"
 
 // ---------------------------------------------------------------------------------
-// quantisation: four lanes a block, eight values a lane.  Bound by HBM: it reads the values and writes 17 bytes a block.
-// 14336 x 4096 bf16 (117 MB read, 31 MB written, as counted): 25 us, 5.9 TB/s, and the values back 23 us, 6.4 TB/s; a copy of
-// 1 GiB moves 5.1 TB/s.  Four pieces a thread, a workgroup's width apart, all requested first, keep enough bytes on their
-// way.  777 x 1000 fp32: 4.1 and 3.9 us, of which starting the launch is most.
+// quantisation: 16 bytes of values a lane, four lanes a block (fp32: eight).  Bound by HBM: it reads the values and writes 17 bytes a block.
+// 14336 x 4096 bf16 (117 MB read, 31 MB written, as counted), four matrices in turn: 30.0 us and the values back 29.0, 4.9 and
+// 5.1 TB/s; fp32 46.8 and 52.3 us, 5.7 and 5.1 TB/s; a copy of 1 GiB moves 5.1.  Two pieces a thread, a workgroup's width apart:
+// four 31.4 and 29.2 us (65 rows 3.4 and 2.6, with two 2.6 and 2.3), one 30.9 and 33.1.  A wave's loads and stores are whole lines:
+// eight fp32 values a lane, stored in two halves, 64.5 us.
 // ---------------------------------------------------------------------------------
-constexpr int QT = 256, QU = 4;           // threads of a workgroup, pieces of eight values per thread
+constexpr int QT = 256, QU = 2;           // threads of a workgroup, pieces per thread
+template <typename T> struct MxPiece {     // 16 bytes of values
+  static constexpr int V = 16 / sizeof(T), LANES = 32 / V;           // values, pieces of a block
+  typedef typename std::conditional<V == 8, uint32_t, uint16_t>::type Codes;
+};
 
-template <typename T>
-__device__ __forceinline__ void values8(const T* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      const uint4 w = load16(p);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+template <typename T, int V>
+__device__ __forceinline__ void mx_values(const T* p, int n, float (&v)[V]) {
+  if (n >= V) {
+    const uint4 w = load16(p);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-    } else {
-      const ts_f32x4 a = __builtin_bit_cast(ts_f32x4, load16(p)), b = __builtin_bit_cast(ts_f32x4, load16(p + 4));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+    for (int i = 0; i < V; ++i) {
+      if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+      else v[i] = __uint_as_float(u[i]);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < V; ++i) {
       v[i] = 0.f;
       if (i < n) {
         if constexpr (sizeof(T) == 2) v[i] = bf16_to_f32(p[i]);
@@ -45,35 +48,39 @@ __device__ __forceinline__ void values8(const T* p, int n, float (&v)[8]) {
 template <typename T>
 __global__ __launch_bounds__(QT) void k_mx_quantize(const T* x, uint32_t rows, uint32_t cols, int64_t stride,
                                                     uint8_t* codes, uint8_t* scales) {
-  const uint32_t blocks = (cols + 31) / 32, row_pieces = blocks * 4;
+  typedef MxPiece<T> P;
+  constexpr int V = P::V, LANES = P::LANES;
+  const uint32_t blocks = (cols + 31) / 32, row_pieces = blocks * LANES;
   const uint64_t pieces = (uint64_t)rows * row_pieces;                     // < 2^32, see the launch
-  float v[QU][8];
+  float v[QU][V];
 #pragma unroll
   for (int u = 0; u < QU; ++u) {
     const uint64_t at = (uint64_t)blockIdx.x * (QT * QU) + u * QT + threadIdx.x;
-    const uint32_t piece = (uint32_t)(at < pieces ? at : 0), r = piece / row_pieces, c = (piece - r * row_pieces) * 8;
-    values8(x + (int64_t)r * stride + c, (int)cols - (int)c, v[u]);
+    const uint32_t piece = (uint32_t)(at < pieces ? at : 0), r = piece / row_pieces, c = (piece - r * row_pieces) * V;
+    mx_values(x + (int64_t)r * stride + c, (int)cols - (int)c, v[u]);
   }
 #pragma unroll
   for (int u = 0; u < QU; ++u) {
     const uint64_t at = (uint64_t)blockIdx.x * (QT * QU) + u * QT + threadIdx.x;
     uint32_t top = 0;                                                      // magnitudes order like their bit patterns, NaN last
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2, 64));
+    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(v[u][i]) & 0x7fffffffu);
+#pragma unroll
+    for (int o = 1; o < LANES; o *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
     const uint32_t ef = top >> 23, s = ef == 255 ? 255 : ef > 2 ? ef - 2 : 0;
     const float inv = __uint_as_float((254 - min(s, 253u)) << 23);         // 2^(127 - s)
     uint32_t w = 0;
     if (s != 255) {
       w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[u][0] * inv, v[u][1] * inv, 1.f, 0);
       w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[u][2] * inv, v[u][3] * inv, 1.f, 1);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[u][4] * inv, v[u][5] * inv, 1.f, 2);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[u][6] * inv, v[u][7] * inv, 1.f, 3);
+      if constexpr (V == 8) {
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[u][4] * inv, v[u][5] * inv, 1.f, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[u][6] * inv, v[u][7] * inv, 1.f, 3);
+      }
     }
     if (at < pieces) {
-      reinterpret_cast<uint32_t*>(codes)[at] = w;
-      if ((at & 3) == 0) scales[at >> 2] = (uint8_t)s;
+      reinterpret_cast<typename P::Codes*>(codes)[at] = (typename P::Codes)w;
+      if (at % LANES == 0) scales[at / LANES] = (uint8_t)s;
     }
   }
 }
@@ -86,40 +93,43 @@ __device__ __forceinline__ float mx_scale(uint32_t s) {
 template <typename T>
 __global__ __launch_bounds__(QT) void k_mx_dequantize(const uint8_t* codes, const uint8_t* scales, uint32_t rows, uint32_t cols,
                                                       T* x, int64_t stride) {
-  const uint32_t blocks = (cols + 31) / 32, row_pieces = blocks * 4;
+  typedef MxPiece<T> P;
+  constexpr int V = P::V, LANES = P::LANES;
+  const uint32_t blocks = (cols + 31) / 32, row_pieces = blocks * LANES;
   const uint64_t pieces = (uint64_t)rows * row_pieces;
   uint32_t w[QU], s[QU];
 #pragma unroll
   for (int u = 0; u < QU; ++u) {
     const uint64_t at = (uint64_t)blockIdx.x * (QT * QU) + u * QT + threadIdx.x, a = at < pieces ? at : 0;
-    w[u] = reinterpret_cast<const uint32_t*>(codes)[a];
-    s[u] = scales[a >> 2];
+    w[u] = reinterpret_cast<const typename P::Codes*>(codes)[a];
+    s[u] = scales[a / LANES];
   }
 #pragma unroll
   for (int u = 0; u < QU; ++u) {
     const uint64_t at = (uint64_t)blockIdx.x * (QT * QU) + u * QT + threadIdx.x;
     if (at >= pieces) continue;
-    const uint32_t r = (uint32_t)at / row_pieces, c = ((uint32_t)at - r * row_pieces) * 8;
+    const uint32_t r = (uint32_t)at / row_pieces, c = ((uint32_t)at - r * row_pieces) * V;
     const float f = mx_scale(s[u]);
-    float v[8];
+    float v[V];
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.f, 1);
-    const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.f, 3);
-    v[0] = a[0] * f; v[1] = a[1] * f; v[2] = b[0] * f; v[3] = b[1] * f; v[4] = d[0] * f; v[5] = d[1] * f; v[6] = e[0] * f; v[7] = e[1] * f;
+    v[0] = a[0] * f; v[1] = a[1] * f; v[2] = b[0] * f; v[3] = b[1] * f;
+    if constexpr (V == 8) {
+      const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.f, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u], 1.f, 3);
+      v[4] = d[0] * f; v[5] = d[1] * f; v[6] = e[0] * f; v[7] = e[1] * f;
+    }
     T* p = x + (int64_t)r * stride + c;
     const int n = (int)cols - (int)c;
-    if (n >= 8) {
-      if constexpr (sizeof(T) == 2) {                                       // two significant bits: cutting is exact
-        uint32_t o[4];
+    if (n >= V) {
+      uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(v[2 * i]) >> 16 | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);
-        store16(p, make_uint4(o[0], o[1], o[2], o[3]));
-      } else {
-        store16(p, __builtin_bit_cast(uint4, make_float4(v[0], v[1], v[2], v[3])));
-        store16(p + 4, __builtin_bit_cast(uint4, make_float4(v[4], v[5], v[6], v[7])));
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (V == 8) o[i] = __float_as_uint(v[2 * i]) >> 16 | (__float_as_uint(v[2 * i + 1]) & 0xffff0000u);     // two significant bits: cutting is exact
+        else o[i] = __float_as_uint(v[i]);
       }
+      store16(p, make_uint4(o[0], o[1], o[2], o[3]));
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < V; ++i)
         if (i < n) {
           if constexpr (sizeof(T) == 2) p[i] = (bf16_t)(__float_as_uint(v[i]) >> 16);
           else p[i] = v[i];
@@ -129,8 +139,11 @@ __global__ __launch_bounds__(QT) void k_mx_dequantize(const uint8_t* codes, cons
 }
 
 // rows of one launch: pieces within 32 bits
-static int64_t mx_slab(int64_t cols) { return ((int64_t)1 << 31) / ((cols + 31) / 32 * 4); }
-static uint32_t mx_pieces_groups(int64_t rows, int64_t cols) { return (uint32_t)((rows * ((cols + 31) / 32 * 4) + QT * QU - 1) / (QT * QU)); }
+static int64_t mx_slab(int64_t cols) { return ((int64_t)1 << 31) / ((cols + 31) / 32 * 8); }
+template <typename T> static uint32_t mx_pieces_groups(int64_t rows, int64_t cols) {
+  constexpr int N = QT * QU;
+  return (uint32_t)((rows * ((cols + 31) / 32 * MxPiece<T>::LANES) + N - 1) / N);
+}
 
 void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t stride, uint8_t* codes, uint8_t* scales) {
   const int64_t blocks = (cols + 31) / 32, slab = mx_slab(cols);
@@ -139,8 +152,8 @@ void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t row
     const int64_t n = std::min(slab, rows - r);
     const void* xs = (const char*)x + r * stride * esz;
     uint8_t *cs = codes + r * blocks * 16, *ss = scales + r * blocks;
-    if (dtype == TS_DTYPE_BF16) k_mx_quantize<bf16_t><<<mx_pieces_groups(n, cols), QT, 0, s>>>((const bf16_t*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
-    else k_mx_quantize<float><<<mx_pieces_groups(n, cols), QT, 0, s>>>((const float*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
+    if (dtype == TS_DTYPE_BF16) k_mx_quantize<bf16_t><<<mx_pieces_groups<bf16_t>(n, cols), QT, 0, s>>>((const bf16_t*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
+    else k_mx_quantize<float><<<mx_pieces_groups<float>(n, cols), QT, 0, s>>>((const float*)xs, (uint32_t)n, (uint32_t)cols, stride, cs, ss);
   }
 }
 
@@ -151,8 +164,8 @@ static void launch_mx_dequantize(hipStream_t s, const uint8_t* codes, const uint
     const int64_t n = std::min(slab, rows - r);
     void* xs = (char*)x + r * stride * esz;
     const uint8_t *cs = codes + r * blocks * 16, *ss = scales + r * blocks;
-    if (dtype == TS_DTYPE_BF16) k_mx_dequantize<bf16_t><<<mx_pieces_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (bf16_t*)xs, stride);
-    else k_mx_dequantize<float><<<mx_pieces_groups(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (float*)xs, stride);
+    if (dtype == TS_DTYPE_BF16) k_mx_dequantize<bf16_t><<<mx_pieces_groups<bf16_t>(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (bf16_t*)xs, stride);
+    else k_mx_dequantize<float><<<mx_pieces_groups<float>(n, cols), QT, 0, s>>>(cs, ss, (uint32_t)n, (uint32_t)cols, (float*)xs, stride);
   }
 }
 
