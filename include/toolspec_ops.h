@@ -114,8 +114,8 @@ ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream stream);
  * page outside [0, n_pages), beyond the table or not below max_len is not seen; contents of
  * positions that are not seen have no influence, whatever they are.  Where nothing is seen, or
  * every score is -infinity, out is 0 and lse -infinity.
- * Scores, sums and outputs are fp32 (probabilities enter the product with the values as two bf16
- * terms, three for fp32 queries); out is rounded once, to q's dtype.
+ * Scores, probabilities, sums and outputs are fp32 (over a bf16 cache fp32 queries and the
+ * probabilities enter the products as three bf16 terms, 24 bits); out is rounded once, to q's dtype.
  *   max_len  : no length is above it (sizes the launch: the bound of the step, not the capacity)
  *   q, out   : [n_seqs] rows of n_q_heads * head_dim, in `dtype`
  *   lse      : natural logarithm of the sum of exp(scores), [n_seqs][n_q_heads] fp32; may be null

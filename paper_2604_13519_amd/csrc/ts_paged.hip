@@ -263,7 +263,7 @@ template <typename T, typename TQ, int HD>
 __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
   constexpr bool BF = sizeof(T) == 2;
   constexpr int QP = BF && sizeof(TQ) == 4 ? 3 : 1;          // terms of a query
-  constexpr int PP = sizeof(TQ) == 4 ? 3 : 2;                // terms of a probability (bf16 caches)
+  constexpr int PP = 3;                                      // terms of a probability (bf16 caches): all of its 24 bits
   constexpr int KC = BF ? HD / 32 : (HD + 15) / 16;          // 16-byte pieces of a key per lane
   constexpr int DT = (HD + 15) / 16;                         // tiles of 16 dimensions
   constexpr int OS = DT * 16 + 4;                            // floats of a head's row in the LDS

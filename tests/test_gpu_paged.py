@@ -206,6 +206,32 @@ def test_attend_scores_far_apart_in_any_order():
             assert bool(((out.double().cpu().view(2, 64) - want).abs() <= tol).all())
 
 
+@pytest.mark.parametrize("dtype,qdtype", TYPES)
+def test_attend_probabilities_have_24_bits(dtype, qdtype):
+    """Two keys with values v and -1: out = (v - p) / (1 + p), which shows p's last bits where v is near p.  Scores have one
+    term, |score| < 1, so p is off by the roundings of scale log2(e), of the score and of the exponential (below 2^-22.4) and
+    the two sums and the quotient by 5 half steps: 2^-21 in all, then half a step of the output."""
+    hd, hq = 128, 1024
+    scale = 2.0 ** -10
+    q = torch.zeros((hq, hd))
+    q[:, 0] = torch.arange(hq) % 128 + 128                     # bf16 holds 128 .. 255
+    q[:, 0] *= 2.0 ** (torch.arange(hq) // 256)                # scores -1/8 .. -1 over all heads
+    k = torch.zeros((1, 1, 16, hd), dtype=dtype)
+    k[0, 0, 1, 0] = -0.5
+    v = torch.full((1, 1, hd, 16), math.nan, dtype=dtype)
+    v[0, 0, :, 0] = 0.5 + torch.arange(hd) / 256.0             # bf16 holds them: 0.5 .. 1 in steps of 2^-8
+    v[0, 0, :, 1] = -1.0
+    for shift in (1.0, 0.93, 0.871):
+        s = scale * shift
+        out, _ = ops.ts_kv_attend(k.cuda(), v.cuda(), ints([[0]]), ints([2]), q.to(qdtype).view(1, -1).cuda(), 2, scale=s)
+        s32 = float(torch.tensor(s, dtype=torch.float32))      # what the call takes
+        p = torch.exp(-0.5 * s32 * q[:, :1].double())
+        want = (v[0, 0, :, 0].double()[None] - p) / (1 + p)
+        err = (out.double().cpu().view(hq, hd) - want).abs()
+        tol = 2.0 ** -21 + torch.finfo(qdtype).eps / 2 * want.abs()
+        assert bool((err <= tol).all()), "%.3g of the tolerance" % float((err / tol).max())
+
+
 def test_attend_strided_rows_and_padding():
     lengths = [40, 700, 3]
     k, v, table, K, V = make_cache(lengths, 2, 64, torch.bfloat16, 8)
