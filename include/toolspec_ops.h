@@ -55,8 +55,9 @@ ts_status ts_mx_packed_bytes(int32_t n_out, int32_t n_in, uint64_t* bytes);
 ts_status ts_mx_pack(const uint8_t* codes, const uint8_t* scales, int32_t n_out, int32_t n_in, void* packed, ts_stream stream);
 
 /* y[r][n] = sum_k x[r][k] W[n][k]: x [rows][n_in] and y [rows][n_out] of the same dtype.  The
- * products are exact (a weight has two significant bits; fp32 rows enter as three bf16 terms
- * that add up to them), the sums are fp32, y is rounded once.  The order of the sums depends on
+ * products are exact (a weight has two significant bits; fp32 rows enter as three bf16 terms of
+ * one sign that add up to them, up to the largest finite number; bits below 2^-133 are lost, so
+ * magnitudes below 2^-110 have fewer than 24), the sums are fp32, y is rounded once.  The order of the sums depends on
  * the sizes only, never on the contents, the device's load or the other rows.
  * A row's result does not depend on the other rows' values.
  * Errors: INVALID_ARG as above (rows in [0, 2^19], strides at least the row,
@@ -115,7 +116,8 @@ ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream stream);
  * positions that are not seen have no influence, whatever they are.  Where nothing is seen, or
  * every score is -infinity, out is 0 and lse -infinity.
  * Scores, probabilities, sums and outputs are fp32 (over a bf16 cache fp32 queries and the
- * probabilities enter the products as three bf16 terms, 24 bits); out is rounded once, to q's dtype.
+ * probabilities enter the products as three bf16 terms, 24 bits, those below 2^-133 lost); out is
+ * rounded once, to q's dtype.
  *   max_len  : no length is above it (sizes the launch: the bound of the step, not the capacity)
  *   q, out   : [n_seqs] rows of n_q_heads * head_dim, in `dtype`
  *   lse      : natural logarithm of the sum of exp(scores), [n_seqs][n_q_heads] fp32; may be null

@@ -45,24 +45,25 @@ __device__ __forceinline__ void store8(void* p, uint2 v) { *reinterpret_cast<ts_
 // Barrier that waits for the LDS alone: global loads stay in flight across it.
 __device__ __forceinline__ void wait_lds() { wait_loads<63>(); }
 
-// fp32 as a sum of bf16 terms: each is the rest so far rounded to nearest, so two carry 16 significant bits at least and
-// three all 24 (a rest below bf16's smallest subnormal, 2^-133, is lost); infinities and NaN stay in the first term.
 // One conversion instruction of gfx950 per pair of values.
 __device__ __forceinline__ ts_bf16x2 to_bf16x2(float a, float b) {
   const ts_f32x2 v = {a, b};
   return __builtin_convertvector(v, ts_bf16x2);
 }
+// fp32 as a sum of bf16 terms of one sign: each is the rest so far cut to bf16, the last rounded to nearest, so three carry all
+// 24 significant bits (a rest below bf16's smallest subnormal, 2^-133, is lost).  Cut, not rounded: the first term of a number next
+// to the largest would round to infinity, and a product that overflows in the first term would meet another of the opposite sign.
+// Infinities stay in the first term, NaN in the last.
 template <int N>
 __device__ __forceinline__ void split_bf16x2(float a, float b, ts_bf16x2 (&t)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    t[i] = to_bf16x2(a, b);
-    if (i + 1 < N) {
-      const uint32_t w = __builtin_bit_cast(uint32_t, t[i]);
-      const float ra = a - __uint_as_float(w << 16), rb = b - __uint_as_float(w & 0xffff0000u);
-      a = i == 0 && !(fabsf(a) < 0x1.ffp127f) ? 0.f : ra;          // from here on the first term is infinite
-      b = i == 0 && !(fabsf(b) < 0x1.ffp127f) ? 0.f : rb;
-    }
+    if (i + 1 == N) { t[i] = to_bf16x2(a, b); break; }
+    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+    t[i] = __builtin_bit_cast(ts_bf16x2, __builtin_amdgcn_perm(ub, ua, 0x07060302u));        // the high halves of both
+    const float ra = a - __uint_as_float(ua & 0xffff0000u), rb = b - __uint_as_float(ub & 0xffff0000u);
+    a = i == 0 && fabsf(a) == INFINITY ? 0.f : ra;
+    b = i == 0 && fabsf(b) == INFINITY ? 0.f : rb;
   }
 }
 

@@ -183,6 +183,26 @@ def test_project_infinities_stay_in_their_rows_and_columns():
     assert bool(y[:, 3].isnan().all()) and int(y.isnan().sum()) == 9
 
 
+@pytest.mark.parametrize("rows", [1, 5, 33, 100, 600])
+def test_project_finite_rows_give_finite_sums(rows):
+    """fp32 rows with one value each, of 24 bits and of any size up to the largest, over weights of any code: what does not
+    overflow is finite, and a code of zero gives zero.  An output is the sum of three exact products of one sign: two additions."""
+    n_out, n_in = 96, 300
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    codes = torch.randint(0, 256, (n_out, 160), dtype=torch.uint8, device="cuda", generator=gen)
+    scales = torch.randint(40, 124, (n_out, 10), dtype=torch.uint8, device="cuda", generator=gen)
+    w = ops.ts_mx_dequantize(codes, scales, n_in).double()
+    top = torch.finfo(torch.float32).max
+    for value in (top, -top, 3.397e38, 1.9999999 * 2.0 ** 100, -1.5 * 2.0 ** 127, 1.0000001):
+        x = torch.zeros((rows, n_in), device="cuda")
+        at = torch.randint(0, n_in, (rows,), device="cuda", generator=gen)
+        x[torch.arange(rows, device="cuda"), at] = value
+        y = ops.ts_mx_project(ops.ts_mx_pack(codes, scales, n_in), n_out, x).double()
+        want = float(torch.tensor(value, dtype=torch.float32)) * w[:, at].t()
+        assert bool(torch.isfinite(y).all()), (rows, value)
+        assert bool(((y - want).abs() <= 2.0 ** -22 * want.abs()).all()), (rows, value)
+
+
 def test_project_extreme_scales():
     """fp32 sums of the smallest and the largest weights; scales down to 2^-127."""
     for e in (0, 1, 40, 200, 230):

@@ -232,6 +232,23 @@ def test_attend_probabilities_have_24_bits(dtype, qdtype):
         assert bool((err <= tol).all()), "%.3g of the tolerance" % float((err / tol).max())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attend_largest_finite_queries(dtype):
+    """fp32 queries up to the largest number: their scores are finite where the keys are small.  A score has one term."""
+    hd = 64
+    top = torch.finfo(torch.float32).max
+    k, v, table, K, V = make_cache([40], 1, hd, dtype, 21)
+    k = torch.where(k.isnan(), k, k * 2.0 ** -126).to(dtype)
+    K = [K[0] * 2.0 ** -126]
+    q = torch.zeros((4, hd))
+    q[0, 3], q[1, 9], q[2, 0], q[3, 63] = top, -top, 3.397e38, -1.5 * 2.0 ** 127
+    out, lse = ops.ts_kv_attend(k, v, table, ints([40]), q.view(1, -1).cuda(), 40, scale=0.25)
+    want, want_lse, rough, d, _ = plain_attend(q.view(-1), K[0], V[0], 1, hd, 0, 0.25)
+    tol = (2 * d[:, None] + 2.0 ** -20 + 2 * 104 * 2.0 ** -24) * rough + 2.0 ** -24 * want.abs()
+    assert bool(((out.double().cpu().view(4, hd) - want).abs() <= tol).all())
+    assert bool(((lse.double().cpu()[0] - want_lse).abs() <= d + 2.0 ** -20 + 104 * 2.0 ** -24 + 2.0 ** -23 * want_lse.abs()).all())
+
+
 def test_attend_strided_rows_and_padding():
     lengths = [40, 700, 3]
     k, v, table, K, V = make_cache(lengths, 2, 64, torch.bfloat16, 8)
