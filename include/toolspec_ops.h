@@ -114,7 +114,8 @@ ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream stream);
  * `window` of them; query head h reads KV head h / (n_q_heads / n_kv_heads).  A position on a
  * page outside [0, n_pages), beyond the table or not below max_len is not seen; contents of
  * positions that are not seen have no influence, whatever they are.  Where nothing is seen, or
- * every score is -infinity, out is 0 and lse -infinity.
+ * every score is -infinity, out is 0 and lse -infinity; a score of +infinity or NaN makes its
+ * head NaN, an infinite value its dimension infinite.
  * Scores, probabilities, sums and outputs are fp32 (over a bf16 cache fp32 queries and the
  * probabilities enter the products as three bf16 terms, 24 bits, those below 2^-133 lost); out is
  * rounded once, to q's dtype.

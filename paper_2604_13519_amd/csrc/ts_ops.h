@@ -67,6 +67,19 @@ __device__ __forceinline__ void split_bf16x2(float a, float b, ts_bf16x2 (&t)[N]
   }
 }
 
+// Terms that meet infinities: 0 times infinity is NaN, so where the first term is not zero no other is either, the least that
+// bf16 holds (2^-133, as much as a term's rest may lose) in its place, of the same sign.
+typedef uint16_t ts_u16x2 __attribute__((ext_vector_type(2)));
+template <int N>
+__device__ __forceinline__ void split_bf16x2_nonzero(float a, float b, ts_bf16x2 (&t)[N]) {
+  split_bf16x2<N>(a, b, t);
+  const ts_u16x2 first = __builtin_bit_cast(ts_u16x2, t[0]), sign = first & (uint16_t)0x8000;
+  const ts_u16x2 least = __builtin_elementwise_min((ts_u16x2)(first & (uint16_t)0x7fff), (ts_u16x2)(uint16_t)1) | sign;
+#pragma unroll
+  for (int i = 1; i < N; ++i)                                    // magnitudes order like their bit patterns, and all have one sign
+    t[i] = __builtin_bit_cast(ts_bf16x2, __builtin_elementwise_max(__builtin_bit_cast(ts_u16x2, t[i]) | sign, least));
+}
+
 // the weights of a model with 4-bit projections (ts_mx.hip), used by the passes of toolspec.h
 size_t mx_packed_bytes(int64_t n_out, int64_t n_in);
 void launch_mx_quantize(hipStream_t s, const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, uint8_t* codes, uint8_t* scales);

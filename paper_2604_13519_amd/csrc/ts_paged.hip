@@ -306,7 +306,7 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           ts_bf16x2 t[QP];
-          split_bf16x2<QP>(x[2 * e], x[2 * e + 1], t);
+          split_bf16x2_nonzero<QP>(x[2 * e], x[2 * e + 1], t);
 #pragma unroll
           for (int p = 0; p < QP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, t[p]);
         }
@@ -437,7 +437,7 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         ts_bf16x2 t[PP];
-        split_bf16x2<PP>(x[2 * e], x[2 * e + 1], t);
+        split_bf16x2_nonzero<PP>(x[2 * e], x[2 * e + 1], t);
 #pragma unroll
         for (int p = 0; p < PP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, t[p]);
       }

@@ -188,6 +188,34 @@ def test_attend_special_values_that_are_seen():
         assert bool((out[:, 7] == math.inf).all()) and torch.equal(out[:, :7], clean.view(2, 64)[:, :7]) and torch.equal(out[:, 8:], clean.view(2, 64)[:, 8:])
 
 
+@pytest.mark.parametrize("dtype,qdtype", TYPES)
+@pytest.mark.parametrize("n", [3, 40, 300])
+def test_attend_infinite_keys_and_values(dtype, qdtype, n):
+    """A key of -infinity counts for nothing and an infinite value makes its dimension infinite, whatever the query's and the
+    probability's last bits are; the other keys and dimensions are as without them."""
+    hd, hq = 64, 24
+    for q_of in (lambda g: torch.ones((1, hq * hd)), lambda g: torch.randn((1, hq * hd), generator=g).abs() + 0.01):
+        q = q_of(torch.Generator().manual_seed(n)).to(qdtype).cuda()
+        k, v, table, K, V = make_cache([n], 1, hd, dtype, 31 + n)
+        clean, clean_lse = ops.ts_kv_attend(k, v, table, ints([n]), q, n)
+        for at in sorted({0, 1, n // 2, n - 1}):
+            page, slot = int(table[0, at // 16]), at % 16
+            k2 = k.clone()
+            k2[page, 0, slot, 5] = -math.inf
+            out, lse = ops.ts_kv_attend(k2, v, table, ints([n]), q, n)
+            keep = [p for p in range(n) if p != at]
+            want, want_lse, rough, d, _ = plain_attend(q.cpu()[0], K[0][keep], V[0][keep], 1, hd, 0, 0.125)
+            tol = (2 * d[:, None] + 2.0 ** -20 + 2 * (n + 64) * 2.0 ** -24) * rough + torch.finfo(qdtype).eps / 2 * want.abs()
+            assert bool(((out.double().cpu().view(hq, hd) - want).abs() <= tol).all()), ("key", at)
+            assert bool(((lse.double().cpu()[0] - want_lse).abs() <= d + 2.0 ** -20 + (n + 64) * 2.0 ** -24 + 2.0 ** -23 * want_lse.abs()).all())
+            v2 = v.clone()
+            v2[page, 0, 7, slot], v2[page, 0, 33, slot] = math.inf, -math.inf
+            out, lse = ops.ts_kv_attend(k, v2, table, ints([n]), q, n)
+            out, other = out.view(hq, hd), [i for i in range(hd) if i not in (7, 33)]
+            assert bool((out[:, 7] == math.inf).all()) and bool((out[:, 33] == -math.inf).all()), ("value", at)
+            assert torch.equal(out[:, other], clean.view(hq, hd)[:, other]) and torch.equal(lse, clean_lse)
+
+
 def test_attend_scores_far_apart_in_any_order():
     """The running maximum rises at every block, falls at every block, and stays."""
     for dtype in (torch.bfloat16, torch.float32):
