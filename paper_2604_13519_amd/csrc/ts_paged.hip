@@ -252,10 +252,10 @@ struct AttendArgs {
 // positions seen by a sequence's token: [lo, hi), and where its chunks start (a block boundary)
 __device__ __forceinline__ void seen_range(const ts_kv_attend_args& a, int seq, int& lo, int& hi, int& base) {
   const int64_t room = (int64_t)a.table_width * 16;
-  hi = max(0, min(a.lengths[seq], a.max_len));
-  const int len = hi;
+  const int len = max(0, a.lengths[seq]);                    // the window is the last of these, seen or not
+  hi = min(len, a.max_len);
   if (hi > room) hi = (int)room;
-  lo = a.window > 0 && len > a.window ? len - a.window : 0;
+  lo = a.window > 0 && len > a.window ? min(len - a.window, hi) : 0;
   base = lo & ~(ATT_KB - 1);
 }
 
@@ -284,8 +284,9 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
   const int split = id % g.splits, seq = id / g.splits;
   int lo, hi, base;
   seen_range(a, seq, lo, hi, base);
-  const int k0 = base + split * g.chunk, k1 = min(hi, k0 + g.chunk);
-  if (split > 0 && k0 >= hi) return;                         // the join knows which splits there are
+  const int64_t from = base + (int64_t)split * g.chunk;      // base and the launch's span may both be near 2^30
+  if (split > 0 && from >= hi) return;                       // the join knows which splits there are
+  const int k0 = (int)from, k1 = (int)min((int64_t)hi, from + g.chunk);
   const int heads = min(16, g.group - tile * 16), head0 = kvh * g.group + tile * 16;
 
   // the queries: lane (head n, group lg) holds the dimensions it multiplies with its keys' pieces

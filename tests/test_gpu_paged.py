@@ -160,6 +160,24 @@ def test_attend_bad_pages_and_unseen_places_have_no_influence():
         assert bool((out == 0).all()) and bool((lse == -math.inf).all())
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_attend_window_of_lengths_beyond_max_len(dtype):
+    """The window is the last positions of the length; of those, what lies at max_len and beyond is not seen."""
+    hq, hd = 4, 64
+    k, v, table, K, V = make_cache([1000], 2, hd, dtype, 17)
+    q = torch.randn((1, hq * hd), generator=torch.Generator().manual_seed(3)).to(dtype)
+    for n, top, window in ((200, 64, 150), (200, 200, 150), (1000, 700, 301), (1000, 700, 350), (999, 998, 3), (1 << 30, 800, (1 << 30) - 90)):
+        out, lse = ops.ts_kv_attend(k, v, table, ints([n]), q.cuda(), top, window=window)
+        lo = n - window
+        want, want_lse, rough, d, _ = plain_attend(q[0], K[0][lo:top], V[0][lo:top], 2, hd, 0, 0.125)
+        tol = (2 * d[:, None] + 2.0 ** -20 + 2 * (top + 64) * 2.0 ** -24) * rough + torch.finfo(dtype).eps / 2 * want.abs()
+        assert bool(((out.double().cpu().view(hq, hd) - want).abs() <= tol).all()), (n, top, window)
+        assert bool(((lse.double().cpu()[0] - want_lse).abs() <= d + 2.0 ** -20 + (top + 64) * 2.0 ** -24 + 2.0 ** -23 * want_lse.abs()).all())
+    for n, top, window in ((200, 64, 100), (200, 64, 136), ((1 << 31) - 1, 1000, 1000), ((1 << 31) - 1, 0, 5)):
+        out, lse = ops.ts_kv_attend(k, v, table, ints([n]), q.cuda(), top, window=window)
+        assert bool((out == 0).all()) and bool((lse == -math.inf).all()), (n, top, window)
+
+
 def test_attend_special_values_that_are_seen():
     for dtype in (torch.bfloat16, torch.float32):
         k, v, table, K, V = make_cache([300], 1, 64, dtype, 4)
