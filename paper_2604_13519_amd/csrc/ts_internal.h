@@ -207,6 +207,22 @@ void gemm_rows_plan(const ts_model* m, int R, int N, int K, int mode, size_t max
 int gemm_rows_chunk(int cfg);
 void launch_gemm_rows_bf16(ts_model* m, const f16_t* X, const f16_t* Wt, float* out, int R, int N, int K, int mt, int cfg,
                            int splits, int mode, f16_t* act_out, float* logits);
+// products with 4-bit weights (ts_mx.hip): what enters, what comes out, the arguments of a launch, and which of the compiled shapes it takes
+enum { MX_IN_BF16 = 0, MX_IN_F32 = 1, MX_IN_PLANES = 2 };   // rows: bf16; fp32 as three bf16 terms; a model's hi and lo halves
+enum { MX_OUT_ROWS = 0, MX_OUT_SWIGLU = 1 };
+enum { MX_DIRECT, MX_DIRECT2, MX_N32, MX_N64, MX_N128, MX_N256 };
+struct MxArgs {
+  const uint8_t* w;
+  const void* x; int64_t x_stride; size_t x_plane;        // elements between the hi and the lo plane
+  void* y; int64_t y_stride; size_t y_plane; int32_t y_f32;
+  unsigned long long* sat;
+  int rows, n_out, n_in, chunks;
+  int per; size_t y_part;                                 // chunks of a split of K, elements between the splits' sums
+};
+struct MxPlan { int shape, rt; float us; };                // rt: row tiles of 16 (N32, N64, N128)
+MxPlan mx_plan(int in, int out, int rows, int n_out, int chunks);
+MxPlan mx_plan_model(int rows, int n_out, int chunks, size_t out_elems, int* splits);
+void launch_mx_by(hipStream_t s, int in, int out, const MxArgs& g, const MxPlan& p);
 // projections of 4-bit models (ts_mx.hip): X in hi and lo halves; out: fp32 partial sums [split][R][N], as many splits as are
 // returned and fit out_elems / the SwiGLU product in hi and lo halves
 int launch_mx_model(ts_model* m, const f16_t* X, const void* W, float* out, size_t out_elems, int R, int N, int K);

@@ -223,18 +223,6 @@ void launch_mx_pack(hipStream_t s, const uint8_t* codes, const uint8_t* scales, 
 // scale by one conversion instruction.  Two significant bits and eight of exponent fit bf16, so nothing is rounded.
 // (Models' rows are halves: see the range of the scales at their loading.)
 // ---------------------------------------------------------------------------------
-enum { MX_IN_BF16 = 0, MX_IN_F32 = 1, MX_IN_PLANES = 2 };   // rows: bf16; fp32 as three bf16 terms; a model's hi and lo halves
-enum { MX_OUT_ROWS = 0, MX_OUT_SWIGLU = 1 };
-
-struct MxArgs {
-  const uint8_t* w;
-  const void* x; int64_t x_stride; size_t x_plane;        // elements between the hi and the lo plane
-  void* y; int64_t y_stride; size_t y_plane; int32_t y_f32;
-  unsigned long long* sat;
-  int rows, n_out, n_in, chunks;
-  int per; size_t y_part;                                 // chunks of a split of K, elements between the splits' sums
-};
-
 template <int IN> struct MxIn { static constexpr int planes = IN == MX_IN_BF16 ? 1 : IN == MX_IN_F32 ? 3 : 2; };
 
 template <int IN>
@@ -667,8 +655,6 @@ static void mx_launch(hipStream_t s, const MxArgs& g) {
 // 16 rows: 4096 columns 7.0, 7.3, 6.9 us, 28672 columns 36.3, 22.7, 13.1 us.
 // 65 rows x 4096 inputs, 28672 columns: 128 columns wide 22.3 us, 64 wide 29.8, 32 wide 47.4, 256 wide 31.6; 4096
 // columns: 32 wide 13.0, 64 wide 14.7, 128 wide 20.9.
-enum { MX_DIRECT, MX_DIRECT2, MX_N32, MX_N64, MX_N128, MX_N256 };
-struct MxPlan { int shape, rt; float us; };
 static constexpr float mx_round_us[3][3][4] = {{{6.8f, 8.7f, 12.1f, 13.0f}, {7.9f, 10.0f, 12.8f, 14.7f}, {11.5f, 14.8f, 17.3f, 20.8f}},
                                                {{0, 0, 0, 0}, {24.8f, 35.3f, 45.8f, 52.f}, {35.f, 47.f, 61.6f, 73.f}},
                                                {{0, 0, 0, 0}, {12.8f, 16.9f, 21.9f, 26.8f}, {23.1f, 29.5f, 37.f, 44.2f}}};
@@ -683,7 +669,7 @@ template <int IN> static bool mx_blocks_hold(int rows, int rt) {
 }
 
 template <int IN, int OUT>
-static MxPlan mx_plan(int rows, int n_out, int chunks) {
+static MxPlan mx_plan_of(int rows, int n_out, int chunks) {
   // one round: [0] + [1] r, of several each: [2] + [3] r
   static constexpr float direct_us[3][2][4] = {{{3.6f, 0.22f, 2.4f, 0.21f}, {4.0f, 0.2f, 2.8f, 0.2f}},
                                                {{7.2f, 0.29f, 4.6f, 0.31f}, {7.6f, 0.25f, 5.6f, 0.28f}},
@@ -746,8 +732,25 @@ static void mx_project_by(hipStream_t s, const MxArgs& g, const MxPlan& p) {
   else mx_project_tiles<IN, OUT, 5>(s, g, p.shape);
 }
 
-template <int IN, int OUT>
-static void mx_project(hipStream_t s, const MxArgs& g) { mx_project_by<IN, OUT>(s, g, mx_plan<IN, OUT>(g.rows, g.n_out, g.chunks)); }
+MxPlan mx_plan(int in, int out, int rows, int n_out, int chunks) {
+  if (in == MX_IN_BF16) return mx_plan_of<MX_IN_BF16, MX_OUT_ROWS>(rows, n_out, chunks);
+  if (in == MX_IN_F32) return mx_plan_of<MX_IN_F32, MX_OUT_ROWS>(rows, n_out, chunks);
+  if (out == MX_OUT_ROWS) return mx_plan_of<MX_IN_PLANES, MX_OUT_ROWS>(rows, n_out, chunks);
+  return mx_plan_of<MX_IN_PLANES, MX_OUT_SWIGLU>(rows, n_out, chunks);
+}
+MxPlan mx_plan_model(int rows, int n_out, int chunks, size_t out_elems, int* splits) {
+  const int most = (int)std::min<size_t>(16, out_elems / ((size_t)rows * n_out));
+  *splits = 1;
+  MxPlan p = mx_plan_splits(rows, n_out, chunks, std::max(most, 1), splits);
+  if (const MxPlan one = mx_plan(MX_IN_PLANES, MX_OUT_ROWS, rows, n_out, chunks); one.us < p.us) { p = one; *splits = 1; }
+  return p;
+}
+void launch_mx_by(hipStream_t s, int in, int out, const MxArgs& g, const MxPlan& p) {
+  if (in == MX_IN_BF16) mx_project_by<MX_IN_BF16, MX_OUT_ROWS>(s, g, p);
+  else if (in == MX_IN_F32) mx_project_by<MX_IN_F32, MX_OUT_ROWS>(s, g, p);
+  else if (out == MX_OUT_ROWS) mx_project_by<MX_IN_PLANES, MX_OUT_ROWS>(s, g, p);
+  else mx_project_by<MX_IN_PLANES, MX_OUT_SWIGLU>(s, g, p);
+}
 
 // ---------------------------------------------------------------------------------
 // a model's projections
@@ -765,19 +768,17 @@ static MxArgs mx_model_args(const ts_model* m, const f16_t* X, const void* W, in
 int launch_mx_model(ts_model* m, const f16_t* X, const void* W, float* out, size_t out_elems, int R, int N, int K) {
   MxArgs g = mx_model_args(m, X, W, R, N, K);
   g.y = out; g.y_stride = N; g.y_f32 = 1;
-  int splits = 1;
-  const int most = (int)std::min<size_t>(16, out_elems / ((size_t)R * N));
-  MxPlan p = mx_plan_splits(R, N, g.chunks, std::max(most, 1), &splits);
-  if (const MxPlan one = mx_plan<MX_IN_PLANES, MX_OUT_ROWS>(R, N, g.chunks); one.us < p.us) { p = one; splits = 1; }
+  int splits;
+  const MxPlan p = mx_plan_model(R, N, g.chunks, out_elems, &splits);
   g.per = (g.chunks + splits - 1) / splits;
   g.y_part = (size_t)R * N;
-  mx_project_by<MX_IN_PLANES, MX_OUT_ROWS>(m->stream, g, p);
+  launch_mx_by(m->stream, MX_IN_PLANES, MX_OUT_ROWS, g, p);
   return splits;
 }
 void launch_mx_model_swiglu(ts_model* m, const f16_t* X, const void* W, f16_t* act_out, int R, int F, int K) {
   MxArgs g = mx_model_args(m, X, W, R, 2 * F, K);
   g.y = act_out; g.y_stride = act_ld(F); g.y_plane = (size_t)(m->ws_rows + TS_MROWS_PER_BLOCK) * act_ld(F);
-  mx_project<MX_IN_PLANES, MX_OUT_SWIGLU>(m->stream, g);
+  launch_mx_by(m->stream, MX_IN_PLANES, MX_OUT_SWIGLU, g, mx_plan(MX_IN_PLANES, MX_OUT_SWIGLU, R, 2 * F, g.chunks));
 }
 
 // ---------------------------------------------------------------------------------
@@ -869,8 +870,8 @@ extern "C" ts_status ts_mx_project(const void* packed, int32_t n_out, int32_t n_
   g.y = y; g.y_stride = y_stride; g.y_f32 = dtype == TS_DTYPE_F32;
   g.n_out = n_out; g.n_in = n_in; g.chunks = g.per = (int)mx_chunks(n_in);
   g.rows = (int)rows;
-  if (dtype == TS_DTYPE_BF16) mx_project<MX_IN_BF16, MX_OUT_ROWS>((hipStream_t)stream, g);
-  else mx_project<MX_IN_F32, MX_OUT_ROWS>((hipStream_t)stream, g);
+  const int in = dtype == TS_DTYPE_BF16 ? MX_IN_BF16 : MX_IN_F32;
+  launch_mx_by((hipStream_t)stream, in, MX_OUT_ROWS, g, mx_plan(in, MX_OUT_ROWS, g.rows, n_out, g.chunks));
   TS_HIP(hipGetLastError());
   return TS_OK;
 }

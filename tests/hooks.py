@@ -44,3 +44,28 @@ def units(n_keys, max_M, hq, hkv, n_cu=256):
     u, s = (C.c_int * (4 * room))(), (C.c_int * n)()
     count = lib().hook_units(n_cu, hq, hkv, n, (C.c_int * n)(*n_keys), max_M, u, s)
     return [tuple(u[4 * i:4 * i + 4]) for i in range(count)], list(s), room
+
+
+# ---- products with 4-bit weights -----------------------------------------------------------
+MX_BF16, MX_F32, MX_PLANES = 0, 1, 2          # what enters
+MX_ROWS, MX_SWIGLU = 0, 1                     # what comes out
+DIRECT, DIRECT2, N32, N64, N128, N256 = range(6)
+
+
+def mx_variants(kind, out):
+    """Every compiled (shape, row tiles) for rows of this kind."""
+    direct = [(DIRECT2, 0)] if out == MX_SWIGLU else [(DIRECT, 0), (DIRECT2, 0)]
+    widths = [N128] if out == MX_SWIGLU else [N32, N64, N128] if kind == MX_BF16 else [N64, N128]
+    return direct + [(w, rt) for w in widths for rt in (2, 3, 4, 5)] + [(N256, 0)]
+
+
+def mx_plan(kind, out, rows, n_out, n_in):
+    s, r = C.c_int(-1), C.c_int(-1)
+    lib().hook_mx_plan(kind, out, rows, n_out, n_in, C.byref(s), C.byref(r))
+    return s.value, r.value
+
+
+def mx_plan_model(rows, n_out, n_in, out_elems):
+    s, r, n = C.c_int(-1), C.c_int(-1), C.c_int(-1)
+    lib().hook_mx_plan_model(rows, n_out, n_in, C.c_long(out_elems), C.byref(s), C.byref(r), C.byref(n))
+    return s.value, r.value if s.value in (N32, N64, N128) else 0, n.value

@@ -33,6 +33,33 @@ int hook_project(const uint16_t* X, const uint16_t* Wt, float* out, uint16_t* ac
   return e != hipSuccess ? (int)e : (int)hipStreamSynchronize(nullptr);
 }
 
+// Plan of a product with 4-bit weights: shape and row tiles; for a model's projection into out_elems sums also the splits of K.
+void hook_mx_plan(int in, int out, int rows, int n_out, int n_in, int* shape, int* rt) {
+  const MxPlan p = mx_plan(in, out, rows, n_out, (n_in + 127) / 128);
+  *shape = p.shape; *rt = p.rt;
+}
+void hook_mx_plan_model(int rows, int n_out, int n_in, long out_elems, int* shape, int* rt, int* splits) {
+  const MxPlan p = mx_plan_model(rows, n_out, (n_in + 127) / 128, (size_t)out_elems, splits);
+  *shape = p.shape; *rt = p.rt;
+}
+
+// One product by the given plan (device pointers).  in: the rows' kind, planes x_plane elements apart; out: rows (y_f32: fp32, else
+// bf16; `splits` partial sums, rows * n_out apart) or SwiGLU planes, y_plane apart.
+int hook_mx_project(const void* w, const void* x, long x_stride, long x_plane, void* y, long y_stride, long y_plane, int y_f32,
+                    unsigned long long* sat, int in, int out, int rows, int n_out, int n_in, int shape, int rt, int splits) {
+  MxArgs g{};
+  g.w = (const uint8_t*)w;
+  g.x = x; g.x_stride = x_stride; g.x_plane = (size_t)x_plane;
+  g.y = y; g.y_stride = y_stride; g.y_plane = (size_t)y_plane; g.y_f32 = y_f32;
+  g.sat = sat;
+  g.rows = rows; g.n_out = n_out; g.n_in = n_in; g.chunks = (n_in + 127) / 128;
+  g.per = (g.chunks + splits - 1) / splits;
+  g.y_part = (size_t)rows * n_out;
+  launch_mx_by(nullptr, in, out, g, MxPlan{shape, rt, 0.f});
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? (int)e : (int)hipStreamSynchronize(nullptr);
+}
+
 int hook_max_units(int n_cu, int n_seqs) {
   ts_model m{};
   m.n_cu = n_cu;
