@@ -44,7 +44,9 @@ typedef void* ts_stream; /* hipStream_t */
  * bytes; host pointers, pointers of different GPUs), DEVICE.  rows or cols 0: nothing to do. */
 ts_status ts_mx_quantize(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride,
                          uint8_t* codes, uint8_t* scales, ts_stream stream);
-/* The values again, in fp32 or bf16 (both hold every one of them exactly). */
+/* The values again, in fp32 or bf16 (both hold every one of them exactly; with scale bytes 253 and 254,
+ * which ts_mx_quantize never writes, magnitudes from 2^128 on come back infinite, and their products
+ * are infinite or NaN). */
 ts_status ts_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols,
                            void* x, int32_t dtype, int64_t row_stride, ts_stream stream);
 

@@ -115,6 +115,23 @@ def test_dequantize_every_code_and_scale():
             assert same(ops.ts_mx_dequantize(codes, scales, 32, dt), want), (s, dt)
 
 
+def test_scales_whose_values_pass_fp32():
+    """Scale bytes that quantising never writes: values up to 2^128 - 1 step as they are, infinities beyond, in both types and in the product."""
+    codes = torch.zeros((16, 16), dtype=torch.uint8, device="cuda")
+    codes[:, 0] = torch.arange(16, dtype=torch.uint8, device="cuda")
+    for s in (252, 253, 254):
+        scales = torch.full((16, 1), s, dtype=torch.uint8, device="cuda")
+        want = GRID[torch.arange(16) % 8] * torch.where(torch.arange(16) >= 8, -1.0, 1.0).double() * 2.0 ** (s - 127)
+        want = torch.where(want.abs() >= 2.0 ** 128, torch.sign(want) * math.inf, want)
+        for dt in (torch.float32, torch.bfloat16):
+            assert same(ops.ts_mx_dequantize(codes, scales, 32, dt)[:, 0], want), (s, dt)
+            x = torch.zeros((3, 32), dtype=dt, device="cuda")
+            x[:, 0] = 0.125
+            y = ops.ts_mx_project(ops.ts_mx_pack(codes, scales, 32), 16, x).double().cpu()
+            finite = torch.isfinite(want)
+            assert bool((y[:, finite] == want[finite] / 8).all()) and not bool(torch.isfinite(y[:, ~finite]).any()), (s, dt)
+
+
 def weights(n_out, n_in, seed):
     g = torch.Generator(device="cuda").manual_seed(seed)
     w = torch.randn((n_out, n_in), generator=g, device="cuda") * torch.exp2(torch.randint(-6, 6, (n_out, 1), generator=g, device="cuda").float())
