@@ -2,7 +2,8 @@
 
 Function names mirror the header.  A call checks what the tensors themselves tell (types, shapes, devices, contiguity
 within a row), allocates outputs that it is not given, and enqueues on the current stream of the tensors' GPU; whatever
-is wrong raises before anything is enqueued.  The arithmetic is the library's: there is no fallback.
+is wrong raises before anything is enqueued.  The arithmetic is the library's: there is no fallback.  No call has a
+backward pass: while gradients are recorded, a tensor that requires one is refused.
 
 Import this module (or torch) before the library is loaded: it then runs on torch's HIP runtime, and not on one of its own.
 """
@@ -57,7 +58,7 @@ _lib = None
 def _load():
     global _lib
     lib = binding.load_library()
-    if _lib is not lib:
+    if _lib is None:
         with open("/proc/self/maps") as maps:
             runtimes = {line.split()[-1] for line in maps if "libamdhip64" in line}
         if len(runtimes) > 1:                              # torch's and the system's: neither knows the other's memory and streams
@@ -94,6 +95,11 @@ def _refuse(what, *args):
     raise ValueError(what % args)
 
 
+def _no_gradient(name):
+    if torch.is_grad_enabled():
+        _refuse("%s requires a gradient, and these calls have none: detach it, or call them under torch.no_grad()", name)
+
+
 def _rows(t, name, cols=None, dtype=None):
     """A matrix whose rows are contiguous; the distance between rows is free.  (address, distance)"""
     shape = t.shape
@@ -110,6 +116,8 @@ def _rows(t, name, cols=None, dtype=None):
     has = t.dtype
     if has is not dtype and (dtype is not None or has not in _DTYPES):
         raise TypeError("%s: %s is needed, got %s" % (name, dtype or "float32 or bfloat16", has))
+    if t.requires_grad:
+        _no_gradient(name)
     if not t.is_cuda:
         _refuse("%s is not on a GPU", name)
     return t.data_ptr(), dist
@@ -130,7 +138,7 @@ def _bytes(t, name, shape=None):
 # ---- 4-bit microscaled values ------------------------------------------------------------
 def ts_mx_quantize(x, codes=None, scales=None):
     """x [rows][cols] fp32 or bf16 -> (codes uint8 [rows][16 * blocks], scales uint8 [rows][blocks]), blocks = ceil(cols / 32)."""
-    lib = _load()
+    lib = _lib or _load()
     px, stride = _rows(x, "x")
     rows, cols = x.shape
     blocks = (cols + 31) // 32
@@ -145,7 +153,7 @@ def ts_mx_quantize(x, codes=None, scales=None):
 
 def ts_mx_dequantize(codes, scales, cols, dtype=torch.float32, out=None):
     """The values [rows][cols] that codes and scales stand for (exact in both types; infinite from 2^128 on)."""
-    lib = _load()
+    lib = _lib or _load()
     rows, blocks = codes.shape[0], (cols + 31) // 32
     pc, ps = _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks))
     if out is None:
@@ -165,7 +173,7 @@ def ts_mx_packed_bytes(n_out, n_in):
 
 def ts_mx_pack(codes, scales, n_in, out=None):
     """Weights [n_out][n_in], given as codes and scales, laid out for ts_mx_project: a uint8 tensor to keep."""
-    lib = _load()
+    lib = _lib or _load()
     n_out, blocks = codes.shape[0], (n_in + 31) // 32
     pc, ps = _bytes(codes, "codes", (n_out, 16 * blocks)), _bytes(scales, "scales", (n_out, blocks))
     n = ts_mx_packed_bytes(n_out, n_in)
@@ -177,7 +185,7 @@ def ts_mx_pack(codes, scales, n_in, out=None):
 
 def ts_mx_project(packed, n_out, x, out=None):
     """x [rows][n_in] times the packed weights' transpose: [rows][n_out] in x's type."""
-    lib = _load()
+    lib = _lib or _load()
     px, xs = _rows(x, "x")
     rows, n_in = x.shape
     pw = _bytes(packed, "packed")
@@ -230,6 +238,8 @@ def _pages(k_pages, v_pages):
     dtype = k_pages.dtype
     if dtype not in _DTYPES or v_pages.dtype != dtype:
         raise TypeError("pages: float32 or bfloat16 are needed, got %s and %s" % (dtype, v_pages.dtype))
+    if k_pages.requires_grad or v_pages.requires_grad:
+        _no_gradient("pages")
     return k_pages.data_ptr(), v_pages.data_ptr(), n, h, hd, _DTYPES[dtype]
 
 
@@ -243,7 +253,7 @@ def _table(t, n_seqs):
 def ts_kv_append(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_theta, q_out=None):
     """Rows of k and v ([rows][kv heads * head_dim]) into the cache at lengths[s], lengths[s] + 1, ... of their sequences, keys
     rotated; with q ([rows][heads * head_dim]) the rotated queries, which are returned.  See the header."""
-    lib = _load()
+    lib = _lib or _load()
     pages = _pages(k_pages, v_pages)
     n, kv_heads, hd = row_offsets.shape[0] - 1, pages[3], pages[4]
     table, t_stride, t_width = _table(table, n)
@@ -283,7 +293,7 @@ def ts_kv_attend_workspace(n_seqs, n_q_heads, n_kv_heads, head_dim, max_len, win
 def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=None, workspace=None, out=None, lse=None):
     """Attention of one token per sequence, q [n_seqs][heads * head_dim]: (out like q, lse fp32 [n_seqs][heads]).  scale None:
     1 / sqrt(head_dim).  workspace: of ts_kv_attend_workspace; without one the call allocates it.  See the header."""
-    lib = _load()
+    lib = _lib or _load()
     pages = _pages(k_pages, v_pages)
     kv_heads, hd = pages[3], pages[4]
     pq, q_stride = _rows(q, "q")

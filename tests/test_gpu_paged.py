@@ -479,6 +479,26 @@ def test_append_in_place_queries():
     assert torch.equal(y[:, :4 * hd], want) and torch.equal(y[:, 4 * hd:], x[:, 4 * hd:])
 
 
+def test_queries_rows_and_pages_that_require_gradients_are_refused():
+    k, v, table, _, _ = make_cache([20], 2, 64, torch.float32, 0, extra=4, fill=0.0)
+    q, kk = torch.randn((1, 256), device="cuda"), torch.randn((1, 128), device="cuda")
+    grad = lambda t: t.clone().requires_grad_()  # noqa: E731
+    k0 = k.clone()
+    for a, b, c, d in ((k, grad(q), kk, kk), (k, q, grad(kk), kk), (k, q, kk, grad(kk)), (grad(k), q, kk, kk)):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            ops.ts_kv_append(a, v, table, ints([20]), ints([0, 1]), b, c, d, 1e4)
+    for a, b in ((k, grad(q)), (grad(k), q)):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            ops.ts_kv_attend(a, v, table, ints([20]), b, 20)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        ops.ts_kv_attend(k, grad(v), table, ints([20]), q, 20)
+    assert torch.equal(k, k0)
+    with torch.no_grad():
+        out, lse = ops.ts_kv_attend(k, v, table, ints([20]), grad(q), 20)
+    want = ops.ts_kv_attend(k, v, table, ints([20]), q, 20)
+    assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 def test_captured_steps_replay_with_other_lengths():
     """Append, attend and the lengths' increment in one graph, replayed over a page border with eager work between."""
     hd, hq, hkv, n = 128, 8, 2, 3

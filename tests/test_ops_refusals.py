@@ -163,6 +163,24 @@ def test_tensors_are_looked_at(lib):
         ops.ts_kv_attend(torch.zeros((3, 2, 16, 64)), torch.zeros((3, 2, 64, 16)), torch.zeros((1, 3), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros((1, 128)), 40)
 
 
+def test_tensors_that_require_gradients_are_refused(lib):
+    """No call has a backward pass: a result without one in a graph that records them would lose the gradient silently."""
+    x = torch.zeros((4, 64), requires_grad=True)
+    plain = torch.zeros((4, 64))
+    packed = torch.zeros(16 * 4 * 17, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="x requires a gradient"):
+        ops.ts_mx_quantize(x)
+    with pytest.raises(ValueError, match="out requires a gradient"):
+        ops._rows(x, "out", 64)
+    with pytest.raises(ValueError, match="x requires a gradient"):
+        ops.ts_mx_project(packed, 16, x)
+    for call in (lambda: ops.ts_mx_quantize(x.detach()), lambda: ops.ts_mx_project(packed, 16, plain)):
+        with pytest.raises(ValueError, match="not on a GPU"):
+            call()
+    with torch.no_grad(), pytest.raises(ValueError, match="not on a GPU"):
+        ops.ts_mx_quantize(x)
+
+
 def test_a_library_on_another_hip_runtime_than_torch_is_refused(lib):
     code = "from paper_2604_13519_amd import binding as B\nB.load_library()\nfrom paper_2604_13519_amd import ops\ntry: ops.ts_mx_packed_bytes(16, 128)\nexcept RuntimeError as e: print(e)"
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
