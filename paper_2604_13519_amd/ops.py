@@ -172,7 +172,8 @@ def ts_mx_packed_bytes(n_out, n_in):
 
 
 def ts_mx_pack(codes, scales, n_in, out=None):
-    """Weights [n_out][n_in], given as codes and scales, laid out for ts_mx_project: a uint8 tensor to keep."""
+    """Weights [n_out][n_in], given as codes and scales, laid out for ts_mx_project: a uint8 tensor to keep.  The tensor object carries
+    the sizes (`ts_mx_shape`), which ts_mx_project holds its call against; of a copy or a view without them only the bytes are checked."""
     lib = _lib or _load()
     n_out, blocks = codes.shape[0], (n_in + 31) // 32
     pc, ps = _bytes(codes, "codes", (n_out, 16 * blocks)), _bytes(scales, "scales", (n_out, blocks))
@@ -180,6 +181,7 @@ def ts_mx_pack(codes, scales, n_in, out=None):
     if out is None:
         out = torch.empty(n, dtype=torch.uint8, device=codes.device)
     binding._check(lib.ts_mx_pack(pc, ps, n_out, n_in, _bytes(out, "out", (n,)), _stream(codes)))
+    out.ts_mx_shape = (n_out, n_in)
     return out
 
 
@@ -189,7 +191,7 @@ def ts_mx_project(packed, n_out, x, out=None):
     px, xs = _rows(x, "x")
     rows, n_in = x.shape
     pw = _bytes(packed, "packed")
-    if n_in < 1 or n_out < 1 or packed.numel() != -(-n_out // 16) * -(-n_in // 128) * _RECORD:
+    if n_in < 1 or n_out < 1 or packed.numel() != -(-n_out // 16) * -(-n_in // 128) * _RECORD or getattr(packed, "ts_mx_shape", (n_out, n_in)) != (n_out, n_in):
         _refuse("packed: not the weights of a [%d][%d] matrix", n_out, n_in)
     if out is None:
         out = x.new_empty((rows, n_out))

@@ -294,6 +294,22 @@ def test_pack_more_records_than_one_launch_counts():
     torch.cuda.empty_cache()
 
 
+def test_weights_of_other_sizes_are_refused():
+    """Also sizes that take the same bytes: whole records of 16 rows and 128 columns."""
+    packed, w = weights(200, 1000, 4)
+    x = torch.randn((3, 1024), device="cuda")
+    for n_out, n_in in ((200, 1001), (200, 999), (200, 1024), (199, 1000), (208, 1000), (200, 900), (184, 1000)):
+        with pytest.raises(ValueError, match="packed"):
+            ops.ts_mx_project(packed, n_out, x[:, :n_in])
+    check_project(packed, w, x[:, :1000], "its own size")
+    codes, scales = ops.ts_mx_quantize(torch.randn((200, 1001), device="cuda"))
+    ops.ts_mx_pack(codes, scales, 1001, packed)                # other weights in the same place: their size counts
+    check_project(packed, ops.ts_mx_dequantize(codes, scales, 1001).double(), x[:, :1001], "packed over")
+    with pytest.raises(ValueError, match="packed"):
+        ops.ts_mx_project(packed, 200, x[:, :1000])
+    check_project(packed.clone(), ops.ts_mx_dequantize(codes, scales, 1001).double(), x[:, :1001], "a copy")
+
+
 def test_pointers_of_the_host_are_refused():
     lib = ops._load()
     x = torch.zeros((4, 64), device="cuda")
