@@ -100,6 +100,17 @@ def _no_gradient(name):
         _refuse("%s requires a gradient, and these calls have none: detach it, or call them under torch.no_grad()", name)
 
 
+def _int(v, name):
+    """An int32 argument: ctypes would cut a larger one to its low bits."""
+    if not -(1 << 31) <= v < 1 << 31:
+        _refuse("%s: %d does not fit 32 bits", name, v)
+    return v
+
+
+def _out_of_range(e):
+    raise ValueError("an argument is out of range: %s" % e) from None
+
+
 def _rows(t, name, cols=None, dtype=None):
     """A matrix whose rows are contiguous; the distance between rows is free.  (address, distance)"""
     shape = t.shape
@@ -167,7 +178,7 @@ def ts_mx_dequantize(codes, scales, cols, dtype=torch.float32, out=None):
 
 def ts_mx_packed_bytes(n_out, n_in):
     n = C.c_uint64()
-    binding._check(_load().ts_mx_packed_bytes(n_out, n_in, C.byref(n)))
+    binding._check(_load().ts_mx_packed_bytes(_int(n_out, "n_out"), _int(n_in, "n_in"), C.byref(n)))
     return n.value
 
 
@@ -208,7 +219,7 @@ def ts_mx_project(packed, n_out, x, out=None):
 def ts_kv_layer_pages(kv, layer):
     """The pages of one layer of a library cache, to be given to ts_kv_append / ts_kv_attend as `k_pages` (with v_pages None)."""
     p = ts_kv_pages()
-    binding._check(_load().ts_kv_layer_pages(kv, layer, C.byref(p)))
+    binding._check(_load().ts_kv_layer_pages(kv, _int(layer, "layer"), C.byref(p)))
     return p
 
 
@@ -222,7 +233,7 @@ def ts_kv_page_table(kv, capacity_tokens):
 def ts_kv_extend(kv, n_pos, stream=None):
     """Counts n_pos positions that were appended on `stream` (a torch stream; default: the current one) as committed."""
     s = (stream or torch.cuda.current_stream()).cuda_stream
-    binding._check(_load().ts_kv_extend(kv, n_pos, s))
+    binding._check(_load().ts_kv_extend(kv, _int(n_pos, "n_pos"), s))
 
 
 def _pages(k_pages, v_pages):
@@ -279,8 +290,11 @@ def ts_kv_append(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_th
         heads = q_width // hd
     elif q_out is not None:
         _refuse("q_out without q")
-    a = _pack_append(*pages, table, t_stride, t_width, _ints(lengths, "lengths", n), _ints(row_offsets, "row_offsets", 2), n, rows, heads, _DTYPES[dtype],
-                     pq, q_stride, pk, k_stride, pv, v_stride, po, o_stride, rope_theta)
+    try:
+        a = _pack_append(*pages, table, t_stride, t_width, _ints(lengths, "lengths", n), _ints(row_offsets, "row_offsets", 2), n, rows, heads, _DTYPES[dtype],
+                         pq, q_stride, pk, k_stride, pv, v_stride, po, o_stride, rope_theta)
+    except struct.error as e:                              # a number that its member cannot hold
+        _out_of_range(e)
     binding._check(lib.ts_kv_append(a, _stream(k)))
     return q_out
 
@@ -288,7 +302,9 @@ def ts_kv_append(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_th
 def ts_kv_attend_workspace(n_seqs, n_q_heads, n_kv_heads, head_dim, max_len, window=0, device="cuda"):
     """A workspace tensor for ts_kv_attend calls of these sizes (None where they need none)."""
     n = C.c_uint64()
-    binding._check(_load().ts_kv_attend_workspace(n_seqs, n_q_heads, n_kv_heads, head_dim, max_len, window, C.byref(n)))
+    sizes = [_int(v, name) for v, name in ((n_seqs, "n_seqs"), (n_q_heads, "n_q_heads"), (n_kv_heads, "n_kv_heads"), (head_dim, "head_dim"),
+                                           (max_len, "max_len"), (window, "window"))]
+    binding._check(_load().ts_kv_attend_workspace(*sizes, C.byref(n)))
     return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
 
 
@@ -318,7 +334,10 @@ def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=N
     if workspace is None:
         workspace = ts_kv_attend_workspace(n, heads, kv_heads, hd, max_len, window, q.device)
     ws, ws_bytes = (0, 0) if workspace is None else (_bytes(workspace, "workspace"), workspace.numel())
-    a = _pack_attend(*pages, table, t_stride, t_width, _ints(lengths, "lengths", n), n, max_len, window, heads, _DTYPES[dtype], pq, q_stride, po, o_stride,
-                     lse.data_ptr(), hd ** -0.5 if scale is None else scale, ws, ws_bytes)
+    try:
+        a = _pack_attend(*pages, table, t_stride, t_width, _ints(lengths, "lengths", n), n, max_len, window, heads, _DTYPES[dtype], pq, q_stride, po, o_stride,
+                         lse.data_ptr(), hd ** -0.5 if scale is None else scale, ws, ws_bytes)
+    except struct.error as e:
+        _out_of_range(e)
     binding._check(lib.ts_kv_attend(a, _stream(q)))
     return out, lse

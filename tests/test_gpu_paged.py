@@ -499,6 +499,15 @@ def test_queries_rows_and_pages_that_require_gradients_are_refused():
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
 
 
+def test_lengths_and_windows_beyond_32_bits_are_refused():
+    k, v, table, _, _ = make_cache([20], 2, 64, torch.bfloat16, 0)
+    q = torch.zeros((1, 256), dtype=torch.bfloat16, device="cuda")
+    for ws in (None, torch.empty(1 << 20, dtype=torch.uint8, device="cuda")):
+        for top, window in ((1 << 31, 0), ((1 << 32) + 20, 0), (20, 1 << 31), (20, (1 << 32) + 4)):
+            with pytest.raises(ValueError, match="32 bits|out of range"):
+                ops.ts_kv_attend(k, v, table, ints([20]), q, top, window=window, workspace=ws)
+
+
 def test_captured_steps_replay_with_other_lengths():
     """Append, attend and the lengths' increment in one graph, replayed over a page border with eager work between."""
     hd, hq, hkv, n = 128, 8, 2, 3

@@ -163,6 +163,21 @@ def test_tensors_are_looked_at(lib):
         ops.ts_kv_attend(torch.zeros((3, 2, 16, 64)), torch.zeros((3, 2, 64, 16)), torch.zeros((1, 3), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros((1, 128)), 40)
 
 
+def test_numbers_beyond_32_bits_are_refused(lib):
+    """ctypes hands on the low 32 bits of a larger number: sizes of another matrix, a length of zero."""
+    big = (1 << 32) + 16
+    for call in (lambda: ops.ts_mx_packed_bytes(big, 128), lambda: ops.ts_mx_packed_bytes(16, big), lambda: ops.ts_mx_packed_bytes(-big, 128),
+                 lambda: ops.ts_kv_attend_workspace(1, 8, 8, 128, 1 << 32), lambda: ops.ts_kv_attend_workspace(1, 8, 8, 128, 100, 1 << 32),
+                 lambda: ops.ts_kv_attend_workspace((1 << 32) + 1, 8, 8, 128, 100), lambda: ops.ts_kv_extend(None, 1 << 32, stream=_NoStream),
+                 lambda: ops.ts_kv_layer_pages(None, 1 << 32)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+
+
+class _NoStream:
+    cuda_stream = 0
+
+
 def test_tensors_that_require_gradients_are_refused(lib):
     """No call has a backward pass: a result without one in a graph that records them would lose the gradient silently."""
     x = torch.zeros((4, 64), requires_grad=True)
