@@ -165,6 +165,8 @@ def ts_mx_quantize(x, codes=None, scales=None):
 def ts_mx_dequantize(codes, scales, cols, dtype=torch.float32, out=None):
     """The values [rows][cols] that codes and scales stand for (exact in both types; infinite from 2^128 on)."""
     lib = _lib or _load()
+    if dtype not in _DTYPES:
+        raise TypeError("dtype: float32 or bfloat16 is needed, got %s" % dtype)
     rows, blocks = codes.shape[0], (cols + 31) // 32
     pc, ps = _bytes(codes, "codes", (rows, 16 * blocks)), _bytes(scales, "scales", (rows, blocks))
     if out is None:

@@ -163,6 +163,13 @@ def test_tensors_are_looked_at(lib):
         ops.ts_kv_attend(torch.zeros((3, 2, 16, 64)), torch.zeros((3, 2, 64, 16)), torch.zeros((1, 3), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), torch.zeros((1, 128)), 40)
 
 
+def test_types_of_values_are_refused_by_name(lib):
+    codes, scales = torch.zeros((4, 32), dtype=torch.uint8), torch.zeros((4, 2), dtype=torch.uint8)
+    for dtype in (torch.float16, torch.float64, torch.int32, None):
+        with pytest.raises(TypeError, match="float32 or bfloat16"):
+            ops.ts_mx_dequantize(codes, scales, 64, dtype)
+
+
 def test_numbers_beyond_32_bits_are_refused(lib):
     """ctypes hands on the low 32 bits of a larger number: sizes of another matrix, a length of zero."""
     big = (1 << 32) + 16
