@@ -82,7 +82,7 @@ typedef struct {
  * the caller has written (every layer) by ts_kv_append on `stream`: waits for that stream, then
  * len += n_pos; an unapplied verify result is dropped, the pending token stays.  The library's own
  * passes run on the model's stream: they see what was appended before ts_kv_extend returned.
- * Errors: INVALID_ARG, KV_CAPACITY (length + n_pos beyond the capacity), DEVICE. */
+ * Errors: INVALID_ARG (also a stream of another GPU), KV_CAPACITY (length + n_pos beyond the capacity), DEVICE. */
 ts_status ts_kv_layer_pages(const ts_kv* kv, int32_t layer, ts_kv_pages* pages);
 ts_status ts_kv_page_table(const ts_kv* kv, int32_t* host_pages, int32_t n_pages);
 ts_status ts_kv_extend(ts_kv* kv, int32_t n_pos, ts_stream stream);

@@ -53,7 +53,9 @@ extern "C" ts_status ts_kv_extend(ts_kv* kv, int32_t n_pos, ts_stream stream) {
   if (!kv) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_extend: null cache");
   if (n_pos < 0) return ts_fail(TS_ERR_INVALID_ARG, "ts_kv_extend: %d positions", n_pos);
   if (n_pos > kv->capacity - kv->P) return ts_fail(TS_ERR_KV_CAPACITY, "committed %d + %d positions exceed the capacity %d", kv->P, n_pos, kv->capacity);
-  DeviceGuard on(kv->model->device);
+  int dev;
+  if (ts_status st = ops_device("ts_kv_extend", {kv->k_pool}, stream, &dev)) return st;      // a stream of another GPU wrote nothing here
+  DeviceGuard on(dev);
   TS_HIP(hipStreamSynchronize((hipStream_t)stream));
   kv->P += n_pos;
   kv->have_result = false;

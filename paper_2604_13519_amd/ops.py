@@ -233,7 +233,7 @@ def ts_kv_page_table(kv, capacity_tokens):
 
 
 def ts_kv_extend(kv, n_pos, stream=None):
-    """Counts n_pos positions that were appended on `stream` (a torch stream; default: the current one) as committed."""
+    """Counts n_pos positions that were appended on `stream` (a torch stream of the cache's GPU; default: the current one) as committed."""
     s = (stream or torch.cuda.current_stream()).cuda_stream
     binding._check(_load().ts_kv_extend(kv, _int(n_pos, "n_pos"), s))
 

@@ -560,6 +560,36 @@ def test_two_streams_at_once():
         assert torch.equal(o, want[i % 2][0]) and torch.equal(l, want[i % 2][1])
 
 
+def test_extend_waits_for_the_stream_it_is_given():
+    """Positions appended on a side stream behind other work are there once the length says so (one GPU here: a stream of
+    another one is refused by the same check as in the other calls)."""
+    cfg = wl.get_config("small_bf16")
+    model = B.ts_model_load(cfg, wl.gen_weights(cfg, 1))
+    kv = B.ts_kv_alloc(model, 64)
+    try:
+        hd, hkv = cfg.head_dim, cfg.n_kv_heads
+        table = torch.from_numpy(ops.ts_kv_page_table(kv, 64)).cuda()[None]
+        rows = torch.randn((5, 2 * hkv * hd), device="cuda").bfloat16()
+        big = torch.randn((4096, 4096), device="cuda")
+        lens, offs = ints([0]), ints([0, 5])
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                big = big @ big * 1e-3
+            for layer in range(cfg.n_layers):
+                ops.ts_kv_append(ops.ts_kv_layer_pages(kv, layer), None, table, lens, offs, None, rows[:, :hkv * hd], rows[:, hkv * hd:], 0.0)
+        ops.ts_kv_extend(kv, 5, stream=side)
+        assert side.query() and B.ts_kv_len(kv) == 5
+        gk, gv = B.ts_kv_export(kv, 0, 5, cfg)
+        want = rows.view(torch.int16).cpu().numpy().view(np.uint16).reshape(5, 2, hkv, hd)
+        for layer in range(cfg.n_layers):
+            assert np.array_equal(gk[layer], want[:, 0]) and np.array_equal(gv[layer], want[:, 1])
+    finally:
+        B.ts_kv_free(kv)
+        B.ts_model_free(model)
+
+
 # ---- together, over a cache of the library -------------------------------------------------------
 @pytest.mark.parametrize("cfg_name", ["small_bf16", "small_fp32"])
 @pytest.mark.parametrize("pooled", [False, True])
