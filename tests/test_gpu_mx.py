@@ -294,6 +294,48 @@ def test_pack_more_records_than_one_launch_counts():
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantize_more_values_than_one_launch_counts(dtype):
+    cols = 40                                                  # two blocks a row: 2^27 rows a launch
+    rows = (1 << 27) + 300
+    if torch.cuda.mem_get_info()[0] < (80 << 30):
+        pytest.skip("80 GB of device memory are needed")
+    x = torch.zeros((rows, cols), dtype=dtype, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    spans = [(0, 40), ((1 << 27) - 30, (1 << 27) + 30), (rows - 40, rows)]
+    for lo, hi in spans:
+        x[lo:hi] = torch.randn((hi - lo, cols), generator=g, device="cuda")
+    codes, scales = ops.ts_mx_quantize(x)
+    back = ops.ts_mx_dequantize(codes, scales, cols, dtype)
+    for lo, hi in spans:
+        want, want_scales = definition(x[lo:hi])
+        assert same(back[lo:hi], want) and torch.equal(scales[lo:hi].cpu(), want_scales)
+    assert not bool(back[100:200].any()) and not bool(codes[100:200].any())
+    del x, codes, scales, back
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_project_rows_and_outputs_beyond_32_bits(dtype):
+    """As many rows as a call takes, inside wider ones: inputs and outputs of more than 2^32 elements."""
+    rows, n_in, n_out, width = 1 << 19, 200, 40, 8448
+    if torch.cuda.mem_get_info()[0] < (100 << 30):
+        pytest.skip("100 GB of device memory are needed")
+    packed, w = weights(n_out, n_in, 9)
+    X = torch.zeros((rows, width), dtype=dtype, device="cuda")
+    Y = torch.full((rows, width), 3.0, dtype=dtype, device="cuda")
+    x, y = X[:, 8248:8448], Y[:, 8400:8440]
+    x.copy_(torch.randn((rows, n_in), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda"))
+    ops.ts_mx_project(packed, n_out, x, y)
+    for lo in (0, 1000, 254100, rows - 300):
+        xs = x[lo:lo + 300].double().contiguous()
+        want = xs @ w.t().contiguous()
+        assert bool(((y[lo:lo + 300].double() - want).abs() <= bound(xs, w, want, dtype) * 1.01).all()), lo
+        assert bool((Y[lo:lo + 300, :8400] == 3.0).all()) and bool((Y[lo:lo + 300, 8440:] == 3.0).all())
+    del X, Y, x, y
+    torch.cuda.empty_cache()
+
+
 def test_weights_of_other_sizes_are_refused():
     """Also sizes that take the same bytes: whole records of 16 rows and 128 columns."""
     packed, w = weights(200, 1000, 4)
