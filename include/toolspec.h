@@ -218,8 +218,9 @@ ts_status ts_prefill(ts_model* m, ts_kv* kv, const int32_t* tokens, int32_t n_to
  *   accepted_nodes  : out, optional (NULL ok), node index of each accepted token
  *   bonus_token     : out, arg-max token after the last accepted node (or the root)
  * Tokens emitted by the step = accepted_tokens[0..l) followed by bonus_token.
- * Errors: INVALID_ARG, INVALID_TREE, TOKEN_RANGE, KV_CAPACITY, STATE (no pending
- * token), DEVICE. */
+ * Errors: INVALID_ARG, INVALID_TREE, TOKEN_RANGE (also: every logit of the last accepted row is
+ * NaN, so that there is no bonus token; the cache has no result then), KV_CAPACITY, STATE (no
+ * pending token), DEVICE. */
 ts_status ts_verify(ts_model* m, ts_kv* kv,
                     const int32_t* draft_tokens, const int32_t* parent_idx, int32_t n_nodes,
                     int32_t* accept_len, int32_t* accepted_tokens, int32_t* accepted_nodes,
