@@ -92,7 +92,8 @@ ts_status ts_kv_extend(ts_kv* kv, int32_t n_pos, ts_stream stream);
 
 /* Appends new rows to the cache.  Rows [row_offsets[s], row_offsets[s + 1]) belong to sequence s
  * and get positions lengths[s], lengths[s] + 1, ... .  Keys are stored rotated (pair
- * (j, j + head_dim / 2) by position * rope_theta^(-2 j / head_dim); rope_theta 0: not rotated),
+ * (j, j + head_dim / 2) by position * rope_theta^(-2 j / head_dim), an angle that is good to 1e-7
+ * radians at any position; rope_theta 0: not rotated),
  * values as they are, both in the cache's dtype; with q, the rotated queries go to q_out (which
  * may be q).  Rows outside every sequence, and rows whose position is negative, beyond the table
  * or on a page outside [0, n_pages), leave cache and q_out as they were.  Lengths are not

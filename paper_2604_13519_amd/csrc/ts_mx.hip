@@ -12,8 +12,8 @@
 
 // ---------------------------------------------------------------------------------
 // quantisation: 16 bytes of values a lane, four lanes a block (fp32: eight).  Bound by HBM: it reads the values and writes 17 bytes a block.
-// 14336 x 4096 bf16 (117 MB read, 31 MB written, as counted), four matrices in turn: 30.0 us and the values back 29.0, 4.9 and
-// 5.1 TB/s; fp32 46.8 and 52.3 us, 5.7 and 5.1 TB/s; a copy of 1 GiB moves 5.1.  Two pieces a thread, a workgroup's width apart:
+// 14336 x 4096 bf16 (117 MB read, 31 MB written, as counted), four matrices in turn: 28.5 us and the values back 28.8, 5.2 TB/s
+// both; fp32 46.8 and 52.3 us, 5.7 and 5.1 TB/s; a copy of 1 GiB moves 5.1.  Two pieces a thread, a workgroup's width apart:
 // four 31.4 and 29.2 us (65 rows 3.4 and 2.6, with two 2.6 and 2.3), one 30.9 and 33.1.  A wave's loads and stores are whole lines:
 // eight fp32 values a lane, stored in two halves, 64.5 us.
 // ---------------------------------------------------------------------------------
@@ -173,7 +173,8 @@ static void launch_mx_dequantize(hipStream_t s, const uint8_t* codes, const uint
 // weights laid out for the product: records of (16 rows, 128 columns), chunk after chunk of a row tile.  A record is
 // what one wave loads for one chunk, contiguous: 16 bytes of codes per lane - lane l = 16 g + n: of row n, codes
 // 8 g .. + 7 of each of the chunk's four blocks, the operand of four matrix instructions - then the four scales of each
-// row.  Rows and blocks beyond the matrix hold zeros.
+// row.  Rows and blocks beyond the matrix hold zeros.  Done once, when a matrix is loaded: 14336 x 4096 28 us, 2.2 TB/s read and
+// written (codes are gathered in 4-byte pieces).
 // ---------------------------------------------------------------------------------
 constexpr int MX_REC = 1024 + 64;
 static int64_t mx_chunks(int64_t n_in) { return (n_in + 127) / 128; }
@@ -353,8 +354,8 @@ __device__ __forceinline__ void mx_emit_swiglu(const MxArgs& g, int row, int f, 
 // Few rows or few columns: KW waves share 16 rows by CT column tiles (of 16), wave w takes chunks w, w + KW, ..., one in use
 // and one on its way.  An input is used by one wave only, so a lane reads its pieces of its row itself: for
 // instruction i of a chunk, 64 neighbouring bytes of each of 16 rows.  The waves' sums meet in the LDS, added in their
-// order.  Bound by the start of the launch and one trip to memory: one bf16 row, 4096 x 4096 (9 MB): 3.6 us, of which 1.5 at
-// a copy's rate; 37 fp32 rows, 1001 x 1031: 5.6 us.
+// order.  Bound by the start of the launch and one trip to memory: one bf16 row, 4096 x 4096 (9 MB): 3.7 us, of which 1.8 at
+// a copy's rate; 37 fp32 rows, 1001 x 1031: 4.9 us.
 template <int IN, int OUT, int CT, int KW>
 __global__ __launch_bounds__(KW * 64) void k_mx_few(MxArgs g) {
   typedef typename MxElem<IN>::T E;
@@ -437,8 +438,8 @@ __global__ __launch_bounds__(KW * 64) void k_mx_few(MxArgs g) {
 // and weights are requested a step ahead.
 // bf16 rows, 4096 inputs: 2048 rows x 14336 columns 200 us, 1.2 PFLOP/s, what the library's product of bf16 matrices of these
 // sizes takes (199); the matrix pipes are busy 65 % of the time, the rest is issuing the widening of the codes, the
-// reads of the LDS and the barrier.  65 rows x 28672 columns 22 - 25 us: its 67 MB need 12 at a copy's rate, its
-// 65 rows 13 at the library's rate, the 80 it multiplies 16.  Rows or weights requested two or three steps ahead are no
+// reads of the LDS and the barrier.  65 rows x 28672 columns 22 - 25 us: its 67 MB need 13 at a copy's rate, its
+// 65 rows 13 at the library's rate, the 80 it multiplies 16, and 224 workgroups leave an eighth of the CUs without work.  Rows or weights requested two or three steps ahead are no
 // faster (25 - 26 us), nor are waves of 64 columns, which read half as much from the LDS (28 us with KW 2, 36 with 4).
 template <int T> struct MxTile;
 template <> struct MxTile<16> { typedef ts_f32x4 Acc; };
@@ -644,7 +645,8 @@ static void mx_launch(hipStream_t s, const MxArgs& g) {
 // Which shape a call takes: the one whose rounds of workgroups (256 CUs) times the time of a round is least.  The times are
 // microseconds of one round at 4096 inputs, measured between events with an eighth of the CUs to all of them at work; what is
 // beyond a start of 2.2 (direct) or 2.6 scales with the inputs.  Several blocks of fewer rows are offered as well as one: 64 rows
-// x 14336 inputs, 4096 columns: two blocks of 32 rows 17.9 us, one of 64 on half the CUs 30.8; 128 fp32 rows, 6144 columns 36.7, 45.6.
+// x 14336 inputs, 4096 columns: two blocks of 32 rows 17.9 us, one of 64 on half the CUs 30.8; 128 fp32 rows, 6144 columns 36.7, 45.6
+// (35.3 since the rows' terms are cut, not rounded; the fp32 times below are those of before).
 // For 2, 3, 4, 5 row tiles of 16, columns a workgroup:
 //   bf16 rows   32:  6.8   8.7  12.1  13.0     64:  7.9  10.0  12.8  14.7     128: 11.5  14.8  17.3  20.8
 //   fp32 rows                                  64: 24.8  35.3  45.8  52       128: 35    47    61.6  73

@@ -10,10 +10,12 @@
 // A workgroup takes the rows that share a page (a single row in a decoding step, up to 16 of a context) and a few
 // heads: the values are transposed within a page, so a page's 16 positions of a dimension are one 32-byte (fp32: 64)
 // piece, written whole.  The angle of position p and pair j is p theta^(-2 j / hd); as a number of turns it is formed and
-// reduced to [-1/2, 1/2] in 64 bits, so that far positions keep their phase, and sine and cosine are taken in fp32.
+// reduced to [-1/2, 1/2] in 64 bits, so that far positions keep their phase, and sine and cosine are taken in fp32: what is left is
+// rounded to 2^-26 of a turn there, 9e-8 radians, as much as a step of fp32 sines.
 //
 // Bound by the start of a launch for a step's rows (one row, 8 + 32 heads of 128: 3.9 us, of which starting a launch is 2 to 3) and by HBM
-// for contexts: 2040 rows of 8 + 64 heads move 80 MB (as counted) in 20 us, 4 TB/s; 2048 rows on whole pages 4.8 TB/s.
+// for contexts: 2040 rows of 8 + 64 heads move 80 MB (as counted) in 21.2 us, 3.8 TB/s; 2048 rows of 8 + 32 heads on whole pages 50 MB
+// in 10.2 us, 4.9 TB/s.
 // ---------------------------------------------------------------------------------
 constexpr int APPEND_THREADS = 256, APPEND_HEADS = 32;     // heads of a workgroup at most
 
@@ -236,8 +238,9 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
 // it needs, and the matching values are 16 contiguous bytes of the transposed page.  Maximum and sum of a head lie in
 // four lanes (l, l + 16, l + 32, l + 48); nothing passes through the LDS before the waves of a workgroup are joined.
 //
-// bf16, 8 KV heads of 128: 8 sequences of up to 32768 tokens, 64 query heads (727 MB, as counted): 125.5 us, 5.8 TB/s, a kernel
-// that only reads the same bytes takes 123; one sequence of 8192, 32 query heads (34 MB): 8.9 us and 3.1 of the join.
+// bf16, 8 KV heads of 128: 8 sequences of up to 32768 tokens, 64 query heads (727 MB, as counted): 125.7 us in a kernel trace, 5.8 TB/s,
+// a kernel that only reads the same bytes takes 123; one sequence of 8192, 32 query heads (34 MB): 10.6 us and 4.0 of the join in
+// the trace, 12.3 both in a captured graph.  fp32, 8 sequences of 8192, 8 KV heads of 128 (537 MB): 103.6 us, 5.2 TB/s.
 // ---------------------------------------------------------------------------------
 constexpr int ATT_WAVES = 4, ATT_KB = 32;
 
@@ -483,7 +486,7 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
       next = pages_of(min(kb + 3 * STEP, last));
       use(fb, kb + STEP);
     }
-  } else {                                                   // 128 fp32 dimensions do not fit twice
+  } else {                                                   // 128 fp32 dimensions do not fit twice; 5.2 TB/s as it is, see above
     int2 next = pages_of(kw);
     for (int kb = kw; kb < k1; kb += STEP) {
       Block f;
@@ -526,8 +529,8 @@ __global__ __launch_bounds__(ATT_WAVES * 64, 2) void k_kv_attend(AttendArgs g) {
 
 // The join of a sequence's splits: out = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i.  A workgroup per (sequence, head):
 // the weights of the splits first, into the LDS, then four dimensions a thread and the splits dealt to the 1024 / HD rows
-// of threads, so that a row's reads are few and all in flight at once.  A launch of its own, 3.1 us: joining in the last
-// workgroup to end needs the parts written through to memory by every workgroup, and one sequence of 8192 took 62 us so, not 12.5.
+// of threads, so that a row's reads are few and all in flight at once.  A launch of its own, 4.0 us in a kernel trace: joining in the
+// last workgroup to end needs the parts written through to memory by every workgroup, and one sequence of 8192 took 62 us so, not 12.5.
 constexpr int ATT_SPLITS = 512;                              // at most, see attend_cut
 template <typename TQ, int HD>
 __global__ __launch_bounds__(256) void k_kv_attend_join(AttendArgs g) {
@@ -669,9 +672,12 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
 // 128, 4 query heads each, microseconds: 8 sequences of 2048 keys 18.1, one a CU 16.8; of 32768 191 and 183; ragged ones, up to
 // 32768, 134 and 117; 16 ragged ones up to 2048 20.5 and 18.9), and so is less than one (8 ragged up to 2048: 16.8, not 12.7).
 // Only where they leave chunks of 128 keys, two a CU are as fast or faster: 8 of 1024 10.0 and 10.5, one of 8192 12.5 and 14.0.
-// A sequence of few keys is not cut, whose join (3.1) takes longer than what it saves, 1.05 per 128 keys of 256 bytes: 256 keys
+// A sequence of few keys is not cut, whose join (3 to 4) takes longer than what it saves, 1.05 per 128 keys of 256 bytes: 256 keys
 // whole 6.2, cut 7.5; 384 7.3 and 7.6; 512 8.4 and 7.4; of 128 bytes 512 keys 5.8 and 7.1, 1024 7.9 and 7.0; of 512 bytes 256 keys
 // 10.9 and 9.5.
+// Where the keys do not divide among the CUs in units of 128, fewer workgroups than CUs are left: one sequence of 8192 keys 512
+// workgroups of 128, 12.3 us, of 8193 176 of 384, 13.7; between 129 and 255 sequences x KV heads each sequence is whole, 16 of 4096 keys
+// 54.8 us (4.9 TB/s), 17 64.2 (4.4), 24 74.4 (5.4), 32 96.9 (5.5).
 constexpr int ATT_CUS = 256;
 static int64_t attend_units(int max_len, int window) {       // of 128 keys, in the longest sequence
   const int64_t span = window > 0 && window < max_len ? (int64_t)window + ATT_KB - 1 : max_len;
