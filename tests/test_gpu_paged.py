@@ -508,6 +508,39 @@ def test_lengths_and_windows_beyond_32_bits_are_refused():
                 ops.ts_kv_attend(k, v, table, ints([20]), q, top, window=window, workspace=ws)
 
 
+def test_as_many_sequences_as_a_call_takes():
+    """2^20 sequences of a page each, a row appended to every one, and attention of 15 heads: 2^24 - 2^20 of them."""
+    n, hq, hd = 1 << 20, 15, 64
+    if torch.cuda.mem_get_info()[0] < (40 << 30):
+        pytest.skip("40 GB of device memory are needed")
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k = torch.randn((n, 1, 16, hd), generator=g, device="cuda", dtype=torch.bfloat16)
+    v = torch.randn((n, 1, hd, 16), generator=g, device="cuda", dtype=torch.bfloat16)
+    table = torch.randperm(n, generator=g, device="cuda").to(torch.int32)[:, None]
+    lens = torch.randint(0, 16, (n,), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.randn((n, (hq + 2) * hd), generator=g, device="cuda", dtype=torch.bfloat16)
+    q, kk, vv = x.split((hq * hd, hd, hd), 1)
+    sample = [0, 1, 63, 64, 4095, 65536, n // 2 + 1, n - 2, n - 1] + [int(i) for i in np.random.default_rng(0).integers(0, n, 60)]
+    pages = table[sample, 0].long()
+    K0, V0 = k[pages, 0].cpu(), v[pages, 0].cpu()
+    turned = ops.ts_kv_append(k, v, table, lens, torch.arange(n + 1, dtype=torch.int32, device="cuda"), q, kk, vv, 1e4)
+    out, lse = ops.ts_kv_attend(k, v, table, lens + 1, turned, 16)
+    K1, V1, nums = k[pages, 0].cpu(), v[pages, 0].cpu(), lens[sample].tolist()
+    for i, (s, m) in enumerate(zip(sample, nums)):
+        want, rough = plain_turn(kk[s].cpu().view(1, hd), m, 1e4)
+        assert near(K1[i, m:m + 1], want, rough) and torch.equal(V1[i, :, m], vv[s].cpu()), s
+        want, rough = plain_turn(q[s].cpu().view(hq, hd), m, 1e4)
+        assert near(turned[s].cpu().view(hq, hd), want, rough), s
+        others = [p for p in range(16) if p != m]
+        assert torch.equal(K1[i, others], K0[i, others]) and torch.equal(V1[i][:, others], V0[i][:, others]), s
+        want, want_lse, rough, d, _ = plain_attend(turned[s].cpu(), K1[i, :m + 1, None], V1[i].t()[:m + 1, None], 1, hd, 0, hd ** -0.5)
+        tol = (2 * d[:, None] + 2.0 ** -20 + 2 * 80 * 2.0 ** -24) * rough + torch.finfo(torch.bfloat16).eps / 2 * want.abs()
+        assert bool(((out[s].double().cpu().view(hq, hd) - want).abs() <= tol).all()), s
+        assert bool(((lse[s].double().cpu() - want_lse).abs() <= d + 2.0 ** -20 + 80 * 2.0 ** -24 + 2.0 ** -23 * want_lse.abs()).all()), s
+    del k, v, x, q, kk, vv, turned, out, lse
+    torch.cuda.empty_cache()
+
+
 def test_captured_steps_replay_with_other_lengths():
     """Append, attend and the lengths' increment in one graph, replayed over a page border with eager work between."""
     hd, hq, hkv, n = 128, 8, 2, 3
