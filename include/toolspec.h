@@ -218,9 +218,10 @@ ts_status ts_prefill(ts_model* m, ts_kv* kv, const int32_t* tokens, int32_t n_to
  *   accepted_nodes  : out, optional (NULL ok), node index of each accepted token
  *   bonus_token     : out, arg-max token after the last accepted node (or the root)
  * Tokens emitted by the step = accepted_tokens[0..l) followed by bonus_token.
- * Errors: INVALID_ARG, INVALID_TREE, TOKEN_RANGE (also: every logit of the last accepted row is
- * NaN, so that there is no bonus token; the cache has no result then), KV_CAPACITY, STATE (no
- * pending token), DEVICE. */
+ * Where every logit of the last accepted row is NaN there is no bonus token: 2^31 - 1 stands for it,
+ * and ts_kv_commit refuses the result.
+ * Errors: INVALID_ARG, INVALID_TREE, TOKEN_RANGE, KV_CAPACITY, STATE (no pending
+ * token), DEVICE. */
 ts_status ts_verify(ts_model* m, ts_kv* kv,
                     const int32_t* draft_tokens, const int32_t* parent_idx, int32_t n_nodes,
                     int32_t* accept_len, int32_t* accepted_tokens, int32_t* accepted_nodes,
@@ -258,7 +259,7 @@ ts_status ts_verify_batch(ts_model* m, ts_kv* const* kvs, int32_t n_seqs,
  * Applies the most recent verify on this cache: the root's K/V stay at slot len,
  * the accepted node of depth d moves to slot len + d (all layers, all KV heads,
  * a pure copy since K is stored rotated), len += l + 1, pending <- bonus token.
- * STATE if there is no unapplied verify result. */
+ * STATE if there is no unapplied verify result, TOKEN_RANGE (nothing changed) if it has no bonus token. */
 ts_status ts_kv_commit(ts_kv* kv);
 
 /* ---- measurement --------------------------------------------------------------

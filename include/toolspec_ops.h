@@ -84,7 +84,7 @@ typedef struct {
  * passes run on the model's stream: they see what was appended before ts_kv_extend returned.
  * Passes of bf16 models read whole blocks of 64 positions in IEEE half: what the pages of their caches
  * hold has to be finite and at most 65504 in magnitude, also behind the length (pages come zeroed); a
- * pass that meets a NaN ends with TOKEN_RANGE.
+ * pass that meets a NaN has no next token (see ts_verify).
  * Errors: INVALID_ARG (also a stream of another GPU), KV_CAPACITY (length + n_pos beyond the capacity), DEVICE. */
 ts_status ts_kv_layer_pages(const ts_kv* kv, int32_t layer, ts_kv_pages* pages);
 ts_status ts_kv_page_table(const ts_kv* kv, int32_t* host_pages, int32_t n_pages);

@@ -935,11 +935,6 @@ static ts_status verify_impl(ts_model* m, ts_kv* const* kvs, int n_seqs, const i
   m->last_rows = R;
 
   // ---- hand the result back -----------------------------------------------------------
-  // Logits that are no numbers have no largest: the index is then none, and committed it would be the next pass's root.
-  for (int s = 0; s < n_seqs; ++s) {
-    const int t = m->res_host[(size_t)s * TS_RESULT_INTS + 1];
-    if (t < 0 || t >= c.vocab) return ts_fail(TS_ERR_TOKEN_RANGE, "sequence %d has no next token: no logit of the row is a number", s);
-  }
   for (int s = 0; s < n_seqs; ++s) {
     ts_kv* kv = kvs[s];
     const int32_t* res = m->res_host + (size_t)s * TS_RESULT_INTS;
@@ -1087,6 +1082,9 @@ extern "C" ts_status ts_kv_commit(ts_kv* kv) {
   if (!kv) return ts_fail(TS_ERR_INVALID_ARG, "null cache");
   if (!kv->have_result) return ts_fail(TS_ERR_STATE, "no unapplied verify result on this cache");
   ts_model* m = kv->model;
+  // logits that are no numbers have no largest: the index is then none, and must not become the next pass's root
+  if (kv->res_bonus < 0 || kv->res_bonus >= m->cfg.vocab)
+    return ts_fail(TS_ERR_TOKEN_RANGE, "the verify result has no next token: no logit of its last row is a number");
   (void)hipSetDevice(m->device);
   const int len = kv->res_accept_len;
   bool moves = false;
