@@ -150,6 +150,100 @@ ts_status ts_kv_attend(const ts_kv_attend_args* args, ts_stream stream);
 ts_status ts_kv_attend_workspace(int32_t n_seqs, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_len,
                                  int32_t window, uint64_t* bytes);
 
+/* ---- more rows, other rotations, 8-bit pages ---------------------------------------
+ * Pages of dtype TS_DTYPE_E4M3 (for the calls below only; head_dim 64 or 128) hold one byte per value, laid out as other
+ * pages are (keys [n_pages][n_kv_heads][16][head_dim], values [n_pages][n_kv_heads][head_dim][16]): OCP e4m3, four
+ * significant bits, largest 448.  k_scales and v_scales, [n_pages][n_kv_heads][16] bytes each, 16-byte aligned, hold e + 127
+ * for each position's row of a head, and a value stands for its e4m3 value times 2^e: e is the least that keeps the row's
+ * largest magnitude at or below 448 * 2^e, and at least -127 (all zeros: -127); values are rounded to nearest, ties to
+ * even.  A row with an infinity or NaN has scale byte 255 and all its values are NaN.  For pages of other types the two are
+ * null.  (A program that writes pages by itself may use other scales; 255 is NaN there too.) */
+enum { TS_DTYPE_E4M3 = 3 };
+typedef struct {
+  ts_kv_pages pages;
+  uint8_t* k_scales; uint8_t* v_scales;
+} ts_kv_pages_any;
+
+/* ts_kv_append for decoder blocks that norm the heads of queries and keys, turn them otherwise, or keep 8-bit pages.  Rows, offsets,
+ * lengths, tables and places as there.  A head of a query or key is, in fp32 and in this order
+ *   normed  : x / sqrt(mean of x^2 + norm_eps) * gain, where there is a gain: q_norm, k_norm, [head_dim] of norm_dtype, each
+ *             may be null
+ *   rotated : its first rope_dim values (even, at most head_dim; 0: none) in pairs - (j, j + rope_dim / 2), or (2 j, 2 j + 1)
+ *             with rope_pairs != 0 - by the angle position * f_j, and multiplied by rope_magnitude; the other values stay.
+ *             f_j = rope_freqs[j], rope_dim / 2 floats in radians per position (a table scaled for long contexts, say), or
+ *             rope_theta^(-2 j / rope_dim) where that is null (rope_theta 0: not rotated).  The angle is as good as that of ts_kv_append
+ *             (a table's entries are taken as exact).
+ * and then rounded once, to its place.  The position of the angle is that of the row, or positions[row] where that is not null
+ * (a draft tree's rows lie one behind the other and are turned by their depths); the row's place is not changed by it.
+ * A head whose squares overflow fp32 is normed to zeros, NaN stays NaN.
+ * Errors: INVALID_ARG (as ts_kv_append; scales missing or misaligned, rope_dim, norm_eps negative or not finite, rope_magnitude not finite,
+ * misaligned gains, frequencies or positions), DEVICE. */
+typedef struct {
+  ts_kv_pages_any cache;
+  const int32_t* table; int64_t table_stride; int32_t table_width;
+  const int32_t* lengths; const int32_t* row_offsets; const int32_t* positions;
+  int32_t n_seqs, n_rows, n_q_heads, dtype;
+  const void* q; int64_t q_stride;
+  const void* k; int64_t k_stride;
+  const void* v; int64_t v_stride;
+  void* q_out; int64_t q_out_stride;
+  const void* q_norm; const void* k_norm;
+  int32_t norm_dtype; float norm_eps;
+  const float* rope_freqs;
+  float rope_theta, rope_magnitude;
+  int32_t rope_dim, rope_pairs;
+} ts_kv_append_norm_rope_args;
+ts_status ts_kv_append_norm_rope(const ts_kv_append_norm_rope_args* args, ts_stream stream);
+
+/* Positions of a cache given back as rows: row row_offsets[s] + i of k_out and v_out is position starts[s] + i of sequence s,
+ * as it is stored (keys rotated), n_kv_heads heads of head_dim, in `dtype` (8-bit values and bf16 widen exactly to fp32 and 8-bit
+ * values to bf16, a scale byte of 253 or more aside, whose values may be infinite; fp32 rounds to bf16 once).  starts null: from position 0 on; k_out or
+ * v_out may be null.  Rows outside every sequence, and rows whose position is negative, beyond the table or on a page outside [0, n_pages),
+ * stay as they were.
+ * Errors: INVALID_ARG (as above; n_rows in [0, 2^23]), DEVICE. */
+typedef struct {
+  ts_kv_pages_any cache;
+  const int32_t* table; int64_t table_stride; int32_t table_width;
+  const int32_t* starts; const int32_t* row_offsets;
+  int32_t n_seqs, n_rows, dtype;
+  void* k_out; int64_t k_stride;
+  void* v_out; int64_t v_stride;
+} ts_kv_read_args;
+ts_status ts_kv_read(const ts_kv_read_args* args, ts_stream stream);
+
+/* Attention of chunks of rows over the cache: rows [row_offsets[s], row_offsets[s + 1]) belong to sequence s and have the
+ * positions lengths[s], lengths[s] + 1, ... whose keys and values ts_kv_append has written with the same lengths and offsets
+ * (row_offsets null: sequence s has row s alone).  A row sees the positions up to its own, with window > 0 only the last
+ * `window` of them; or, where ancestors is not null, the positions before lengths[s], row 0 of its chunk, and those rows j >= 1 of its
+ * chunk whose bit j - 1 of ancestors[row] is set (a draft tree of a root and up to 64 nodes; no row beyond 64 is seen; a row's own
+ * bit is set like any other; window has to be 0).  out, lse, scale, heads, pages out of range, max_len (here: no position of
+ * a row is at or above it), contents of what is not seen, and rows that see nothing: as ts_kv_attend; rows outside every sequence
+ * stay as they were in out and lse.  A seen infinite value makes its dimension infinite, or NaN where its probability is zero.
+ * Scores, sums and outputs are fp32; queries and probabilities of fp32 rows enter the products over bf16 and 8-bit pages with 24 bits;
+ * probabilities of bf16 rows are rounded to bf16, once, for the product with the values, not for their sum, where a chunk has
+ * more rows x heads per KV head than one tile (16), and have 24 bits too where it has not.
+ *   q, out    : [n_rows] rows of n_q_heads * head_dim, in `dtype`
+ *   lse       : [n_rows][n_q_heads] fp32, or null
+ *   ancestors : [n_rows] 64-bit sets, or null
+ *   workspace : ts_kv_attend_rows_workspace bytes for the same sizes, 16-byte aligned, contents irrelevant (null where that is 0)
+ * Errors: INVALID_ARG (as ts_kv_attend; window with ancestors, n_rows in [0, 2^23], n_rows below n_seqs where row_offsets is null,
+ * n_rows * n_q_heads or the workgroups beyond 2^24), DEVICE. */
+typedef struct {
+  ts_kv_pages_any cache;
+  const int32_t* table; int64_t table_stride; int32_t table_width;
+  const int32_t* lengths; const int32_t* row_offsets; const uint64_t* ancestors;
+  int32_t n_seqs, n_rows, max_len, window, n_q_heads, dtype;
+  const void* q; int64_t q_stride;
+  void* out; int64_t out_stride;
+  float* lse;
+  float scale;
+  void* workspace; uint64_t workspace_bytes;
+} ts_kv_attend_rows_args;
+ts_status ts_kv_attend_rows(const ts_kv_attend_rows_args* args, ts_stream stream);
+/* Bytes of workspace a call with these sizes needs, whatever the pages' type; never decreases with max_len at the same other sizes. */
+ts_status ts_kv_attend_rows_workspace(int32_t n_seqs, int32_t n_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                      int32_t max_len, int32_t window, uint64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

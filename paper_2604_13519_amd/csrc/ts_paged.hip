@@ -1,8 +1,6 @@
 // One layer's step over a paged cache: rows appended with the rotary embedding applied on the way, and attention of one
 // new token per sequence, split over the cache's length and joined.
-#include <math.h>
-
-#include "ts_ops.h"
+#include "ts_paged.h"
 
 // ---------------------------------------------------------------------------------
 // append
@@ -17,86 +15,11 @@
 // for contexts: 2040 rows of 8 + 64 heads move 80 MB (as counted) in 21.2 us, 3.8 TB/s; 2048 rows of 8 + 32 heads on whole pages 50 MB
 // in 10.2 us, 4.9 TB/s.
 // ---------------------------------------------------------------------------------
-constexpr int APPEND_THREADS = 256, APPEND_HEADS = 32;     // heads of a workgroup at most
-
-template <typename T> __device__ __forceinline__ float widen(T v) {
-  if constexpr (sizeof(T) == 2) return bf16_to_f32(v);
-  else return v;
-}
-// N consecutive elements in vectors
-template <int N, typename T>
-__device__ __forceinline__ void load_n(const T* p, float (&v)[N]) {
-  uint32_t u[N * sizeof(T) / 4];
-  if constexpr (N * sizeof(T) == 4) u[0] = load4(p);
-  else if constexpr (N * sizeof(T) == 8) { const uint2 w = load8(p); u[0] = w.x; u[1] = w.y; }
-  else
-#pragma unroll
-    for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) {
-      const uint4 w = load16((const char*)p + 16 * i);
-      u[4 * i] = w.x; u[4 * i + 1] = w.y; u[4 * i + 2] = w.z; u[4 * i + 3] = w.w;
-    }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if constexpr (sizeof(T) == 2) v[i] = __uint_as_float(i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
-    else v[i] = __uint_as_float(u[i]);
-  }
-}
-template <int N, typename T>
-__device__ __forceinline__ void store_n(T* p, const float (&v)[N]) {
-  uint32_t u[N * sizeof(T) / 4];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if constexpr (sizeof(T) == 2) { if (!(i & 1)) u[i / 2] = __builtin_bit_cast(uint32_t, to_bf16x2(v[i], v[i + 1])); }
-    else u[i] = __float_as_uint(v[i]);
-  }
-  if constexpr (N * sizeof(T) == 4) store4(p, u[0]);
-  else if constexpr (N * sizeof(T) == 8) store8(p, make_uint2(u[0], u[1]));
-  else
-#pragma unroll
-    for (int i = 0; i < (int)(N * sizeof(T) / 16); ++i) store16((char*)p + 16 * i, make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]));
-}
-
-// those of positions p0 .. p0 + N - 1 that lie in [lo, hi), in as few pieces as there are
-template <int N, typename T>
-__device__ __forceinline__ void store_some(T* p, int p0, int lo, int hi, const float* v) {
-  if (lo <= p0 && p0 + N <= hi) {
-    if constexpr (N == 1) st_from_f32(p, v[0]);
-    else {
-      float w[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = v[i];
-      store_n<N>(p, w);
-    }
-  } else if constexpr (N > 1) {
-    if (lo < p0 + N / 2) store_some<N / 2>(p, p0, lo, hi, v);
-    if (hi > p0 + N / 2) store_some<N / 2>(p + N / 2, p0 + N / 2, lo, hi, v + N / 2);
-  }
-}
-
 struct AppendArgs {
   ts_kv_append_args a;
   double log2_theta;                     // rope_theta > 0
   int window, heads;                     // of a workgroup: rows it looks for pages in, heads
 };
-
-// the last sequence whose first row is not behind `row`, -1 if none: 64 offsets at a time, one per lane
-__device__ __forceinline__ int seq_of_row(const int32_t* offsets, int n, int row) {
-  const int lane = threadIdx.x % 64;
-  int lo = 0, left = n;                  // offsets [lo, lo + left) are open; all before lo are <= row
-  for (;;) {
-    const int step = (left + 63) / 64;
-    const int i = lane * step;
-    const int c = __popcll(__ballot(i < left && offsets[lo + (i < left ? i : 0)] <= row));
-    if (c == 0) return lo - 1;
-    if (step == 1) return lo + c - 1;
-    lo += (c - 1) * step + 1;
-    left = min(step - 1, left - (c - 1) * step - 1);
-    if (left <= 0) return lo - 1;
-  }
-}
-
-// `cnt` rows from `row` on into slots `slot`, ... of a page, heads [head0, head1) of (queries, keys, values)
-struct AppendPage { int row, cnt, slot, page, head0, head1, hq, hkv; int64_t pos; };
 
 // Queries and keys, in pieces of VE pairs.  A thread requests all its pieces (more than four: in batches) before it stores
 // one - the stores may alias the loads for all the compiler knows - and the sines are worked out while they come.
@@ -157,40 +80,6 @@ __device__ __forceinline__ void append_turned(const AppendArgs& g, const AppendP
   }
 }
 
-template <typename TI, typename TC, int HD>
-__device__ __forceinline__ void append_values(const AppendArgs& g, const AppendPage& at) {
-  const ts_kv_append_args& a = g.a;
-  const int tid = threadIdx.x, cnt = at.cnt, slot = at.slot, row = at.row, page = at.page, hkv = at.hkv, turned = at.hq + at.hkv, head0 = at.head0, head1 = at.head1;
-  // values: a thread writes the positions of a dimension, of two for rows of bf16.  All rows are requested at once (what
-  // lies outside the new ones is the nearest of them, not stored); they go in vectors, cut at the ends.
-  constexpr int DV = 4 / sizeof(TI), SV = 16 / sizeof(TC);
-  const int val0 = max(head0, turned), end = slot + cnt;
-  for (int i = tid; i < (head1 - val0) * HD / DV; i += APPEND_THREADS) {
-    const int h = val0 - turned + i * DV / HD, d = i * DV % HD;
-    const TI* src = (const TI*)a.v + (int64_t)row * a.v_stride + h * HD + d;
-    TC* dst = (TC*)a.pages.v + (((int64_t)page * hkv + h) * HD + d) * 16;
-    if (cnt == 1) {
-      float w[DV];
-      load_n<DV>(src, w);
-#pragma unroll
-      for (int e = 0; e < DV; ++e) st_from_f32(dst + e * 16 + slot, w[e]);
-      continue;
-    }
-    float v[DV][16];
-#pragma unroll
-    for (int p = 0; p < 16; ++p) {
-      float w[DV];
-      load_n<DV>(src + (int64_t)min(max(p - slot, 0), cnt - 1) * a.v_stride, w);
-#pragma unroll
-      for (int e = 0; e < DV; ++e) v[e][p] = w[e];
-    }
-#pragma unroll
-    for (int p0 = 0; p0 < 16; p0 += SV)
-#pragma unroll
-      for (int e = 0; e < DV; ++e) store_some<SV>(dst + e * 16 + p0, p0, slot, end, &v[e][p0]);
-  }
-}
-
 // TI rows' element, TC cache's element
 template <typename TI, typename TC, int HD>
 __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
@@ -220,7 +109,7 @@ __global__ __launch_bounds__(APPEND_THREADS) void k_kv_append(AppendArgs g) {
     const AppendPage at{row, cnt, slot, page, head0, head1, hq, hkv, pos};
     __syncthreads();                                         // freq is there, the last page's cs no longer read
     if (head0 < turned) append_turned<TI, TC, HD>(g, at, freq, cs);
-    if (head1 > turned) append_values<TI, TC, HD>(g, at);
+    if (head1 > turned) append_values<TI, TC, HD>(a.v, a.v_stride, a.pages.v, at);
   }
 }
 
@@ -594,17 +483,8 @@ __global__ __launch_bounds__(256) void k_kv_attend_join(AttendArgs g) {
 // ---------------------------------------------------------------------------------
 static ts_status check_pages(const char* call, const ts_kv_pages& p, const int32_t* table, int64_t table_stride, int32_t table_width, const int32_t* lengths,
                              int32_t n_seqs, int32_t dtype) {
-  if (!p.k || !p.v || !table || !lengths) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
-  if (!ops_dtype_ok(p.dtype) || !ops_dtype_ok(dtype)) return ts_fail(TS_ERR_INVALID_ARG, "%s: dtype must be TS_DTYPE_F32 or TS_DTYPE_BF16", call);
-  if (p.n_pages < 1 || p.n_kv_heads < 1 || p.n_kv_heads > 65536) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d pages of %d KV heads", call, p.n_pages, p.n_kv_heads);
-  const int hd = p.head_dim;
-  if (p.dtype == TS_DTYPE_BF16 ? hd != 64 && hd != 128 : hd != 8 && hd != 16 && hd != 32 && hd != 64 && hd != 128)
-    return ts_fail(TS_ERR_INVALID_ARG, "%s: head_dim %d (bf16: 64 or 128; fp32: a power of two in [8,128])", call, hd);
-  if (!aligned_to(p.k, 16) || !aligned_to(p.v, 16)) return ts_fail(TS_ERR_INVALID_ARG, "%s: pages must be 16-byte aligned", call);
-  if (n_seqs < 1 || n_seqs > (1 << 20)) return ts_fail(TS_ERR_INVALID_ARG, "%s: n_seqs %d outside [1, 2^20]", call, n_seqs);
-  if (table_width < 1 || table_stride < table_width) return ts_fail(TS_ERR_INVALID_ARG, "%s: page table of width %d, stride %lld", call, table_width, (long long)table_stride);
-  if (!aligned_to(table, 4) || !aligned_to(lengths, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned table or lengths", call);
-  return TS_OK;
+  if (!ops_dtype_ok(p.dtype)) return ts_fail(TS_ERR_INVALID_ARG, "%s: dtype must be TS_DTYPE_F32 or TS_DTYPE_BF16", call);
+  return check_kv_pages(call, p, table, table_stride, table_width, lengths, n_seqs, dtype);
 }
 
 template <typename TI, typename TC>

@@ -1,0 +1,473 @@
+// Rows into and out of a paged cache of any type: appended with a norm of each head and a rotation of any layout in the same
+// pass, quantised to 8 bits where the pages are, and read back.
+#include "ts_paged.h"
+
+// ---------------------------------------------------------------------------------
+// append
+//
+// A workgroup takes the rows that share a page (up to 16) and a few heads.  LPV lanes hold a head's row, VE values each: the mean of
+// squares, and the largest magnitude for 8 bits, are sums and maxima over them.  A value's partner of the rotation is its
+// neighbour, in the lane, or half of rope_dim away, in another lane: normed rows pass through the LDS of their wave.  Angles are
+// formed and reduced in 64 bits as turns, sine and cosine taken in fp32, once per row and pair for all heads of the workgroup.
+// Values are transposed within a page; 8-bit ones are first quantised by rows, into the LDS, since a row's scale is needed
+// before its first byte.
+// ---------------------------------------------------------------------------------
+constexpr int RA_THREADS = 256, RA_HEADS = 8;
+
+struct AppendAnyArgs {
+  ts_kv_append_norm_rope_args a;
+  double log2_theta;
+  int window;                            // rows a workgroup looks for pages in
+  bool turn;                             // rope_dim > 0 and frequencies that are not all zero
+};
+
+template <int LPV>
+__device__ __forceinline__ float sum_over(float v) {
+#pragma unroll
+  for (int o = LPV / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+template <int LPV>
+__device__ __forceinline__ uint32_t max_over(uint32_t v) {
+#pragma unroll
+  for (int o = LPV / 2; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  return v;
+}
+// the bits of the largest magnitude of a row: magnitudes order like their bits, NaN above infinity
+template <int LPV, int VE>
+__device__ __forceinline__ uint32_t top_bits(const float (&x)[VE]) {
+  uint32_t t = 0;
+#pragma unroll
+  for (int e = 0; e < VE; ++e) t = max(t, __float_as_uint(x[e]) & 0x7fffffffu);
+  return max_over<LPV>(t);
+}
+template <int VE>
+__device__ __forceinline__ void to_codes(const float (&x)[VE], uint32_t byte, uint32_t (&w)[VE / 4]) {
+  const float inv = __uint_as_float((254u - min(byte, 253u)) << 23);
+#pragma unroll
+  for (int e = 0; e < VE; e += 4) w[e / 4] = byte == 255 ? 0x7f7f7f7fu : f32_to_e4m3(x[e] * inv, x[e + 1] * inv, x[e + 2] * inv, x[e + 3] * inv);
+}
+
+template <typename TI, typename TC, int HD>
+struct AppendAny {
+  static constexpr int VE = sizeof(TI) == 2 ? 8 : 4, LPV = HD / VE, VECS = RA_THREADS / LPV, BATCH = 4, HALF = HD / 2;
+  static constexpr bool E8 = sizeof(TC) == 1;
+  float2 cs[16 * HALF];
+  double freq[HALF];
+  union {
+    float x[RA_THREADS / 64][64 * VE];           // normed rows of a wave
+    uint8_t v[E8 ? RA_HEADS * 16 * HD : 1];      // quantised values, [head][position][dimension]
+  };
+};
+
+// queries and keys
+template <typename TI, typename TC, int HD>
+__device__ __forceinline__ void any_turned(const AppendAnyArgs& g, const AppendPage& at, AppendAny<TI, TC, HD>& s) {
+  typedef AppendAny<TI, TC, HD> S;
+  constexpr int VE = S::VE, LPV = S::LPV, HALF = S::HALF, BATCH = S::BATCH;
+  const ts_kv_append_norm_rope_args& a = g.a;
+  const int tid = threadIdx.x, cnt = at.cnt, n = (min(at.head1, at.hq + at.hkv) - at.head0) * cnt;
+  const int c = tid % LPV, d0 = c * VE, rd = a.rope_dim, rh = rd / 2;
+  const bool whole = rd % (2 * VE) == 0;                     // a lane's partners are one lane's
+  float* mine = s.x[tid / 64] + tid % 64 / LPV * HD;
+  auto gains = [&](const void* p, float (&v)[VE]) {
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] = a.norm_dtype == TS_DTYPE_BF16 ? bf16_to_f32(((const bf16_t*)p)[d0 + e]) : ((const float*)p)[d0 + e];
+  };
+  float gq[VE], gk[VE];
+  if (a.q_norm && at.head0 < at.hq) gains(a.q_norm, gq);
+  if (a.k_norm && at.head1 > at.hq) gains(a.k_norm, gk);
+  for (int i0 = 0; i0 < n; i0 += BATCH * S::VECS) {
+    float x[BATCH][VE];
+    int rr[BATCH], hh[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i0 + b * S::VECS >= n) break;
+      const int i = min(i0 + b * S::VECS + tid / LPV, n - 1);
+      hh[b] = i / cnt;
+      rr[b] = i - hh[b] * cnt;
+      hh[b] += at.head0;
+      const int64_t row = at.row + rr[b];
+      load_n<VE>((hh[b] < at.hq ? (const TI*)a.q + row * a.q_stride + (int64_t)hh[b] * HD : (const TI*)a.k + row * a.k_stride + (int64_t)(hh[b] - at.hq) * HD) + d0, x[b]);
+    }
+    if (g.turn && i0 == 0) {
+      for (int i = tid; i < cnt * rh; i += RA_THREADS) {
+        const int r = i / rh, j = i - r * rh;
+        const int64_t p = a.positions ? a.positions[at.row + r] : at.pos + r;
+        const double t = s.freq[j] * (double)p, rest = t - rint(t);
+        float sn, cn;
+        sincospif(2.f * (float)rest, &sn, &cn);
+        s.cs[r * HALF + j] = make_float2(cn * a.rope_magnitude, sn * a.rope_magnitude);
+      }
+      __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i0 + b * S::VECS >= n) break;
+      const bool is_q = hh[b] < at.hq;
+      float (&v)[VE] = x[b];
+      if (is_q ? a.q_norm != nullptr : a.k_norm != nullptr) {      // all lanes of a row go one way
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) ss += v[e] * v[e];
+        const float rs = 1.f / sqrtf(sum_over<LPV>(ss) * (1.f / HD) + a.norm_eps);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) v[e] = v[e] * rs * (is_q ? gq[e] : gk[e]);
+      }
+      if (g.turn) {
+        const float2* cs = s.cs + rr[b] * HALF;
+        if (a.rope_pairs) {
+#pragma unroll
+          for (int e = 0; e < VE; e += 2) {
+            if (d0 + e >= rd) break;
+            const float2 w = cs[(d0 + e) / 2];
+            const float u = v[e] * w.x - v[e + 1] * w.y;
+            v[e + 1] = v[e + 1] * w.x + v[e] * w.y;
+            v[e] = u;
+          }
+        } else {
+          // one wave writes and reads here, and its LDS accesses are done in order
+#pragma unroll
+          for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4*>(mine + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          __builtin_amdgcn_wave_barrier();
+          asm volatile("" ::: "memory");
+          if (whole && d0 < rd) {
+            const bool low = d0 < rh;
+            const float* other = mine + (low ? d0 + rh : d0 - rh);
+            const float2* w = cs + (low ? d0 : d0 - rh);
+#pragma unroll
+            for (int e = 0; e < VE; ++e) v[e] = v[e] * w[e].x + (low ? -other[e] : other[e]) * w[e].y;
+          } else if (!whole) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+              const int d = d0 + e;
+              if (d >= rd) break;
+              const bool low = d < rh;
+              const float2 w = cs[low ? d : d - rh];
+              const float o = mine[low ? d + rh : d - rh];
+              v[e] = v[e] * w.x + (low ? -o : o) * w.y;
+            }
+          }
+          __builtin_amdgcn_wave_barrier();
+          asm volatile("" ::: "memory");
+        }
+      }
+      const bool there = i0 + b * S::VECS + tid / LPV < n;
+      if constexpr (S::E8) {
+        const uint32_t byte = scale_byte(top_bits<LPV>(v));
+        if (there && !is_q) {
+          const int64_t at16 = ((int64_t)at.page * at.hkv + (hh[b] - at.hq)) * 16 + at.slot + rr[b];
+          uint32_t w[VE / 4];
+          to_codes(v, byte, w);
+          uint8_t* dst = (uint8_t*)a.cache.pages.k + at16 * HD + d0;
+          if constexpr (VE == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+          else *reinterpret_cast<uint32_t*>(dst) = w[0];
+          if (c == 0) a.cache.k_scales[at16] = (uint8_t)byte;
+        }
+      } else if (there && !is_q) {
+        store_n<VE>((TC*)a.cache.pages.k + (((int64_t)at.page * at.hkv + (hh[b] - at.hq)) * 16 + at.slot + rr[b]) * HD + d0, v);
+      }
+      if (there && is_q) store_n<VE>((TI*)a.q_out + (int64_t)(at.row + rr[b]) * a.q_out_stride + (int64_t)hh[b] * HD + d0, v);
+    }
+  }
+}
+
+// bytes [lo, hi) of the sixteen in w, in as few pieces as there are
+template <int N>
+__device__ __forceinline__ void store_bytes(uint8_t* p, int p0, int lo, int hi, const uint32_t* w) {
+  if (hi <= p0 || lo >= p0 + N) return;
+  if (lo <= p0 && p0 + N <= hi) {
+    if constexpr (N == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if constexpr (N == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    else if constexpr (N == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+    else if constexpr (N == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)(w[0] >> p0 % 4 * 8);
+    else *p = (uint8_t)(w[0] >> p0 % 4 * 8);
+  } else if constexpr (N > 1) {
+    store_bytes<N / 2>(p, p0, lo, hi, w);
+    store_bytes<N / 2>(p + N / 2, p0 + N / 2, lo, hi, N >= 8 ? w + N / 8 : w);
+  }
+}
+
+// values into 8-bit pages
+template <typename TI, int HD>
+__device__ __forceinline__ void any_values8(const AppendAnyArgs& g, const AppendPage& at, AppendAny<TI, e4m3_t, HD>& s) {
+  typedef AppendAny<TI, e4m3_t, HD> S;
+  constexpr int VE = S::VE, LPV = S::LPV, BATCH = S::BATCH;
+  const ts_kv_append_norm_rope_args& a = g.a;
+  const int tid = threadIdx.x, cnt = at.cnt, turned = at.hq + at.hkv, val0 = max(at.head0, turned), n = (at.head1 - val0) * cnt;
+  const int d0 = tid % LPV * VE;
+  uint8_t* vp = (uint8_t*)a.cache.pages.v;
+  __syncthreads();                                           // the normed rows' place is no longer read
+  for (int i0 = 0; i0 < n; i0 += BATCH * S::VECS) {
+    float x[BATCH][VE];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      if (i0 + b * S::VECS >= n) break;
+      const int i = min(i0 + b * S::VECS + tid / LPV, n - 1), h = i / cnt;
+      load_n<VE>((const TI*)a.v + (int64_t)(at.row + i - h * cnt) * a.v_stride + (int64_t)(val0 - turned + h) * HD + d0, x[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = i0 + b * S::VECS + tid / LPV, h = i / cnt, r = i - h * cnt;
+      if (i0 + b * S::VECS >= n) break;
+      const uint32_t byte = scale_byte(top_bits<LPV>(x[b]));
+      if (i >= n) continue;
+      uint32_t w[VE / 4];
+      to_codes(x[b], byte, w);
+      const int64_t head = (int64_t)at.page * at.hkv + (val0 - turned + h);
+      if (d0 == 0) a.cache.v_scales[head * 16 + at.slot + r] = (uint8_t)byte;
+      if (cnt == 1) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) vp[(head * HD + d0 + e) * 16 + at.slot] = (uint8_t)(w[e / 4] >> e % 4 * 8);
+      } else {
+        uint8_t* to = s.v + (h * 16 + at.slot + r) * HD + d0;
+        if constexpr (VE == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(to) = w[0];
+      }
+    }
+  }
+  if (cnt == 1) return;
+  __syncthreads();
+  // four dimensions a thread: sixteen positions of them, transposed by bytes
+  for (int i = tid; i < (at.head1 - val0) * HD / 4; i += RA_THREADS) {
+    const int h = i * 4 / HD, d = i * 4 % HD;
+    uint32_t w[4][4];
+#pragma unroll
+    for (int p = 0; p < 16; p += 4) {
+      const uint8_t* from = s.v + (h * 16 + p) * HD + d;
+      const uint32_t r0 = *(const uint32_t*)from, r1 = *(const uint32_t*)(from + HD), r2 = *(const uint32_t*)(from + 2 * HD), r3 = *(const uint32_t*)(from + 3 * HD);
+      const uint32_t lo01 = __builtin_amdgcn_perm(r1, r0, 0x05010400u), hi01 = __builtin_amdgcn_perm(r1, r0, 0x07030602u);      // bytes 0 0 1 1, 2 2 3 3
+      const uint32_t lo23 = __builtin_amdgcn_perm(r3, r2, 0x05010400u), hi23 = __builtin_amdgcn_perm(r3, r2, 0x07030602u);
+      w[0][p / 4] = __builtin_amdgcn_perm(lo23, lo01, 0x05040100u);
+      w[1][p / 4] = __builtin_amdgcn_perm(lo23, lo01, 0x07060302u);
+      w[2][p / 4] = __builtin_amdgcn_perm(hi23, hi01, 0x05040100u);
+      w[3][p / 4] = __builtin_amdgcn_perm(hi23, hi01, 0x07060302u);
+    }
+    uint8_t* dst = vp + (((int64_t)at.page * at.hkv + (val0 - turned + h)) * HD + d) * 16;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) store_bytes<16>(dst + 16 * e, 0, at.slot, at.slot + cnt, w[e]);
+  }
+}
+
+template <typename TI, typename TC, int HD>
+__global__ __launch_bounds__(RA_THREADS) void k_kv_append_any(AppendAnyArgs g) {
+  __shared__ AppendAny<TI, TC, HD> s;
+  const ts_kv_append_norm_rope_args& a = g.a;
+  const int tid = threadIdx.x, hkv = a.cache.pages.n_kv_heads, hq = a.q ? a.n_q_heads : 0;
+  const int head0 = blockIdx.y * RA_HEADS, turned = hq + hkv, head1 = min(head0 + RA_HEADS, turned + hkv);
+  if (g.turn && head0 < turned && tid < a.rope_dim / 2)      // turns per position
+    s.freq[tid] = (a.rope_freqs ? (double)a.rope_freqs[tid] : exp2(g.log2_theta * (-2.0 * tid / a.rope_dim))) * 0.15915494309189535;
+
+  // the page's first new row takes the others along; a workgroup takes the pages whose first new row is in its window
+  const int window1 = min((int)(blockIdx.x + 1) * g.window, a.n_rows);
+  for (int row = blockIdx.x * g.window, cnt; row < window1; row += cnt) {
+    cnt = 1;
+    const int seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
+    if (seq < 0 || seq >= a.n_seqs) continue;
+    const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.n_rows);
+    const int64_t pos = (int64_t)a.lengths[seq] + row - first;
+    if (pos < 0 || row >= end) continue;
+    const int slot = (int)(pos & 15);
+    cnt = min(16 - slot, end - row);
+    if ((row != max(first, 0) && slot != 0) || pos >= (int64_t)a.table_width * 16) continue;
+    const int page = a.table[(int64_t)seq * a.table_stride + pos / 16];
+    if (page < 0 || page >= a.cache.pages.n_pages) continue;
+    const AppendPage at{row, cnt, slot, page, head0, head1, hq, hkv, pos};
+    __syncthreads();                                         // freq is there, the last page's LDS contents no longer read
+    if (head0 < turned) any_turned<TI, TC, HD>(g, at, s);
+    if (head1 > turned) {
+      if constexpr (sizeof(TC) == 1) any_values8<TI, HD>(g, at, s);
+      else append_values<TI, TC, HD>(a.v, a.v_stride, a.cache.pages.v, at);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// read: the way back.  A workgroup takes the positions of a page and a few heads, keys first; a thread of the values takes all positions
+// of a few dimensions, so that a wave's rows are written in long pieces.
+// ---------------------------------------------------------------------------------
+struct ReadArgs {
+  ts_kv_read_args a;
+  int window;
+};
+
+template <typename TC, typename TO, int HD>
+__global__ __launch_bounds__(RA_THREADS) void k_kv_read(ReadArgs g) {
+  constexpr int VE = sizeof(TC) == 1 && sizeof(TO) == 2 ? 8 : 4, PIECES = HD / VE, DV = 4 / sizeof(TC);
+  const ts_kv_read_args& a = g.a;
+  const int tid = threadIdx.x, hkv = a.cache.pages.n_kv_heads;
+  const int head0 = blockIdx.y * RA_HEADS, head1 = min(head0 + RA_HEADS, 2 * hkv);
+  const int window1 = min((int)(blockIdx.x + 1) * g.window, a.n_rows);
+  for (int row = blockIdx.x * g.window, cnt; row < window1; row += cnt) {
+    cnt = 1;
+    const int seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
+    if (seq < 0 || seq >= a.n_seqs) continue;
+    const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.n_rows);
+    const int64_t pos = (a.starts ? (int64_t)a.starts[seq] : 0) + row - first;
+    if (pos < 0 || row >= end) continue;
+    const int slot = (int)(pos & 15);
+    cnt = min(16 - slot, end - row);
+    if ((row != max(first, 0) && slot != 0) || pos >= (int64_t)a.table_width * 16) continue;
+    const int page = a.table[(int64_t)seq * a.table_stride + pos / 16];
+    if (page < 0 || page >= a.cache.pages.n_pages) continue;
+    if (a.k_out && head0 < hkv) {
+      const int n = (min(head1, hkv) - head0) * cnt * PIECES;
+      for (int i = tid; i < n; i += RA_THREADS) {
+        const int c = i % PIECES, hr = i / PIECES, h = head0 + hr / cnt, r = hr % cnt;
+        const int64_t at16 = ((int64_t)page * hkv + h) * 16 + slot + r;
+        float v[VE];
+        if constexpr (sizeof(TC) == 1) {
+          const uint8_t* src = (const uint8_t*)a.cache.pages.k + at16 * HD + c * VE;
+          const float scale = scale_of(a.cache.k_scales[at16]);
+#pragma unroll
+          for (int e = 0; e < VE; e += 4) e4m3_to_f32(*(const uint32_t*)(src + e), v + e);
+#pragma unroll
+          for (int e = 0; e < VE; ++e) v[e] *= scale;
+        } else {
+          load_n<VE>((const TC*)a.cache.pages.k + at16 * HD + c * VE, v);
+        }
+        store_n<VE>((TO*)a.k_out + (int64_t)(row + r) * a.k_stride + (int64_t)h * HD + c * VE, v);
+      }
+    }
+    if (a.v_out && head1 > hkv) {
+      const int val0 = max(head0, hkv) - hkv;
+      for (int i = tid; i < (head1 - hkv - val0) * HD / DV; i += RA_THREADS) {
+        const int h = val0 + i * DV / HD, d = i * DV % HD;
+        const int64_t head = (int64_t)page * hkv + h;
+        float v[DV][16];
+#pragma unroll
+        for (int e = 0; e < DV; ++e) {
+          if constexpr (sizeof(TC) == 1) {
+            const uint4 w = *reinterpret_cast<const uint4*>((const uint8_t*)a.cache.pages.v + (head * HD + d + e) * 16);
+            e4m3_to_f32(w.x, v[e]); e4m3_to_f32(w.y, v[e] + 4); e4m3_to_f32(w.z, v[e] + 8); e4m3_to_f32(w.w, v[e] + 12);
+          } else {
+            load_n<16>((const TC*)a.cache.pages.v + (head * HD + d + e) * 16, v[e]);
+          }
+        }
+        if constexpr (sizeof(TC) == 1) {
+          const uint4 sc = *reinterpret_cast<const uint4*>(a.cache.v_scales + head * 16);
+          const uint32_t u[4] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+          for (int p = 0; p < 16; ++p) {
+            const float scale = scale_of(u[p / 4] >> p % 4 * 8 & 255);
+#pragma unroll
+            for (int e = 0; e < DV; ++e) v[e][p] *= scale;
+          }
+        }
+        TO* dst = (TO*)a.v_out + (int64_t)row * a.v_stride + (int64_t)h * HD + d;
+#pragma unroll
+        for (int p = 0; p < 16; ++p) {
+          if (p < slot || p >= slot + cnt) continue;
+          float w[DV];
+#pragma unroll
+          for (int e = 0; e < DV; ++e) w[e] = v[e][p];
+          TO* to = dst + (int64_t)(p - slot) * a.v_stride;
+          if constexpr (DV * sizeof(TO) >= 4) store_n<DV>(to, w);
+          else st_from_f32(to, w[0]);
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------------
+// rows of a window, as ts_kv_append takes them
+static int window_of(int n_rows, int n_seqs) {
+  const int each = n_rows / n_seqs;
+  return each < 2 ? 1 : each < 8 ? 2 : each < 256 ? 4 : each < 1024 ? 8 : 16;
+}
+
+template <typename TI>
+static void launch_append_any(const AppendAnyArgs& g, dim3 grid, hipStream_t s) {
+  const ts_kv_pages& p = g.a.cache.pages;
+#define TS_APPEND_ANY(TC, HD) if (p.head_dim == HD) return k_kv_append_any<TI, TC, HD><<<grid, RA_THREADS, 0, s>>>(g)
+  if (p.dtype == TS_DTYPE_E4M3) { TS_APPEND_ANY(e4m3_t, 64); TS_APPEND_ANY(e4m3_t, 128); }
+  else if (p.dtype == TS_DTYPE_BF16) { TS_APPEND_ANY(bf16_t, 64); TS_APPEND_ANY(bf16_t, 128); }
+  else { TS_APPEND_ANY(float, 8); TS_APPEND_ANY(float, 16); TS_APPEND_ANY(float, 32); TS_APPEND_ANY(float, 64); TS_APPEND_ANY(float, 128); }
+#undef TS_APPEND_ANY
+}
+
+extern "C" ts_status ts_kv_append_norm_rope(const ts_kv_append_norm_rope_args* args, ts_stream stream) {
+  const char* call = "ts_kv_append_norm_rope";
+  if (!args) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  const ts_kv_append_norm_rope_args& a = *args;
+  const ts_kv_pages& p = a.cache.pages;
+  ts_status st = check_kv_pages_any(call, a.cache, a.table, a.table_stride, a.table_width, a.lengths, a.n_seqs, a.dtype);
+  if (st) return st;
+  const int hd = p.head_dim, esz = ops_esz(a.dtype);
+  if (a.n_rows < 0 || a.n_rows > (1 << 23)) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d rows outside [0, 2^23]", call, a.n_rows);
+  if (!a.row_offsets || !aligned_to(a.row_offsets, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: null or misaligned row_offsets", call);
+  if (!aligned_to(a.positions, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned positions", call);
+  if (!(a.rope_theta >= 0.f) || !(a.rope_theta < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "%s: rope_theta %g must be zero or positive", call, a.rope_theta);
+  if (a.rope_dim < 0 || a.rope_dim > hd || a.rope_dim % 2) return ts_fail(TS_ERR_INVALID_ARG, "%s: rope_dim %d must be even and in [0, %d]", call, a.rope_dim, hd);
+  if (!aligned_to(a.rope_freqs, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned rope_freqs", call);
+  if (!(fabsf(a.rope_magnitude) < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "%s: rope_magnitude must be finite", call);
+  if (a.q_norm || a.k_norm) {
+    if (!ops_dtype_ok(a.norm_dtype)) return ts_fail(TS_ERR_INVALID_ARG, "%s: norm_dtype must be TS_DTYPE_F32 or TS_DTYPE_BF16", call);
+    if (!(a.norm_eps >= 0.f) || !(a.norm_eps < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "%s: norm_eps %g must be zero or positive", call, a.norm_eps);
+    if (!aligned_to(a.q_norm, ops_esz(a.norm_dtype)) || !aligned_to(a.k_norm, ops_esz(a.norm_dtype))) return ts_fail(TS_ERR_INVALID_ARG, "%s: gains are not aligned to their type", call);
+  }
+  if ((a.q != nullptr) != (a.q_out != nullptr)) return ts_fail(TS_ERR_INVALID_ARG, "%s: q and q_out belong together", call);
+  if (a.q && (a.n_q_heads < 1 || a.n_q_heads > 65536)) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d query heads", call, a.n_q_heads);
+  if (a.n_rows == 0) return TS_OK;
+  if (!a.k || !a.v) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  const int64_t kv_row = (int64_t)p.n_kv_heads * hd, q_row = (int64_t)a.n_q_heads * hd;
+  if (a.k_stride < kv_row || a.v_stride < kv_row || (a.q && (a.q_stride < q_row || a.q_out_stride < q_row)))
+    return ts_fail(TS_ERR_INVALID_ARG, "%s: a row stride is below its row", call);
+  if (!aligned_to(a.k, esz) || !aligned_to(a.v, esz) || !aligned_to(a.q, esz) || !aligned_to(a.q_out, esz))
+    return ts_fail(TS_ERR_INVALID_ARG, "%s: rows are not aligned to their type", call);
+  int dev;
+  if ((st = ops_device(call, {p.k, p.v, a.cache.k_scales, a.cache.v_scales, a.table, a.lengths, a.row_offsets, a.positions, a.q, a.k, a.v, a.q_out, a.q_norm, a.k_norm, a.rope_freqs},
+                       stream, &dev))) return st;
+  DeviceGuard on(dev);
+  AppendAnyArgs g{};
+  g.a = a;
+  g.turn = a.rope_dim > 0 && (a.rope_freqs || a.rope_theta > 0.f);
+  g.log2_theta = a.rope_theta > 0.f ? log2((double)a.rope_theta) : 0.0;
+  g.window = window_of(a.n_rows, a.n_seqs);
+  const int heads = (a.q ? a.n_q_heads : 0) + 2 * p.n_kv_heads;
+  const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + RA_HEADS - 1) / RA_HEADS);
+  if (a.dtype == TS_DTYPE_BF16) launch_append_any<bf16_t>(g, grid, (hipStream_t)stream);
+  else launch_append_any<float>(g, grid, (hipStream_t)stream);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}
+
+template <typename TO>
+static void launch_read(const ReadArgs& g, dim3 grid, hipStream_t s) {
+  const ts_kv_pages& p = g.a.cache.pages;
+#define TS_READ(TC, HD) if (p.head_dim == HD) return k_kv_read<TC, TO, HD><<<grid, RA_THREADS, 0, s>>>(g)
+  if (p.dtype == TS_DTYPE_E4M3) { TS_READ(e4m3_t, 64); TS_READ(e4m3_t, 128); }
+  else if (p.dtype == TS_DTYPE_BF16) { TS_READ(bf16_t, 64); TS_READ(bf16_t, 128); }
+  else { TS_READ(float, 8); TS_READ(float, 16); TS_READ(float, 32); TS_READ(float, 64); TS_READ(float, 128); }
+#undef TS_READ
+}
+
+extern "C" ts_status ts_kv_read(const ts_kv_read_args* args, ts_stream stream) {
+  const char* call = "ts_kv_read";
+  if (!args) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  const ts_kv_read_args& a = *args;
+  const ts_kv_pages& p = a.cache.pages;
+  ts_status st = check_kv_pages_any(call, a.cache, a.table, a.table_stride, a.table_width, a.row_offsets, a.n_seqs, a.dtype);
+  if (st) return st;
+  if (a.n_rows < 0 || a.n_rows > (1 << 23)) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d rows outside [0, 2^23]", call, a.n_rows);
+  if (!aligned_to(a.starts, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned starts", call);
+  if (a.n_rows == 0 || (!a.k_out && !a.v_out)) return TS_OK;
+  const int64_t kv_row = (int64_t)p.n_kv_heads * p.head_dim;
+  if ((a.k_out && a.k_stride < kv_row) || (a.v_out && a.v_stride < kv_row)) return ts_fail(TS_ERR_INVALID_ARG, "%s: a row stride is below its row", call);
+  const int esz = ops_esz(a.dtype);
+  if (!aligned_to(a.k_out, esz) || !aligned_to(a.v_out, esz)) return ts_fail(TS_ERR_INVALID_ARG, "%s: rows are not aligned to their type", call);
+  int dev;
+  if ((st = ops_device(call, {p.k, p.v, a.cache.k_scales, a.cache.v_scales, a.table, a.starts, a.row_offsets, a.k_out, a.v_out}, stream, &dev))) return st;
+  DeviceGuard on(dev);
+  ReadArgs g{};
+  g.a = a;
+  g.window = window_of(a.n_rows, a.n_seqs);
+  const dim3 grid((a.n_rows + g.window - 1) / g.window, (2 * p.n_kv_heads + RA_HEADS - 1) / RA_HEADS);
+  if (a.dtype == TS_DTYPE_BF16) launch_read<bf16_t>(g, grid, (hipStream_t)stream);
+  else launch_read<float>(g, grid, (hipStream_t)stream);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}

@@ -1,0 +1,651 @@
+// Attention of chunks of rows over a paged cache of any type: causal chunks, windows, draft trees, single tokens.
+#include "ts_paged.h"
+
+// ---------------------------------------------------------------------------------
+// The rows of a chunk and the query heads that share a KV head are the columns of one problem: column m of (sequence, KV head) is
+// row m / group, head m % group, and all columns go over the same keys and values.  Tiles of 16 NT columns, one pass with a
+// running maximum and sum, four waves that take blocks of KB keys in turn, the cache's length split over workgroups
+// and joined where the tiles alone do not fill the card.
+//
+// Matrix instructions without any exchange between lanes: S^T = K Q^T puts 16 columns on the lanes (lane l: column l % 16) and four keys
+// of a tile in a lane's registers; O^T = V^T P^T wants eight (fp32: one) consecutive keys of a column in a lane.
+// Which key is which row of K's tile is free: row m of tile t takes key KB / 4 (m / 4) + 4 t + m % 4, and the probabilities that a
+// lane has computed are, in place, the operand it needs next.
+//
+// Where rows see different keys of a block, probabilities of unseen ones are zero, and zero times an infinite or NaN value
+// is not: such blocks are looked through, and values that are not finite are replaced by zeros and counted by indicator products,
+// so that they reach the rows that see them and no other.
+// ---------------------------------------------------------------------------------
+constexpr int RO_WAVES = 4;
+
+struct RowsArgs {
+  ts_kv_attend_rows_args a;
+  float scale_log2;                      // scores enter 2^x
+  int group, chunk, splits;              // query heads per KV head, keys per workgroup, workgroups per tile at most
+  int seq_tiles;                         // without offsets: tiles of a sequence's one row
+  float* part_o;                         // [n_rows][n_q_heads][splits][head_dim], relative to 2^m
+  float* part_ml;                        // [n_rows][n_q_heads][splits][2]
+};
+
+// the last i in [0, n) with f(i) <= key, -1 if none; f does not decrease.  64 at a time, one per lane.
+template <typename F>
+__device__ __forceinline__ int last_at_most(int n, int64_t key, F f) {
+  const int lane = threadIdx.x % 64;
+  int lo = 0, left = n;
+  for (;;) {
+    const int step = (left + 63) / 64, i = lane * step;
+    const int c = __popcll(__ballot(i < left && f(lo + (i < left ? i : 0)) <= key));
+    if (c == 0) return lo - 1;
+    if (step == 1) return lo + c - 1;
+    lo += (c - 1) * step + 1;
+    left = min(step - 1, left - (c - 1) * step - 1);
+    if (left <= 0) return lo - 1;
+  }
+}
+
+// a sequence's rows and where they are
+struct RowSeq {
+  int first, end;                        // rows, within [0, n_rows)
+  int64_t zero;                          // the position of row r is zero + r
+  int start;                             // position of the chunk's row 0, cut to +-2^30
+  int cap;                               // positions at or above are not seen
+};
+__device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int seq) {
+  RowSeq s;
+  const int64_t len = a.lengths[seq];
+  const int off = a.row_offsets ? a.row_offsets[seq] : seq;
+  s.end = a.row_offsets ? max(min(a.row_offsets[seq + 1], a.n_rows), 0) : seq + 1;
+  s.first = min(max(off, 0), a.n_rows);                      // both cut, so that their difference fits whatever the offsets are
+  s.zero = len - off;
+  s.start = (int)max((int64_t)-(1 << 30), min((int64_t)1 << 30, len));
+  s.cap = (int)min((int64_t)a.max_len, (int64_t)a.table_width * 16);
+  return s;
+}
+// positions [lo, hi) that a row can see (with ancestors: some of them)
+__device__ __forceinline__ int2 row_range(const ts_kv_attend_rows_args& a, const RowSeq& s, int row) {
+  const int64_t p = s.zero + row, up = a.ancestors ? s.zero + s.end : p + 1;
+  const int hi = (int)max((int64_t)0, min((int64_t)s.cap, up));
+  const int lo = a.window > 0 ? (int)max((int64_t)0, min((int64_t)hi, p + 1 - a.window)) : 0;
+  return make_int2(lo, hi);
+}
+
+template <typename T> struct RowsOf;     // keys of a block
+template <> struct RowsOf<bf16_t> { static constexpr int KB = 32; };
+template <> struct RowsOf<float> { static constexpr int KB = 32; };
+template <> struct RowsOf<e4m3_t> { static constexpr int KB = 64; };
+
+// eight e4m3 values as bf16, exactly
+__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true)));
+}
+__device__ __forceinline__ bool not_finite(uint32_t bf16_pair) {
+  return (bf16_pair & 0x7f80u) == 0x7f80u || (bf16_pair & 0x7f800000u) == 0x7f800000u;
+}
+// 0: +infinity, 1: -infinity, 2: NaN
+__device__ __forceinline__ bool of_class(uint32_t f32_bits, int cls) {
+  return cls == 0 ? f32_bits == 0x7f800000u : cls == 1 ? f32_bits == 0xff800000u : (f32_bits & 0x7fffffffu) > 0x7f800000u;
+}
+__device__ __forceinline__ float class_value(int cls) { return __uint_as_float(cls == 0 ? 0x7f800000u : cls == 1 ? 0xff800000u : 0x7fc00000u); }
+
+template <typename T, typename TQ, int HD, int NT>
+__global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_rows(RowsArgs g) {
+  constexpr bool F32 = sizeof(T) == 4, E8 = sizeof(T) == 1;
+  constexpr int KB = RowsOf<T>::KB, KT = KB / 16, KL = KB / 4, PG = KB / 16;   // keys of a block, tiles of them, keys of a lane, pages
+  constexpr int QP = !F32 && sizeof(TQ) == 4 ? 3 : 1;                          // terms of a query
+  constexpr int PP = !F32 && (sizeof(TQ) == 4 || NT == 1) ? 3 : 1;             // terms of a probability
+  constexpr int KC = (HD * (int)sizeof(T) + 63) / 64;                          // 16-byte pieces of a key per lane
+  constexpr int QS = F32 ? KC : HD / 32;                                       // steps of the products with a query
+  constexpr int DT = (HD + 15) / 16;                                           // tiles of 16 dimensions
+  constexpr int TM = 16 * NT, OS = DT * 16 + 4;
+  __shared__ float so[RO_WAVES * 16 * OS];
+  __shared__ float sm[RO_WAVES][16], sl[RO_WAVES][16];
+  const ts_kv_attend_rows_args& a = g.a;
+  const ts_kv_pages& pages = a.cache.pages;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 16, lg = lane / 16;
+  int id = blockIdx.x;
+  const int hkv = pages.n_kv_heads, kvh = id % hkv; id /= hkv;
+  const int split = id % g.splits, t = id / g.splits, G = g.group;
+  // Sequence s has tile slots [off G / TM + s, ...): as many as its tiles or one more, without a sum over the others.
+  int seq;
+  int64_t m0;
+  if (a.row_offsets) {
+    auto slot = [&](int s) { return ((int64_t)min(max(a.row_offsets[s], 0), a.n_rows) * G / TM) + s; };
+    seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, slot));
+    if (seq < 0) return;
+    m0 = (t - slot(seq)) * TM;
+  } else {
+    seq = t / g.seq_tiles;
+    m0 = (int64_t)(t - seq * g.seq_tiles) * TM;
+  }
+  const RowSeq rs = row_seq(a, seq);
+  const int64_t M = (int64_t)(rs.end - rs.first) * G;
+  if (m0 >= M) return;
+  const int cols = (int)min((int64_t)TM, M - m0), row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
+  const int2 low = row_range(a, rs, row0), high = row_range(a, rs, row0 + (rem + cols - 1) / G);
+  const int lo = low.x, hi = high.y;                         // what any column sees, and what all do
+  const int all_lo = high.x, all_hi = a.ancestors ? min(max(rs.start + 1, 0), low.y) : low.y;
+  const int64_t from = ((int64_t)(lo / g.chunk) + split) * g.chunk;
+  if (split > 0 && from >= hi) return;
+  const int k0 = (int)max(from, (int64_t)(lo & ~(KB - 1))), k1 = (int)min((int64_t)hi, from + g.chunk);
+
+  // columns: lane n of tile j
+  int c_lo[NT], c_hi[NT];
+  uint64_t c_set[NT];
+  uint4 q[NT][QP][QS];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int m = rem + min(j * 16 + n, cols - 1), row = row0 + m / G, head = kvh * G + m % G;
+    const int2 range = row_range(a, rs, row);
+    c_lo[j] = range.x; c_hi[j] = range.y;
+    c_set[j] = a.ancestors ? a.ancestors[row] : 0;
+    const TQ* src = (const TQ*)a.q + (int64_t)row * a.q_stride + (int64_t)head * HD;
+#pragma unroll
+    for (int c = 0; c < QS; ++c) {
+      constexpr int E = F32 ? 4 : 8;
+      float x[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = E8 ? (c / 2 * 4 + lg) * 16 + c % 2 * 8 + e : (c * 4 + lg) * E + e;
+        x[e] = d < HD ? widen(src[d < HD ? d : 0]) : 0.f;
+      }
+      if constexpr (!F32) {
+        uint32_t u[QP][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ts_bf16x2 w[QP];
+          split_bf16x2_nonzero<QP>(x[2 * e], x[2 * e + 1], w);
+#pragma unroll
+          for (int p = 0; p < QP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, w[p]);
+        }
+#pragma unroll
+        for (int p = 0; p < QP; ++p) q[j][p][c] = make_uint4(u[p][0], u[p][1], u[p][2], u[p][3]);
+      } else {
+        q[j][0][c] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+      }
+    }
+  }
+
+  ts_f32x4 o[NT][DT];
+  float m[NT], l[NT];                                        // l: of this lane's keys only
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    m[j] = -INFINITY; l[j] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[j][d] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int32_t* table = a.table + (int64_t)seq * a.table_stride;
+  const char* kp = (const char*)pages.k;
+  const char* vp = (const char*)pages.v;
+  const int64_t head_bytes = (int64_t)16 * HD * sizeof(T), page_bytes = hkv * head_bytes;
+
+  struct Pages { int p[PG]; };
+  struct Block { uint4 k[KT][KC], v[F32 ? 2 : 1][DT], ks, vs; bool ok[PG]; };
+  auto pages_of = [&](int kb) {                              // the later ones may lie behind the last position
+    Pages p;
+#pragma unroll
+    for (int i = 0; i < PG; ++i) p.p[i] = kb + 16 * i < hi ? table[kb / 16 + i] : -1;
+    return p;
+  };
+  auto fetch = [&](Block& f, const Pages& pg) {              // pages that do not exist: another is read, and masked
+    int64_t at[PG];
+    int some = 0;
+#pragma unroll
+    for (int i = 0; i < PG; ++i) {
+      f.ok[i] = pg.p[i] >= 0 && pg.p[i] < pages.n_pages;
+      some = f.ok[i] ? pg.p[i] : some;
+      at[i] = some * page_bytes + kvh * head_bytes;
+    }
+    auto pick = [&](int i) { return PG == 2 ? (i == 0 ? at[0] : at[1]) : (i < 2 ? (i == 0 ? at[0] : at[1]) : (i == 2 ? at[2] : at[PG - 1])); };
+    const int64_t mine = PG == 4 ? pick(n / 4) : pick(n / 8);          // bf16 and 8 bits: the page of this lane's key
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+      const int key = F32 ? 16 * t + n : KL * (n / 4) + 4 * t + n % 4;
+      const char* row = kp + (F32 ? at[t] : mine) + key % 16 * HD * (int)sizeof(T);
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int b = (c * 4 + lg) * 16;
+        if (HD * (int)sizeof(T) % 64 == 0 || b < HD * (int)sizeof(T)) f.k[t][c] = *reinterpret_cast<const uint4*>(row + b);
+        else f.k[t][c] = make_uint4(0, 0, 0, 0);
+      }
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          if (HD % 16 == 0 || d * 16 + n < HD) f.v[t][d] = *reinterpret_cast<const uint4*>(vp + at[t] + (d * 16 + n) * 64 + lg * 16);
+          else f.v[t][d] = make_uint4(0, 0, 0, 0);
+        }
+    } else if constexpr (E8) {
+      const int64_t own = pick(lg);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) f.v[0][d] = *reinterpret_cast<const uint4*>(vp + own + (d * 16 + n) * 16);
+      f.ks = *reinterpret_cast<const uint4*>(a.cache.k_scales + own / HD);      // 16 HD bytes of codes to 16 of scales
+      f.vs = *reinterpret_cast<const uint4*>(a.cache.v_scales + own / HD);
+    } else {
+      const char* col = vp + pick(lg / 2) + (lg & 1) * 16;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) f.v[0][d] = *reinterpret_cast<const uint4*>(col + (d * 16 + n) * 32);
+    }
+  };
+  auto use = [&](Block& f, int kb) {
+    ts_f32x4 s[NT][KT];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) s[j][t] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < QS; ++c) {
+        if constexpr (F32) {
+          const ts_f32x4 kx = __builtin_bit_cast(ts_f32x4, f.k[t][c]);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const ts_f32x4 qx = __builtin_bit_cast(ts_f32x4, q[j][0][c]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], s[j][t], 0, 0, 0);
+          }
+        } else {
+          uint4 kx;
+          if constexpr (E8) kx = c % 2 ? widen8(f.k[t][c / 2].z, f.k[t][c / 2].w) : widen8(f.k[t][c / 2].x, f.k[t][c / 2].y);
+          else kx = f.k[t][c];
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int p = QP - 1; p >= 0; --p)
+              s[j][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, kx), __builtin_bit_cast(ts_bf16x8, q[j][p][c]), s[j][t], 0, 0, 0);
+        }
+      }
+    }
+    auto key_of = [&](int i) { return kb + (F32 ? 16 * (i / 4) + 4 * lg + i % 4 : KL * lg + i); };      // a lane's i-th key
+    bool whole = kb >= all_lo && kb + KB <= min(all_hi, k1);
+#pragma unroll
+    for (int i = 0; i < PG; ++i) whole = whole && f.ok[i];
+    uint32_t keep[NT];
+    uint32_t pk[NT][PP][KL / 2];                             // probabilities as pairs of bf16 terms
+    float px[F32 ? NT : 1][F32 ? KL : 1];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      float x[KL];
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        float scale = g.scale_log2;
+        if constexpr (E8) scale *= scale_of((i < 8 ? (i < 4 ? f.ks.x : f.ks.y) : (i < 12 ? f.ks.z : f.ks.w)) >> i % 4 * 8 & 255);
+        x[i] = s[j][i / 4][i % 4] * scale;
+      }
+      if (!whole) {
+        keep[j] = 0;
+#pragma unroll
+        for (int i = 0; i < KL; ++i) {
+          const int key = key_of(i), own = key - rs.start;
+          bool in = key >= c_lo[j] && key < min(c_hi[j], k1);
+          if (F32) in = in && f.ok[i / 4];
+          else if (E8) in = in && (lg < 2 ? (lg == 0 ? f.ok[0] : f.ok[1]) : (lg == 2 ? f.ok[2 % PG] : f.ok[3 % PG]));
+          else in = in && (lg < 2 ? f.ok[0] : f.ok[1]);
+          if (a.ancestors) in = in && (own <= 0 || (own <= 64 && (c_set[j] >> (own - 1 & 63) & 1)));
+          x[i] = in ? x[i] : -INFINITY;
+          keep[j] |= in ? 1u << i : 0;
+        }
+      }
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < KL; ++i) top = fmaxf(top, x[i]);
+      top = fmaxf(max_over_lane_groups(top), m[j]);
+      if (__ballot(top > m[j])) {                            // the sums so far move to the new reference
+        const float w = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - top);
+        l[j] *= w;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[j][d] *= w;
+        m[j] = top;
+      }
+      const float ref = m[j] == -INFINITY ? 0.f : m[j];
+#pragma unroll
+      for (int i = 0; i < KL; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
+        l[j] += x[i];
+        if constexpr (E8) {
+          x[i] *= scale_of((i < 8 ? (i < 4 ? f.vs.x : f.vs.y) : (i < 12 ? f.vs.z : f.vs.w)) >> i % 4 * 8 & 255);
+          if (!whole) x[i] = keep[j] >> i & 1 ? x[i] : 0.f;            // the scale of what is not seen may be NaN
+        }
+      }
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < KL; ++i) px[j][i] = x[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < KL / 2; ++i) {
+          ts_bf16x2 w[PP];
+          if constexpr (PP == 1) w[0] = to_bf16x2(x[2 * i], x[2 * i + 1]);
+          else split_bf16x2_nonzero<PP>(x[2 * i], x[2 * i + 1], w);
+#pragma unroll
+          for (int p = 0; p < PP; ++p) pk[j][p][i] = __builtin_bit_cast(uint32_t, w[p]);
+        }
+      }
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint32_t v[4] = {f.v[t][d].x, f.v[t][d].y, f.v[t][d].z, f.v[t][d].w};
+          if (!whole && __ballot((v[0] & 0x7f800000u) == 0x7f800000u || (v[1] & 0x7f800000u) == 0x7f800000u || (v[2] & 0x7f800000u) == 0x7f800000u ||
+                                 (v[3] & 0x7f800000u) == 0x7f800000u)) {
+            for (int cls = 0; cls < 3; ++cls)
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                ts_f32x4 hit = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                  hit = __builtin_amdgcn_mfma_f32_16x16x4f32(of_class(v[r], cls) ? 1.f : 0.f, keep[j] >> (4 * t + r) & 1 ? 1.f : 0.f, hit, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[j][d][r] += hit[r] > 0.f ? class_value(cls) : 0.f;
+              }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) v[r] = (v[r] & 0x7f800000u) == 0x7f800000u ? 0 : v[r];
+          }
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[j][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[r]), px[j][4 * t + r], o[j][d], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int u = 0; u < KB / 32; ++u)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          uint4 v;
+          if constexpr (E8) v = u ? widen8(f.v[0][d].z, f.v[0][d].w) : widen8(f.v[0][d].x, f.v[0][d].y);
+          else v = f.v[0][d];
+          if (!whole && __ballot(not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w))) {
+            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            for (int cls = 0; cls < 3; ++cls) {
+              uint32_t is[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) is[e] = (of_class(w[e] << 16, cls) ? 0x3f80u : 0) | (of_class(w[e] & 0xffff0000u, cls) ? 0x3f800000u : 0);
+#pragma unroll
+              for (int j = 0; j < NT; ++j) {
+                uint32_t in[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) in[e] = (keep[j] >> (8 * u + 2 * e) & 1 ? 0x3f80u : 0) | (keep[j] >> (8 * u + 2 * e + 1) & 1 ? 0x3f800000u : 0);
+                const ts_f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, make_uint4(is[0], is[1], is[2], is[3])),
+                                                                              __builtin_bit_cast(ts_bf16x8, make_uint4(in[0], in[1], in[2], in[3])), ts_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[j][d][r] += hit[r] > 0.f ? class_value(cls) : 0.f;
+              }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] &= ((w[e] & 0x7f80u) == 0x7f80u ? 0 : 0xffffu) | ((w[e] & 0x7f800000u) == 0x7f800000u ? 0 : 0xffff0000u);
+            v = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int p = PP - 1; p >= 0; --p)
+              o[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, v),
+                                                                __builtin_bit_cast(ts_bf16x8, make_uint4(pk[j][p][4 * u], pk[j][p][4 * u + 1], pk[j][p][4 * u + 2], pk[j][p][4 * u + 3])), o[j][d], 0, 0, 0);
+        }
+    }
+  };
+  // The next block is requested before one is used; past the end the last is requested again, since the waits count the loads
+  // behind the ones they wait for.
+  constexpr int STEP = RO_WAVES * KB;
+  const int kw = k0 + wave * KB;
+  if (kw + STEP >= k1) {
+    if (kw < k1) {
+      Block f;
+      fetch(f, pages_of(kw));
+      use(f, kw);
+    }
+  } else if constexpr (NT * HD <= 256 && !(F32 && HD == 128)) {
+    const int last = kw + (k1 - 1 - kw) / STEP * STEP;
+    Block fa, fb;
+    fetch(fa, pages_of(kw));
+    Pages next = pages_of(kw + STEP);
+    for (int kb = kw; kb < k1; kb += 2 * STEP) {
+      fetch(fb, next);
+      next = pages_of(min(kb + 2 * STEP, last));
+      use(fa, kb);
+      if (kb + STEP >= k1) break;
+      fetch(fa, next);
+      next = pages_of(min(kb + 3 * STEP, last));
+      use(fb, kb + STEP);
+    }
+  } else {
+    Pages next = pages_of(kw);
+    for (int kb = kw; kb < k1; kb += STEP) {
+      Block f;
+      fetch(f, next);
+      next = pages_of(kb + STEP);
+      use(f, kb);
+    }
+  }
+
+  // the four waves' parts, a tile of columns at a time
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    if (j * 16 >= cols) break;
+    if (j) __syncthreads();
+    l[j] += __shfl_xor(l[j], 16, 64);
+    l[j] += __shfl_xor(l[j], 32, 64);
+    if (lane < 16) { sm[wave][n] = m[j]; sl[wave][n] = l[j]; }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<ts_f32x4*>(&so[(wave * 16 + n) * OS + d * 16 + lg * 4]) = o[j][d];
+    __syncthreads();
+    for (int i = tid; i < min(16, cols - j * 16) * HD; i += RO_WAVES * 64) {
+      const int c = i / HD, d = i % HD, mc = rem + j * 16 + c, row = row0 + mc / G, head = kvh * G + mc % G;
+      float top = sm[0][c];
+#pragma unroll
+      for (int w = 1; w < RO_WAVES; ++w) top = fmaxf(top, sm[w][c]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, val = 0.f;
+#pragma unroll
+      for (int w = 0; w < RO_WAVES; ++w) {
+        const float x = __builtin_amdgcn_exp2f(sm[w][c] - ref);
+        sum += x * sl[w][c];
+        val += x * so[(w * 16 + c) * OS + d];
+      }
+      const int64_t at = (int64_t)row * a.n_q_heads + head;
+      if (g.splits == 1) {
+        st_from_f32((TQ*)a.out + (int64_t)row * a.out_stride + (int64_t)head * HD + d, sum == 0.f ? 0.f : val / sum);
+        if (a.lse && d == 0) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+      } else {
+        const int64_t part = at * g.splits + (lo / g.chunk + split) % g.splits;
+        g.part_o[part * HD + d] = val;
+        if (d == 0) *reinterpret_cast<float2*>(g.part_ml + part * 2) = make_float2(top, sum);
+      }
+    }
+  }
+}
+
+// The join of a row's splits: chunk c of the cache's positions lies at place c % splits.  A workgroup per (row, head), four
+// dimensions a thread, the splits dealt to the rows of threads.
+constexpr int RO_SPLITS = 512;                               // at most, see rows_cut
+template <typename TQ, int HD>
+__global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
+  constexpr int COLS = HD / 4, ROWS = 256 / COLS;
+  __shared__ float sw[RO_SPLITS + 1];
+  __shared__ float4 sv[256];
+  __shared__ float red[2][4];
+  const ts_kv_attend_rows_args& a = g.a;
+  const int tid = threadIdx.x, wave = tid / 64, h = blockIdx.x % a.n_q_heads, row = blockIdx.x / a.n_q_heads;
+  int seq = row;
+  if (a.row_offsets) {
+    seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
+    if (seq < 0 || seq >= a.n_seqs || row >= a.row_offsets[seq + 1]) return;
+  }
+  const RowSeq rs = row_seq(a, seq);
+  const int2 range = row_range(a, rs, row);
+  const int c0 = range.x / g.chunk, used = max(1, (range.y + g.chunk - 1) / g.chunk - c0);       // a row that sees nothing: one empty part
+  const int64_t at = (int64_t)row * a.n_q_heads + h;
+  const float2* ml = reinterpret_cast<const float2*>(g.part_ml) + at * g.splits;
+  float top = -INFINITY;
+  for (int i = tid; i < used; i += 256) top = fmaxf(top, ml[(c0 + i) % g.splits].x);
+  top = wave_max(top);
+  if (tid % 64 == 0) red[0][wave] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+  for (int i = tid; i < used; i += 256) {
+    const float2 p = ml[(c0 + i) % g.splits];
+    const float f = __builtin_amdgcn_exp2f(p.x - ref);
+    sw[i] = f;
+    sum += f * p.y;
+  }
+  sum = wave_sum(sum);
+  if (tid % 64 == 0) red[1][wave] = sum;
+  __syncthreads();
+  sum = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+  const int d = tid % COLS, r = tid / COLS;
+  const float4* part = reinterpret_cast<const float4*>(g.part_o) + at * g.splits * COLS + d;
+  float4 val = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int i = r; i < used; i += ROWS) {
+    const float4 v = part[(int64_t)((c0 + i) % g.splits) * COLS];
+    const float f = sw[i];
+    val.x += f * v.x; val.y += f * v.y; val.z += f * v.z; val.w += f * v.w;
+  }
+  sv[tid] = val;
+  __syncthreads();
+  if (tid >= HD) return;
+  const float* sc = reinterpret_cast<const float*>(sv);
+  float out = 0.f;
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) out += sc[i * HD + tid];
+  st_from_f32((TQ*)a.out + (int64_t)row * a.out_stride + (int64_t)h * HD + tid, sum == 0.f ? 0.f : out / sum);
+  if (a.lse && tid == 0) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+}
+
+// ---------------------------------------------------------------------------------
+// entry points
+// ---------------------------------------------------------------------------------
+constexpr int RO_CUS = 256, RO_UNIT = 128;
+
+struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup, keys of a split, splits, tile slots per KV head
+
+// Tiles of 16 columns where a sequence has no more, of 64 (fp32: 32) where it has.
+static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : 4; }
+static int64_t rows_units(int max_len, int window) {         // of 128 keys, in what one tile sees
+  const int64_t span = window > 0 && (int64_t)window + 64 < max_len ? window + 64 : max_len;
+  return std::max<int64_t>(1, (span + RO_UNIT - 1) / RO_UNIT);
+}
+// workgroups without a split
+static int64_t rows_whole(int64_t n_seqs, int64_t n_rows, int group, int hkv, int nt) {
+  return std::max<int64_t>(n_seqs, (n_rows * group + 16 * nt - 1) / (16 * nt)) * hkv;
+}
+static int64_t rows_room(int64_t n_seqs, int64_t n_rows, int group, int hkv, int max_len, int window) {
+  int64_t room = 1;
+  for (int nt : {1, 2, 4}) room = std::max(room, std::min(rows_units(max_len, window), 2 * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
+  return room > 1 && window > 0 ? room + 1 : room;
+}
+static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
+  const int group = a.n_q_heads / a.cache.pages.n_kv_heads, hkv = a.cache.pages.n_kv_heads;
+  RowsCut c;
+  c.nt = rows_nt(a.n_seqs, a.n_rows, group, a.cache.pages.dtype == TS_DTYPE_F32 || a.dtype == TS_DTYPE_F32);
+  const int tm = 16 * c.nt;
+  c.slots = a.row_offsets ? (int64_t)a.n_rows * group / tm + a.n_seqs : (int64_t)a.n_seqs * ((group + tm - 1) / tm);
+  const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), unit = a.cache.pages.dtype == TS_DTYPE_E4M3 ? 2 : 1;
+  const int64_t units = (rows_units(a.max_len, a.window) + unit - 1) / unit;
+  int64_t per = 1;
+  if (units * whole > 2 * RO_CUS) {
+    const int64_t want = std::max<int64_t>(1, RO_CUS / whole);
+    per = (units + want - 1) / want;
+  }
+  if (units <= 2) per = units;
+  c.chunk = (int)(per * unit * RO_UNIT);
+  c.splits = (int)((units + per - 1) / per);
+  if (c.splits == 1) c.chunk = 1 << 30;                      // one chunk, wherever a window lies
+  else if (a.window > 0) ++c.splits;
+  return c;
+}
+
+static ts_status check_rows(const char* call, int32_t n_seqs, int32_t n_rows, int32_t hq, int32_t hkv, int32_t max_len, int32_t window) {
+  if (n_seqs < 1 || n_seqs > (1 << 20)) return ts_fail(TS_ERR_INVALID_ARG, "%s: n_seqs %d outside [1, 2^20]", call, n_seqs);
+  if (n_rows < 0 || n_rows > (1 << 23)) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d rows outside [0, 2^23]", call, n_rows);
+  if (hkv < 1 || hkv > 65536 || hq < 1 || hq > 65536 || hq % hkv) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d query heads over %d KV heads", call, hq, hkv);
+  if (max_len < 0 || max_len > (1 << 30)) return ts_fail(TS_ERR_INVALID_ARG, "%s: max_len %d outside [0, 2^30]", call, max_len);
+  if (window < 0) return ts_fail(TS_ERR_INVALID_ARG, "%s: window %d is negative", call, window);
+  const int64_t slots = (int64_t)n_rows * (hq / hkv) / 16 + (int64_t)n_seqs * ((hq / hkv + 15) / 16);
+  constexpr int64_t kMost = (1 << 24) - 1;                   // workgroups of 256 whose threads a launch can count
+  if (slots * hkv * rows_room(n_seqs, n_rows, hq / hkv, hkv, max_len, window) > kMost || (int64_t)n_rows * hq > kMost)
+    return ts_fail(TS_ERR_INVALID_ARG, "%s: %d rows of %d sequences and %d heads are too many for one call", call, n_rows, n_seqs, hq);
+  return TS_OK;
+}
+
+extern "C" ts_status ts_kv_attend_rows_workspace(int32_t n_seqs, int32_t n_rows, int32_t hq, int32_t hkv, int32_t head_dim, int32_t max_len, int32_t window,
+                                                 uint64_t* bytes) {
+  const char* call = "ts_kv_attend_rows_workspace";
+  if (!bytes) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  ts_status st = check_rows(call, n_seqs, n_rows, hq, hkv, max_len, window);
+  if (st) return st;
+  if (head_dim < 8 || head_dim > 128) return ts_fail(TS_ERR_INVALID_ARG, "%s: head_dim %d", call, head_dim);
+  const int64_t room = rows_room(n_seqs, n_rows, hq / hkv, hkv, max_len, window);
+  *bytes = room > 1 ? (uint64_t)n_rows * hq * room * (head_dim + 2) * 4 : 0;
+  return TS_OK;
+}
+
+template <typename T, typename TQ, int HD>
+static void launch_rows(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
+  constexpr int BIG = sizeof(T) == 4 || sizeof(TQ) == 4 ? 2 : 4;
+  const uint32_t grid = (uint32_t)(c.slots * g.a.cache.pages.n_kv_heads * c.splits);
+  if (c.nt == 1) k_kv_attend_rows<T, TQ, HD, 1><<<grid, RO_WAVES * 64, 0, s>>>(g);
+  else k_kv_attend_rows<T, TQ, HD, BIG><<<grid, RO_WAVES * 64, 0, s>>>(g);
+  if (c.splits > 1) k_kv_attend_rows_join<TQ, HD><<<(uint32_t)(g.a.n_rows * g.a.n_q_heads), 256, 0, s>>>(g);
+}
+template <typename TQ>
+static void launch_rows_q(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
+  const ts_kv_pages& p = g.a.cache.pages;
+#define TS_ROWS(T, HD) if (p.head_dim == HD) return launch_rows<T, TQ, HD>(g, c, s)
+  if (p.dtype == TS_DTYPE_E4M3) { TS_ROWS(e4m3_t, 64); TS_ROWS(e4m3_t, 128); }
+  else if (p.dtype == TS_DTYPE_BF16) { TS_ROWS(bf16_t, 64); TS_ROWS(bf16_t, 128); }
+  else { TS_ROWS(float, 8); TS_ROWS(float, 16); TS_ROWS(float, 32); TS_ROWS(float, 64); TS_ROWS(float, 128); }
+#undef TS_ROWS
+}
+
+extern "C" ts_status ts_kv_attend_rows(const ts_kv_attend_rows_args* args, ts_stream stream) {
+  const char* call = "ts_kv_attend_rows";
+  if (!args) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  const ts_kv_attend_rows_args& a = *args;
+  const ts_kv_pages& p = a.cache.pages;
+  ts_status st = check_kv_pages_any(call, a.cache, a.table, a.table_stride, a.table_width, a.lengths, a.n_seqs, a.dtype);
+  if (st) return st;
+  if ((st = check_rows(call, a.n_seqs, a.n_rows, a.n_q_heads, p.n_kv_heads, a.max_len, a.window))) return st;
+  if (!a.row_offsets && a.n_rows < a.n_seqs) return ts_fail(TS_ERR_INVALID_ARG, "%s: %d rows for %d sequences", call, a.n_rows, a.n_seqs);
+  if (!aligned_to(a.row_offsets, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned row_offsets", call);
+  if (!aligned_to(a.ancestors, 8)) return ts_fail(TS_ERR_INVALID_ARG, "%s: misaligned ancestors", call);
+  if (a.ancestors && a.window) return ts_fail(TS_ERR_INVALID_ARG, "%s: window and ancestors exclude each other", call);
+  if (!(fabsf(a.scale) < INFINITY)) return ts_fail(TS_ERR_INVALID_ARG, "%s: scale must be finite", call);
+  if (a.n_rows == 0) return TS_OK;
+  if (!a.q || !a.out) return ts_fail(TS_ERR_INVALID_ARG, "%s: null argument", call);
+  const int64_t q_row = (int64_t)a.n_q_heads * p.head_dim;
+  if (a.q_stride < q_row || a.out_stride < q_row) return ts_fail(TS_ERR_INVALID_ARG, "%s: a row stride is below its row", call);
+  const int esz = ops_esz(a.dtype);
+  if (!aligned_to(a.q, esz) || !aligned_to(a.out, esz) || !aligned_to(a.lse, 4)) return ts_fail(TS_ERR_INVALID_ARG, "%s: rows are not aligned to their type", call);
+  const RowsCut c = rows_cut(a);
+  if (c.splits > 1) {
+    uint64_t need = 0;
+    if ((st = ts_kv_attend_rows_workspace(a.n_seqs, a.n_rows, a.n_q_heads, p.n_kv_heads, p.head_dim, a.max_len, a.window, &need))) return st;
+    if (!a.workspace || a.workspace_bytes < need || !aligned_to(a.workspace, 16))
+      return ts_fail(TS_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %llu bytes, got %llu", call, (unsigned long long)need, (unsigned long long)a.workspace_bytes);
+  }
+  int dev;
+  if ((st = ops_device(call, {p.k, p.v, a.cache.k_scales, a.cache.v_scales, a.table, a.lengths, a.row_offsets, a.ancestors, a.q, a.out, a.lse, c.splits > 1 ? a.workspace : nullptr},
+                       stream, &dev))) return st;
+  DeviceGuard on(dev);
+  RowsArgs g{};
+  g.a = a;
+  g.scale_log2 = a.scale * 1.4426950408889634f;
+  g.group = a.n_q_heads / p.n_kv_heads;
+  g.chunk = c.chunk;
+  g.splits = c.splits;
+  g.seq_tiles = (g.group + 16 * c.nt - 1) / (16 * c.nt);
+  g.part_o = (float*)a.workspace;
+  g.part_ml = g.part_o + (int64_t)a.n_rows * a.n_q_heads * c.splits * p.head_dim;
+  if (a.dtype == TS_DTYPE_BF16) launch_rows_q<bf16_t>(g, c, (hipStream_t)stream);
+  else launch_rows_q<float>(g, c, (hipStream_t)stream);
+  TS_HIP(hipGetLastError());
+  return TS_OK;
+}

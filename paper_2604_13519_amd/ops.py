@@ -17,8 +17,10 @@ from . import binding
 from .binding import TS_DTYPE_BF16, TS_DTYPE_F32, TS_PAGE_SIZE
 
 EXPORTS = ("ts_mx_quantize", "ts_mx_dequantize", "ts_mx_packed_bytes", "ts_mx_pack", "ts_mx_project", "ts_kv_layer_pages", "ts_kv_page_table",
-           "ts_kv_extend", "ts_kv_append", "ts_kv_attend", "ts_kv_attend_workspace")
+           "ts_kv_extend", "ts_kv_append", "ts_kv_attend", "ts_kv_attend_workspace", "ts_kv_append_norm_rope", "ts_kv_read", "ts_kv_attend_rows",
+           "ts_kv_attend_rows_workspace")
 
+TS_DTYPE_E4M3 = 3                                          # pages of 8-bit values
 _DTYPES = {torch.float32: TS_DTYPE_F32, torch.bfloat16: TS_DTYPE_BF16}
 _RECORD = 16 * 4 * 17                                      # bytes of packed weights per 16 rows and 128 columns
 
@@ -42,6 +44,34 @@ class ts_kv_attend_args(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
 
 
+class ts_kv_pages_any(C.Structure):
+    _fields_ = [("pages", ts_kv_pages), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p)]
+
+
+class ts_kv_append_norm_rope_args(C.Structure):
+    _fields_ = [("cache", ts_kv_pages_any), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int32),
+                ("lengths", C.c_void_p), ("row_offsets", C.c_void_p), ("positions", C.c_void_p),
+                ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("n_q_heads", C.c_int32), ("dtype", C.c_int32),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("k", C.c_void_p), ("k_stride", C.c_int64), ("v", C.c_void_p), ("v_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("q_out_stride", C.c_int64), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p),
+                ("norm_dtype", C.c_int32), ("norm_eps", C.c_float), ("rope_freqs", C.c_void_p), ("rope_theta", C.c_float), ("rope_magnitude", C.c_float),
+                ("rope_dim", C.c_int32), ("rope_pairs", C.c_int32)]
+
+
+class ts_kv_read_args(C.Structure):
+    _fields_ = [("cache", ts_kv_pages_any), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int32),
+                ("starts", C.c_void_p), ("row_offsets", C.c_void_p), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("dtype", C.c_int32),
+                ("k_out", C.c_void_p), ("k_stride", C.c_int64), ("v_out", C.c_void_p), ("v_stride", C.c_int64)]
+
+
+class ts_kv_attend_rows_args(C.Structure):
+    _fields_ = [("cache", ts_kv_pages_any), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int32),
+                ("lengths", C.c_void_p), ("row_offsets", C.c_void_p), ("ancestors", C.c_void_p),
+                ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("max_len", C.c_int32), ("window", C.c_int32), ("n_q_heads", C.c_int32), ("dtype", C.c_int32),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("out", C.c_void_p), ("out_stride", C.c_int64), ("lse", C.c_void_p), ("scale", C.c_float),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64)]
+
+
 def _packer(cls):
     """Packs the members of a structure, those of its own structures in place: a quarter of the time that building the structure takes."""
     def codes(c):
@@ -52,6 +82,7 @@ def _packer(cls):
 
 
 _pack_append, _pack_attend = _packer(ts_kv_append_args), _packer(ts_kv_attend_args)
+_pack_append_norm_rope, _pack_read, _pack_rows = _packer(ts_kv_append_norm_rope_args), _packer(ts_kv_read_args), _packer(ts_kv_attend_rows_args)
 _lib = None
 
 
@@ -77,6 +108,10 @@ def _load():
             "ts_kv_append": [p, p],
             "ts_kv_attend": [p, p],
             "ts_kv_attend_workspace": [i32, i32, i32, i32, i32, i32, C.POINTER(C.c_uint64)],
+            "ts_kv_append_norm_rope": [p, p],
+            "ts_kv_read": [p, p],
+            "ts_kv_attend_rows": [p, p],
+            "ts_kv_attend_rows_workspace": [i32, i32, i32, i32, i32, i32, i32, C.POINTER(C.c_uint64)],
         }.items():
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = args, i32
@@ -342,4 +377,172 @@ def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=N
     except struct.error as e:
         _out_of_range(e)
     binding._check(lib.ts_kv_attend(a, _stream(q)))
+    return out, lse
+
+
+# ---- more rows, other rotations, 8-bit pages ----------------------------------------------
+def _any_pages(k_pages, v_pages, scales):
+    """The members of a ts_kv_pages_any: pages of fp32 or bf16 (or a library cache's layer) without scales, or of float8_e4m3fn with (k_scales, v_scales)."""
+    if v_pages is None or k_pages.dtype is not torch.float8_e4m3fn:
+        if scales is not None:
+            _refuse("scales belong to float8_e4m3fn pages")
+        return _pages(k_pages, v_pages) + (0, 0)
+    ks = k_pages.shape
+    if len(ks) != 4 or ks[2] != TS_PAGE_SIZE or not k_pages.is_contiguous() or not v_pages.is_contiguous() or not k_pages.is_cuda or not v_pages.is_cuda:
+        _refuse("k_pages: a contiguous [pages][heads][%d][head_dim] tensor on a GPU is needed, got %s", TS_PAGE_SIZE, tuple(ks))
+    n, h, _, hd = ks
+    if v_pages.shape != (n, h, hd, TS_PAGE_SIZE):
+        _refuse("v_pages: shape %s is needed, got %s", (n, h, hd, TS_PAGE_SIZE), tuple(v_pages.shape))
+    if v_pages.dtype is not torch.float8_e4m3fn:
+        raise TypeError("pages: two of one type are needed, got %s and %s" % (k_pages.dtype, v_pages.dtype))
+    if scales is None or len(scales) != 2:
+        _refuse("scales: (k_scales, v_scales) are needed with float8_e4m3fn pages")
+    shape = (n, h, TS_PAGE_SIZE)
+    return k_pages.data_ptr(), v_pages.data_ptr(), n, h, hd, TS_DTYPE_E4M3, _bytes(scales[0], "k_scales", shape), _bytes(scales[1], "v_scales", shape)
+
+
+def _gain(t, name, hd, dtype):
+    if t is None:
+        return 0
+    if t.dtype not in _DTYPES or (dtype is not None and t.dtype is not dtype):
+        raise TypeError("%s: %s is needed, got %s" % (name, dtype or "float32 or bfloat16", t.dtype))
+    if t.shape != (hd,) or not t.is_contiguous() or not t.is_cuda:
+        _refuse("%s: %d contiguous values on a GPU are needed, got %s", name, hd, tuple(t.shape))
+    if t.requires_grad:
+        _no_gradient(name)
+    return t.data_ptr()
+
+
+def ts_kv_append_norm_rope(k_pages, v_pages, table, lengths, row_offsets, q, k, v, rope_theta=0.0, rope_dim=None, rope_pairs=False, rope_freqs=None,
+                           rope_magnitude=1.0, q_norm=None, k_norm=None, norm_eps=1e-6, positions=None, scales=None, q_out=None):
+    """ts_kv_append with norms of the heads (gains q_norm, k_norm [head_dim]), rotations of the first rope_dim values (None: all) in halves or
+    neighbouring pairs, by theta or a table rope_freqs (fp32 [rope_dim / 2], radians per position), at the rows' positions or at given ones
+    (int32 [rows]), and into pages of any type (float8_e4m3fn pages: scales = (k_scales, v_scales), uint8 [pages][heads][16]).  Returns
+    the queries as rotated (q_out; zeros where a row belongs to no sequence).  See the header."""
+    lib = _lib or _load()
+    pages = _any_pages(k_pages, v_pages, scales)
+    n, kv_heads, hd = row_offsets.shape[0] - 1, pages[3], pages[4]
+    table, t_stride, t_width = _table(table, n)
+    width = kv_heads * hd
+    pk, k_stride = _rows(k, "k", width)
+    dtype, rows = k.dtype, k.shape[0]
+    pv, v_stride = _rows(v, "v", width, dtype)
+    if v.shape[0] != rows:
+        _refuse("v: %d rows are needed, got %d", rows, v.shape[0])
+    pq, q_stride, po, o_stride, heads = 0, 0, 0, 0, 0
+    if q is not None:
+        pq, q_stride = _rows(q, "q", None, dtype)
+        q_rows, q_width = q.shape
+        if q_rows != rows or q_width < 1 or q_width % hd:
+            _refuse("q: %d rows of a multiple of %d values are needed, got %s", rows, hd, tuple(q.shape))
+        if q_out is None:
+            q_out = torch.zeros(q.shape, dtype=dtype, device=q.device)
+        po, o_stride = _rows(q_out, "q_out", q_width, dtype)
+        if q_out.shape[0] != rows:
+            _refuse("q_out: %d rows are needed, got %d", rows, q_out.shape[0])
+        heads = q_width // hd
+    elif q_out is not None or q_norm is not None:
+        _refuse("q_out or q_norm without q")
+    if rope_dim is None:
+        rope_dim = hd
+    norm_type = q_norm.dtype if q_norm is not None else None
+    pqn, pkn = _gain(q_norm, "q_norm", hd, None), _gain(k_norm, "k_norm", hd, norm_type)
+    if k_norm is not None:
+        norm_type = k_norm.dtype
+    freqs = 0
+    if rope_freqs is not None:
+        if rope_freqs.dtype is not torch.float32 or not rope_freqs.is_cuda or rope_freqs.dim() != 1 or not rope_freqs.is_contiguous() or rope_freqs.shape[0] * 2 != rope_dim:
+            _refuse("rope_freqs: %d contiguous fp32 on a GPU are needed, got %s %s", rope_dim // 2, rope_freqs.dtype, tuple(rope_freqs.shape))
+        if rope_freqs.requires_grad:
+            _no_gradient("rope_freqs")
+        freqs = rope_freqs.data_ptr()
+    try:
+        a = _pack_append_norm_rope(*pages, table, t_stride, t_width, _ints(lengths, "lengths", n), _ints(row_offsets, "row_offsets", 2),
+                                   0 if positions is None else _ints(positions, "positions", rows), n, rows, heads, _DTYPES[dtype], pq, q_stride, pk, k_stride,
+                                   pv, v_stride, po, o_stride, pqn, pkn, _DTYPES.get(norm_type, 0), norm_eps, freqs, rope_theta, rope_magnitude, rope_dim, bool(rope_pairs))
+    except (struct.error, OverflowError) as e:             # a number that its member cannot hold
+        _out_of_range(e)
+    binding._check(lib.ts_kv_append_norm_rope(a, _stream(k)))
+    return q_out
+
+
+def ts_kv_read(k_pages, v_pages, table, starts, row_offsets, n_rows, dtype=torch.bfloat16, scales=None, k_out=None, v_out=None):
+    """Positions starts[s], starts[s] + 1, ... of each sequence as rows row_offsets[s], ...: (k, v), [n_rows][heads * head_dim] of `dtype`, zeros where a
+    row is no position.  starts None: from 0 on.  With k_out and / or v_out (of `dtype`) only those are written.  See the header."""
+    lib = _lib or _load()
+    if dtype not in _DTYPES:
+        raise TypeError("dtype: float32 or bfloat16 is needed, got %s" % dtype)
+    pages = _any_pages(k_pages, v_pages, scales)
+    n, width = row_offsets.shape[0] - 1, pages[3] * pages[4]
+    p_table, t_stride, t_width = _table(table, n)
+    if n_rows < 0:
+        _refuse("n_rows: %d", n_rows)
+    if k_out is None and v_out is None:
+        both = torch.zeros((2, n_rows, width), dtype=dtype, device=table.device)
+        k_out, v_out = both[0], both[1]
+    at = []
+    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
+        if t is None:
+            at += (0, 0)
+            continue
+        at += _rows(t, name, width, dtype)
+        if t.shape[0] != n_rows:
+            _refuse("%s: %d rows are needed, got %d", name, n_rows, t.shape[0])
+    try:
+        a = _pack_read(*pages, p_table, t_stride, t_width, 0 if starts is None else _ints(starts, "starts", n), _ints(row_offsets, "row_offsets", 2), n, n_rows,
+                       _DTYPES[dtype], *at)
+    except struct.error as e:
+        _out_of_range(e)
+    binding._check(lib.ts_kv_read(a, _stream(table)))
+    return k_out, v_out
+
+
+def ts_kv_attend_rows_workspace(n_seqs, n_rows, n_q_heads, n_kv_heads, head_dim, max_len, window=0, device="cuda"):
+    """A workspace tensor for ts_kv_attend_rows calls of these sizes (None where they need none)."""
+    n = C.c_uint64()
+    sizes = [_int(v, name) for v, name in ((n_seqs, "n_seqs"), (n_rows, "n_rows"), (n_q_heads, "n_q_heads"), (n_kv_heads, "n_kv_heads"), (head_dim, "head_dim"),
+                                           (max_len, "max_len"), (window, "window"))]
+    binding._check(_load().ts_kv_attend_rows_workspace(*sizes, C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+
+
+def ts_kv_attend_rows(k_pages, v_pages, table, lengths, row_offsets, q, max_len, window=0, scale=None, ancestors=None, scales=None, workspace=None,
+                      out=None, lse=None):
+    """Attention of the rows of chunks, q [rows][heads * head_dim], over a cache of any type that holds them at lengths[s], lengths[s] + 1, ...:
+    (out like q, lse fp32 [rows][heads]; allocated ones are zeros where a row belongs to no sequence).  row_offsets None: one row a sequence.
+    ancestors: int64 [rows], the sets of a draft tree.  scale None: 1 / sqrt(head_dim).  workspace: of ts_kv_attend_rows_workspace; without one the
+    call allocates it.  See the header."""
+    lib = _lib or _load()
+    pages = _any_pages(k_pages, v_pages, scales)
+    kv_heads, hd = pages[3], pages[4]
+    pq, q_stride = _rows(q, "q")
+    rows, width = q.shape
+    if width < 1 or width % hd:
+        _refuse("q: rows of a multiple of %d values are needed, got %s", hd, tuple(q.shape))
+    n = rows if row_offsets is None else row_offsets.shape[0] - 1
+    table, t_stride, t_width = _table(table, n)
+    heads, dtype = width // hd, q.dtype
+    if out is None:
+        out = q.new_empty((rows, width)) if row_offsets is None else q.new_zeros((rows, width))
+    po, o_stride = _rows(out, "out", width, dtype)
+    if out.shape[0] != rows:
+        _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
+    if lse is None:
+        lse = q.new_empty((rows, heads), dtype=torch.float32) if row_offsets is None else q.new_zeros((rows, heads), dtype=torch.float32)
+    elif lse.shape != (rows, heads) or lse.dtype is not torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
+        _refuse("lse: a contiguous fp32 [%d][%d] tensor on a GPU is needed, got %s %s", rows, heads, lse.dtype, tuple(lse.shape))
+    sets = 0
+    if ancestors is not None:
+        if ancestors.dtype is not torch.int64 or not ancestors.is_cuda or ancestors.dim() != 1 or not ancestors.is_contiguous() or ancestors.shape[0] < rows:
+            _refuse("ancestors: at least %d contiguous int64 on a GPU are needed, got %s %s", rows, ancestors.dtype, tuple(ancestors.shape))
+        sets = ancestors.data_ptr()
+    if workspace is None:
+        workspace = ts_kv_attend_rows_workspace(n, rows, heads, kv_heads, hd, max_len, window, q.device)
+    ws, ws_bytes = (0, 0) if workspace is None else (_bytes(workspace, "workspace"), workspace.numel())
+    try:
+        a = _pack_rows(*pages, table, t_stride, t_width, _ints(lengths, "lengths", n), 0 if row_offsets is None else _ints(row_offsets, "row_offsets", 2), sets,
+                       n, rows, max_len, window, heads, _DTYPES[dtype], pq, q_stride, po, o_stride, lse.data_ptr(), hd ** -0.5 if scale is None else scale, ws, ws_bytes)
+    except (struct.error, OverflowError) as e:
+        _out_of_range(e)
+    binding._check(lib.ts_kv_attend_rows(a, _stream(q)))
     return out, lse
