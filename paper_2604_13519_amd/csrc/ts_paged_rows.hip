@@ -460,6 +460,321 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
   }
 }
 
+// ---------------------------------------------------------------------------------
+// Many columns over bf16 and 8-bit pages, bf16 rows: bound by the matrix pipes and by the soft-max beside them.  Eight waves of 32
+// columns share the keys and values of a block of 64 through the LDS; two waves a SIMD, so that one's soft-max runs while the
+// other multiplies.  The running maximum is a reference that moves only when a score passes it by more than 2^8, so that
+// sums are rarely rescaled.  The matrix layout is the one above in tiles of 32 x 32: row m of K's tile is key m with its bits 2 and 3
+// swapped.  Blocks go through registers (8-bit ones are widened there, times their scales, once for all waves) into two LDS slots: while
+// block b is used, b + 1 waits in registers and is written behind it, then b + 2 is requested; one barrier a block.
+// ---------------------------------------------------------------------------------
+constexpr int RW_WAVES = 8, RW_TM = RW_WAVES * 32;
+typedef float ts_f32x16 __attribute__((ext_vector_type(16)));
+
+template <typename T, int HD>
+__global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g) {
+  constexpr bool E8 = sizeof(T) == 1;
+  constexpr int DT = HD / 32, KS = HD / 16, PAGE = 16 * HD;               // tiles of 32 dimensions, steps of 16, elements of a page and head
+  constexpr int RING = 2, LOADS = (4 * PAGE * (int)sizeof(T) + 16 * RW_WAVES * 64 - 1) / (16 * RW_WAVES * 64);      // 16-byte loads of a thread for keys, and for values
+  constexpr int PER_PAGE = PAGE * (int)sizeof(T) / 16;                    // 16-byte pieces of a page
+  constexpr float LAZY = 8.f;
+  __shared__ int dirty;
+  __shared__ ts_u32x4 sk[RING][4 * PAGE / 8], sv[RING][4 * PAGE / 8];
+  const ts_kv_attend_rows_args& a = g.a;
+  const ts_kv_pages& pages = a.cache.pages;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 32, h = lane / 32;
+  int id = gridDim.x - 1 - blockIdx.x;                       // the last tiles of a chunk see most
+  const int hkv = pages.n_kv_heads, kvh = id % hkv; id /= hkv;
+  const int split = id % g.splits, t = id / g.splits, G = g.group;
+  int seq;
+  int64_t m0;
+  if (a.row_offsets) {
+    auto slot = [&](int s) { return ((int64_t)min(max(a.row_offsets[s], 0), a.n_rows) * G / RW_TM) + s; };
+    seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, slot));
+    if (seq < 0) return;
+    m0 = (t - slot(seq)) * RW_TM;
+  } else {
+    seq = t / g.seq_tiles;
+    m0 = (int64_t)(t - seq * g.seq_tiles) * RW_TM;
+  }
+  const RowSeq rs = row_seq(a, seq);
+  const int64_t M = (int64_t)(rs.end - rs.first) * G;
+  if (m0 >= M) return;
+  const int cols = (int)min((int64_t)RW_TM, M - m0), row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
+  const int lo = row_range(a, rs, row0).x, hi = row_range(a, rs, row0 + (rem + cols - 1) / G).y;
+  const int64_t from = ((int64_t)(lo / g.chunk) + split) * g.chunk;
+  if (split > 0 && from >= hi) return;
+  const int k0 = (int)max(from, (int64_t)(lo & ~63)), k1 = (int)min((int64_t)hi, from + g.chunk);
+  const int blocks = k1 > k0 ? (k1 - k0 + 63) / 64 : 0;
+  // this wave's columns
+  const int mine0 = min(wave * 32, cols - 1), mine1 = min(wave * 32 + 32, cols) - 1;     // one of them again where there is none
+  const bool active = wave * 32 < cols;
+  const int2 w_low = row_range(a, rs, row0 + (rem + mine0) / G), w_high = row_range(a, rs, row0 + (rem + max(mine1, mine0)) / G);
+  const int all_lo = w_high.x, all_hi = min(a.ancestors ? min(max(rs.start + 1, 0), w_low.y) : w_low.y, k1);
+
+  const int tile_lo = row_range(a, rs, row0 + (rem + cols - 1) / G).x;
+  const int tile_hi = min(a.ancestors ? min(max(rs.start + 1, 0), row_range(a, rs, row0).y) : row_range(a, rs, row0).y, k1);
+
+  const float scale = g.scale_log2 == 0.f ? 0x1p-149f : fabsf(g.scale_log2);       // never zero: times -infinity
+  int c_lo, c_hi;
+  uint64_t c_set;
+  ts_u32x4 q[KS];
+  {
+    const int m = rem + min(wave * 32 + n, cols - 1), row = row0 + m / G, head = kvh * G + m % G;
+    const int2 range = row_range(a, rs, row);
+    c_lo = range.x; c_hi = min(range.y, k1);
+    c_set = a.ancestors ? a.ancestors[row] : 0;
+    const bf16_t* src = (const bf16_t*)a.q + (int64_t)row * a.q_stride + (int64_t)head * HD;
+    const uint32_t sign = g.scale_log2 < 0.f ? 0x80008000u : 0;      // a negative scale turns the query, exactly
+#pragma unroll
+    for (int c = 0; c < KS; ++c) {
+      const uint4 w = load16(src + c * 16 + h * 8);
+      q[c] = ts_u32x4{w.x ^ sign, w.y ^ sign, w.z ^ sign, w.w ^ sign};
+    }
+  }
+  ts_f32x16 o[DT];
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+  // ---- blocks: pages, registers, LDS
+  const int32_t* table = a.table + (int64_t)seq * a.table_stride;
+  typedef int32_t Pages __attribute__((ext_vector_type(4)));
+  auto pages_of = [&](int b) __attribute__((always_inline)) {
+    auto one = [&](int i) { return k0 + b * 64 + 16 * i < hi && b < blocks ? table[k0 / 16 + b * 4 + i] : -1; };
+    return Pages{one(0), one(1), one(2), one(3)};
+  };
+  auto good = [&](int page) __attribute__((always_inline)) { return page >= 0 && page < pages.n_pages; };
+  auto good_bits = [&](Pages p) __attribute__((always_inline)) { return (good(p[0]) ? 1 : 0) | (good(p[1]) ? 2 : 0) | (good(p[2]) ? 4 : 0) | (good(p[3]) ? 8 : 0); };
+  ts_u32x4 st_k[LOADS], st_v[LOADS], st_vs[E8 ? LOADS : 1];
+  uint32_t st_ks[E8 ? LOADS : 1];
+  auto request = [&](Pages p) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int piece = i * RW_WAVES * 64 + tid, pg = __builtin_amdgcn_readfirstlane(piece / PER_PAGE), in = piece % PER_PAGE;
+      const int which = pg == 0 ? p[0] : pg == 1 ? p[1] : pg == 2 ? p[2] : p[3];
+      const int64_t head = (int64_t)(good(which) ? which : 0) * hkv + kvh;
+      st_k[i] = *reinterpret_cast<const ts_u32x4*>((const char*)pages.k + head * PAGE * sizeof(T) + in * 16);
+      st_v[i] = *reinterpret_cast<const ts_u32x4*>((const char*)pages.v + head * PAGE * sizeof(T) + in * 16);
+      if constexpr (E8) {
+        st_ks[i] = a.cache.k_scales[head * 16 + in * 16 / HD];
+        st_vs[i] = *reinterpret_cast<const ts_u32x4*>(a.cache.v_scales + head * 16);
+      }
+    }
+  };
+  // 16-byte pieces of a key lie where no two of 16 lanes that read the same piece of different keys meet on a bank
+  auto key_place = [&](int key, int piece) __attribute__((always_inline)) { return key * (HD / 8) + (HD == 128 ? piece ^ (key & 15) : piece ^ (key >> 1 & 7)); };
+  auto widen_values = [&](uint32_t lo4, uint32_t hi4, uint32_t s_lo, uint32_t s_hi) __attribute__((always_inline)) {      // eight keys of a dimension
+    float x[4], y[4];
+    e4m3_to_f32(lo4, x);
+    e4m3_to_f32(hi4, y);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { x[e] *= scale_of(s_lo >> 8 * e & 255); y[e] *= scale_of(s_hi >> 8 * e & 255); }
+    return ts_u32x4{__builtin_bit_cast(uint32_t, to_bf16x2(x[0], x[1])), __builtin_bit_cast(uint32_t, to_bf16x2(x[2], x[3])),
+                    __builtin_bit_cast(uint32_t, to_bf16x2(y[0], y[1])), __builtin_bit_cast(uint32_t, to_bf16x2(y[2], y[3]))};
+  };
+  // values that are not finite become zeros where not every column sees them
+  auto clean = [&](ts_u32x4 v) __attribute__((always_inline)) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool x = (v[e] & 0x7f80u) == 0x7f80u, y = (v[e] & 0x7f800000u) == 0x7f800000u;
+      bad |= x | y;
+      v[e] &= (x ? 0 : 0xffffu) | (y ? 0 : 0xffff0000u);
+    }
+    if (bad) dirty = 1;
+    return v;
+  };
+  auto write = [&](int slot, bool all_see) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int piece = i * RW_WAVES * 64 + tid, pg = piece / PER_PAGE, in = piece % PER_PAGE;
+      if (LOADS * RW_WAVES * 64 > 4 * PER_PAGE && piece >= 4 * PER_PAGE) break;      // of small blocks the other waves have no part
+      ts_u32x4 v[E8 ? 2 : 1];
+      if constexpr (E8) {
+        const int key = pg * 16 + in * 16 / HD, c = in % (HD / 16) * 2;
+        const float ks = scale_of(st_ks[i]);
+        uint32_t u[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x[4];
+          e4m3_to_f32(st_k[i][e], x);
+          u[2 * e] = __builtin_bit_cast(uint32_t, to_bf16x2(x[0] * ks, x[1] * ks));
+          u[2 * e + 1] = __builtin_bit_cast(uint32_t, to_bf16x2(x[2] * ks, x[3] * ks));
+        }
+        sk[slot][key_place(key, c)] = ts_u32x4{u[0], u[1], u[2], u[3]};
+        sk[slot][key_place(key, c + 1)] = ts_u32x4{u[4], u[5], u[6], u[7]};
+        v[0] = widen_values(st_v[i][0], st_v[i][1], st_vs[i][0], st_vs[i][1]);
+        v[1] = widen_values(st_v[i][2], st_v[i][3], st_vs[i][2], st_vs[i][3]);
+      } else {
+        sk[slot][key_place(pg * 16 + in / (HD / 8), in % (HD / 8))] = st_k[i];
+        v[0] = st_v[i];
+      }
+#pragma unroll
+      for (int e = 0; e < (E8 ? 2 : 1); ++e) {
+        if (!all_see) v[e] = clean(v[e]);
+        sv[slot][piece * (E8 ? 2 : 1) + e] = v[e];
+      }
+    }
+  };
+
+  const int kn = (n & ~12) | (n & 4) << 1 | (n & 8) >> 1;    // the key that is row n of K's tile
+  // truth values without branches
+  auto sees = [&](int key, bool ok) __attribute__((always_inline)) { return (key >= c_lo) & (key < c_hi) & ok; };
+  auto sees_tree = [&](int key) __attribute__((always_inline)) {
+    const int own = key - rs.start;
+    return (own <= 0) | ((own <= 64) & ((int)(c_set >> ((own - 1) & 63)) & 1));
+  };
+  auto use = [&](int slot, int kb, int ok) __attribute__((always_inline)) {
+    ts_f32x16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < KS; ++c)
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ts_bf16x8, sk[slot][key_place(t * 32 + kn, c * 2 + h)]), __builtin_bit_cast(ts_bf16x8, q[c]), s[t], 0, 0, 0);
+    }
+    if (!(kb >= all_lo && kb + 64 <= all_hi && ok == 15)) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[t][i] = sees(kb + 32 * t + 16 * (i / 8) + 8 * h + i % 8, (ok >> (2 * t + i / 8) & 1) != 0) ? s[t][i] : -INFINITY;
+      if (a.ancestors) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[t][i] = sees_tree(kb + 32 * t + 16 * (i / 8) + 8 * h + i % 8) ? s[t][i] : -INFINITY;
+      }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
+    const uint32_t u = __float_as_uint(top);
+    const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    top = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * scale;
+    if (__ballot(top > m + LAZY)) {                          // the sums so far move to the new reference
+      const float next = top > m + LAZY ? top : m, w = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+      l *= w;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] *= w;
+      m = next;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      ts_u32x4 p[2];
+#pragma unroll
+      for (int i = 0; i < 16; i += 2) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale, -ref)), y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], scale, -ref));
+        l += x;
+        l += y;
+        p[i / 8][i / 2 % 4] = __builtin_bit_cast(uint32_t, to_bf16x2(x, y));
+      }
+#pragma unroll
+      for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ts_bf16x8, sv[slot][((t * 2 + v) * HD + d * 32 + n) * 2 + h]), __builtin_bit_cast(ts_bf16x8, p[v]), o[d], 0, 0, 0);
+    }
+  };
+  auto whole = [&](int b, int ok) { return k0 + b * 64 >= tile_lo && k0 + b * 64 + 64 <= tile_hi && ok == 15; };
+
+  if (tid == 0) dirty = 0;
+  __syncthreads();
+  if (blocks) {
+    Pages next = pages_of(0);
+    int ok = good_bits(next), ok_next;
+    request(next);
+    write(0, whole(0, ok));
+    next = pages_of(1);
+    ok_next = good_bits(next);
+    if (blocks > 1) request(next);
+    next = pages_of(2);
+    __syncthreads();
+    for (int b = 0; b < blocks; ++b) {
+      if (active) use(b & 1, k0 + b * 64, ok);
+      if (b + 1 < blocks) write(b + 1 & 1, whole(b + 1, ok_next));
+      if (b + 2 < blocks) request(next);
+      __syncthreads();
+      ok = ok_next;
+      ok_next = good_bits(next);
+      next = pages_of(b + 3);
+    }
+  }
+  // Values that are not finite, in blocks whose keys not every column sees, were left out: here they reach those that do.
+  if (blocks && dirty) {
+    for (int b = 0; b < blocks; ++b) {
+      const Pages pg = pages_of(b);
+      if (whole(b, good_bits(pg))) continue;
+      for (int u = 0; u < 4; ++u) {
+        const int page = u == 0 ? pg[0] : u == 1 ? pg[1] : u == 2 ? pg[2] : pg[3];
+        if (!good(page)) continue;
+        const int kb = k0 + b * 64 + u * 16 + 8 * h;
+        const int64_t head = (int64_t)page * hkv + kvh;
+        ts_u32x4 in;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const bool one = sees(kb + e, true) & (!a.ancestors | sees_tree(kb + e));
+          in[e / 2] = (e & 1 ? in[e / 2] : 0) | (one ? (e & 1 ? 0x3f800000u : 0x3f80u) : 0);
+        }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          ts_u32x4 v;
+          if constexpr (E8) {
+            const uint2 w = *reinterpret_cast<const uint2*>((const char*)pages.v + (head * HD + d * 32 + n) * 16 + 8 * h), sc = *reinterpret_cast<const uint2*>(a.cache.v_scales + head * 16 + 8 * h);
+            v = widen_values(w.x, w.y, sc.x, sc.y);
+          } else {
+            v = *reinterpret_cast<const ts_u32x4*>((const char*)pages.v + (head * HD + d * 32 + n) * 32 + 16 * h);
+          }
+          for (int cls = 0; cls < 3; ++cls) {
+            ts_u32x4 is;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) is[e] = (of_class(v[e] << 16, cls) ? 0x3f80u : 0) | (of_class(v[e] & 0xffff0000u, cls) ? 0x3f800000u : 0);
+            ts_f32x16 hit;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) hit[i] = 0.f;
+            hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ts_bf16x8, is), __builtin_bit_cast(ts_bf16x8, in), hit, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] += hit[i] > 0.f ? class_value(cls) : 0.f;
+          }
+        }
+      }
+    }
+  }
+  if (!active) return;
+  const uint32_t u = __float_as_uint(l);
+  const auto both = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const float sum = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+  if (wave * 32 + n >= cols) return;
+  const int mc = rem + wave * 32 + n, row = row0 + mc / G, head = kvh * G + mc % G;
+  const int64_t at = (int64_t)row * a.n_q_heads + head;
+  if (g.splits == 1) {
+    const float inv = 1.f / sum;
+    bf16_t* dst = (bf16_t*)a.out + (int64_t)row * a.out_stride + (int64_t)head * HD;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = sum == 0.f ? 0.f : o[d][i + e] * inv;
+        store_n<4>(dst + d * 32 + 2 * i + 4 * h, x);
+      }
+    if (a.lse && h == 0) a.lse[at] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.69314718055994531f;
+  } else {
+    const int64_t part = at * g.splits + (lo / g.chunk + split) % g.splits;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(g.part_o + part * HD + d * 32 + 2 * i + 4 * h) = make_float4(o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]);
+    if (h == 0) *reinterpret_cast<float2*>(g.part_ml + part * 2) = make_float2(m, sum);
+  }
+}
+
 // The join of a row's splits: chunk c of the cache's positions lies at place c % splits.  A workgroup per (row, head), four
 // dimensions a thread, the splits dealt to the rows of threads.
 constexpr int RO_SPLITS = 512;                               // at most, see rows_cut
@@ -524,12 +839,12 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
 // ---------------------------------------------------------------------------------
 constexpr int RO_CUS = 256, RO_UNIT = 128;
 
-struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup, keys of a split, splits, tile slots per KV head
+struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup (16: the wide kernel), keys of a split, splits, tile slots per KV head
 
 // Tiles of 16 columns where a sequence has no more, of 64 (fp32: 32) where it has.
-static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : 4; }
+static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 128 ? 4 : 16; }
 static int64_t rows_units(int max_len, int window) {         // of 128 keys, in what one tile sees
-  const int64_t span = window > 0 && (int64_t)window + 64 < max_len ? window + 64 : max_len;
+  const int64_t span = window > 0 && (int64_t)window + 256 < max_len ? window + 256 : max_len;
   return std::max<int64_t>(1, (span + RO_UNIT - 1) / RO_UNIT);
 }
 // workgroups without a split
@@ -538,7 +853,7 @@ static int64_t rows_whole(int64_t n_seqs, int64_t n_rows, int group, int hkv, in
 }
 static int64_t rows_room(int64_t n_seqs, int64_t n_rows, int group, int hkv, int max_len, int window) {
   int64_t room = 1;
-  for (int nt : {1, 2, 4}) room = std::max(room, std::min(rows_units(max_len, window), 2 * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
+  for (int nt : {1, 2, 4, 16}) room = std::max(room, std::min(rows_units(max_len, window), 2 * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
   return room > 1 && window > 0 ? room + 1 : room;
 }
 static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
@@ -591,6 +906,13 @@ template <typename T, typename TQ, int HD>
 static void launch_rows(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
   constexpr int BIG = sizeof(T) == 4 || sizeof(TQ) == 4 ? 2 : 4;
   const uint32_t grid = (uint32_t)(c.slots * g.a.cache.pages.n_kv_heads * c.splits);
+  if constexpr (sizeof(T) != 4 && sizeof(TQ) == 2) {
+    if (c.nt == 16) {
+      k_kv_attend_wide<T, HD><<<grid, RW_WAVES * 64, 0, s>>>(g);
+      if (c.splits > 1) k_kv_attend_rows_join<TQ, HD><<<(uint32_t)(g.a.n_rows * g.a.n_q_heads), 256, 0, s>>>(g);
+      return;
+    }
+  }
   if (c.nt == 1) k_kv_attend_rows<T, TQ, HD, 1><<<grid, RO_WAVES * 64, 0, s>>>(g);
   else k_kv_attend_rows<T, TQ, HD, BIG><<<grid, RO_WAVES * 64, 0, s>>>(g);
   if (c.splits > 1) k_kv_attend_rows_join<TQ, HD><<<(uint32_t)(g.a.n_rows * g.a.n_q_heads), 256, 0, s>>>(g);
