@@ -11,6 +11,9 @@ typedef uint16_t f16_t;    // IEEE half bit pattern in memory
 // them to the global address space keeps vector memory and LDS waits independent.
 #define TS_GLOBAL __attribute__((address_space(1)))
 #define TS_LDS __attribute__((address_space(3)))
+// What no launch in flight writes: uniform addresses are read by scalar loads, which do not wait behind vector loads, also where a
+// barrier or a store stands before them.
+#define TS_CONSTANT __attribute__((address_space(4)))
 
 __device__ __forceinline__ float bf16_to_f32(bf16_t u) { return __uint_as_float((uint32_t)u << 16); }
 

@@ -116,12 +116,25 @@ __device__ __forceinline__ void append_values(const void* v_rows, int64_t v_stri
 // ---- 8-bit pages ------------------------------------------------------------------
 struct e4m3_t { uint8_t b; };
 
-// 2^(byte - 127); 255: NaN
-__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte == 0 ? 0x00400000u : byte == 255 ? 0x7fc00000u : byte << 23); }
-// four values, the bits of one dword
-__device__ __forceinline__ void e4m3_to_f32(uint32_t w, float* v) {
-  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, 1.f, true);
+// The conversions of gfx950 take a scale as the exponent field of an fp32, its other bits ignored: 2^(field - 127), 255 is NaN; exactly what
+// a scale byte says.  scale_at<I>(w): the operand for byte I of w.
+template <int I> __device__ __forceinline__ float scale_at(uint32_t w) { return __uint_as_float(I == 3 ? w >> 1 : w << (23 - 8 * I)); }
+// four values, the bits of one dword, times the scale
+__device__ __forceinline__ void e4m3_to_f32(uint32_t w, float scale, float* v) {
+  const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
   v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
+}
+// four values of one dword times four scales, the bytes of another
+__device__ __forceinline__ void e4m3_to_f32(uint32_t w, uint32_t scales, float* v) {
+  v[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale_at<0>(scales), false)[0];
+  v[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale_at<1>(scales), false)[1];
+  v[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale_at<2>(scales), true)[0];
+  v[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale_at<3>(scales), true)[1];
+}
+// eight values of one scale as bf16, rounded only where bf16 is subnormal
+__device__ __forceinline__ ts_u32x4 e4m3_to_bf16(uint32_t a, uint32_t b, float scale) {
+  return ts_u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
+                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};
 }
 __device__ __forceinline__ uint32_t f32_to_e4m3(float a, float b, float c, float d) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);

@@ -318,11 +318,9 @@ __global__ __launch_bounds__(RA_THREADS) void k_kv_read(ReadArgs g) {
         float v[VE];
         if constexpr (sizeof(TC) == 1) {
           const uint8_t* src = (const uint8_t*)a.cache.pages.k + at16 * HD + c * VE;
-          const float scale = scale_of(a.cache.k_scales[at16]);
+          const float scale = scale_at<0>(a.cache.k_scales[at16]);
 #pragma unroll
-          for (int e = 0; e < VE; e += 4) e4m3_to_f32(*(const uint32_t*)(src + e), v + e);
-#pragma unroll
-          for (int e = 0; e < VE; ++e) v[e] *= scale;
+          for (int e = 0; e < VE; e += 4) e4m3_to_f32(*(const uint32_t*)(src + e), scale, v + e);
         } else {
           load_n<VE>((const TC*)a.cache.pages.k + at16 * HD + c * VE, v);
         }
@@ -335,23 +333,16 @@ __global__ __launch_bounds__(RA_THREADS) void k_kv_read(ReadArgs g) {
         const int h = val0 + i * DV / HD, d = i * DV % HD;
         const int64_t head = (int64_t)page * hkv + h;
         float v[DV][16];
+        ts_u32x4 sc = {0, 0, 0, 0};
+        if constexpr (sizeof(TC) == 1) sc = *reinterpret_cast<const ts_u32x4*>(a.cache.v_scales + head * 16);
 #pragma unroll
         for (int e = 0; e < DV; ++e) {
           if constexpr (sizeof(TC) == 1) {
-            const uint4 w = *reinterpret_cast<const uint4*>((const uint8_t*)a.cache.pages.v + (head * HD + d + e) * 16);
-            e4m3_to_f32(w.x, v[e]); e4m3_to_f32(w.y, v[e] + 4); e4m3_to_f32(w.z, v[e] + 8); e4m3_to_f32(w.w, v[e] + 12);
+            const ts_u32x4 w = *reinterpret_cast<const ts_u32x4*>((const char*)a.cache.pages.v + (head * HD + d + e) * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e4m3_to_f32(w[i], sc[i], v[e] + 4 * i);
           } else {
             load_n<16>((const TC*)a.cache.pages.v + (head * HD + d + e) * 16, v[e]);
-          }
-        }
-        if constexpr (sizeof(TC) == 1) {
-          const uint4 sc = *reinterpret_cast<const uint4*>(a.cache.v_scales + head * 16);
-          const uint32_t u[4] = {sc.x, sc.y, sc.z, sc.w};
-#pragma unroll
-          for (int p = 0; p < 16; ++p) {
-            const float scale = scale_of(u[p / 4] >> p % 4 * 8 & 255);
-#pragma unroll
-            for (int e = 0; e < DV; ++e) v[e][p] *= scale;
           }
         }
         TO* dst = (TO*)a.v_out + (int64_t)row * a.v_stride + (int64_t)h * HD + d;

@@ -1,4 +1,6 @@
 // Attention of chunks of rows over a paged cache of any type: causal chunks, windows, draft trees, single tokens.
+#include <type_traits>
+
 #include "ts_paged.h"
 
 // ---------------------------------------------------------------------------------
@@ -50,16 +52,44 @@ struct RowSeq {
   int start;                             // position of the chunk's row 0, cut to +-2^30
   int cap;                               // positions at or above are not seen
 };
-__device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int seq) {
+__device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int off, int end, int64_t len) {
   RowSeq s;
-  const int64_t len = a.lengths[seq];
-  const int off = a.row_offsets ? a.row_offsets[seq] : seq;
-  s.end = a.row_offsets ? max(min(a.row_offsets[seq + 1], a.n_rows), 0) : seq + 1;
+  s.end = max(min(end, a.n_rows), 0);
   s.first = min(max(off, 0), a.n_rows);                      // both cut, so that their difference fits whatever the offsets are
   s.zero = len - off;
   s.start = (int)max((int64_t)-(1 << 30), min((int64_t)1 << 30, len));
   s.cap = (int)min((int64_t)a.max_len, (int64_t)a.table_width * 16);
   return s;
+}
+__device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int seq) {
+  return a.row_offsets ? row_seq(a, a.row_offsets[seq], a.row_offsets[seq + 1], a.lengths[seq]) : row_seq(a, seq, seq + 1, a.lengths[seq]);
+}
+// The sequence of a tile of `tm` columns and its first column, -1 if there is none.  Sequence s has tile slots [off group / tm + s, ...): as
+// many as its tiles or one more, without a sum over the others.
+__device__ __forceinline__ int tile_of(const RowsArgs& g, int t, int tm, int64_t& m0, RowSeq& rs) {
+  const ts_kv_attend_rows_args& a = g.a;
+  int seq;
+  if (!a.row_offsets) {
+    seq = t / g.seq_tiles;
+    m0 = (int64_t)(t - seq * g.seq_tiles) * tm;
+    rs = row_seq(a, seq);
+  } else {
+    auto slot = [&](int off, int s) { return (int64_t)min(max(off, 0), a.n_rows) * g.group / tm + s; };
+    if (a.n_seqs < 64) {                                     // offsets and lengths in one trip to memory
+      const int lane = threadIdx.x % 64, off = a.row_offsets[min(lane, a.n_seqs)], len = a.lengths[min(lane, a.n_seqs - 1)];
+      seq = __popcll(__ballot(lane < a.n_seqs && slot(off, lane) <= t)) - 1;
+      if (seq < 0) return -1;
+      const int first = __builtin_amdgcn_readlane(off, seq);
+      m0 = (t - slot(first, seq)) * tm;
+      rs = row_seq(a, first, __builtin_amdgcn_readlane(off, seq + 1), __builtin_amdgcn_readlane(len, seq));
+    } else {
+      seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, [&](int s) { return slot(a.row_offsets[s], s); }));
+      if (seq < 0) return -1;
+      m0 = (t - slot(a.row_offsets[seq], seq)) * tm;
+      rs = row_seq(a, seq);
+    }
+  }
+  return m0 < (int64_t)(rs.end - rs.first) * g.group ? seq : -1;
 }
 // positions [lo, hi) that a row can see (with ancestors: some of them)
 __device__ __forceinline__ int2 row_range(const ts_kv_attend_rows_args& a, const RowSeq& s, int row) {
@@ -69,18 +99,8 @@ __device__ __forceinline__ int2 row_range(const ts_kv_attend_rows_args& a, const
   return make_int2(lo, hi);
 }
 
-template <typename T> struct RowsOf;     // keys of a block
-template <> struct RowsOf<bf16_t> { static constexpr int KB = 32; };
-template <> struct RowsOf<float> { static constexpr int KB = 32; };
-template <> struct RowsOf<e4m3_t> { static constexpr int KB = 64; };
-
-// eight e4m3 values as bf16, exactly
-__device__ __forceinline__ uint4 widen8(uint32_t a, uint32_t b) {
-  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false)),
-                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true)));
-}
+// whether one of four scales is NaN
+__device__ __forceinline__ bool nan_scale(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u) != 0; }
 __device__ __forceinline__ bool not_finite(uint32_t bf16_pair) {
   return (bf16_pair & 0x7f80u) == 0x7f80u || (bf16_pair & 0x7f800000u) == 0x7f800000u;
 }
@@ -93,7 +113,7 @@ __device__ __forceinline__ float class_value(int cls) { return __uint_as_float(c
 template <typename T, typename TQ, int HD, int NT>
 __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_rows(RowsArgs g) {
   constexpr bool F32 = sizeof(T) == 4, E8 = sizeof(T) == 1;
-  constexpr int KB = RowsOf<T>::KB, KT = KB / 16, KL = KB / 4, PG = KB / 16;   // keys of a block, tiles of them, keys of a lane, pages
+  constexpr int KB = 32, KT = KB / 16, KL = KB / 4;                            // keys of a block, tiles of them, keys of a lane
   constexpr int QP = !F32 && sizeof(TQ) == 4 ? 3 : 1;                          // terms of a query
   constexpr int PP = !F32 && (sizeof(TQ) == 4 || NT == 1) ? 3 : 1;             // terms of a probability
   constexpr int KC = (HD * (int)sizeof(T) + 63) / 64;                          // 16-byte pieces of a key per lane
@@ -108,21 +128,11 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
   int id = blockIdx.x;
   const int hkv = pages.n_kv_heads, kvh = id % hkv; id /= hkv;
   const int split = id % g.splits, t = id / g.splits, G = g.group;
-  // Sequence s has tile slots [off G / TM + s, ...): as many as its tiles or one more, without a sum over the others.
-  int seq;
   int64_t m0;
-  if (a.row_offsets) {
-    auto slot = [&](int s) { return ((int64_t)min(max(a.row_offsets[s], 0), a.n_rows) * G / TM) + s; };
-    seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, slot));
-    if (seq < 0) return;
-    m0 = (t - slot(seq)) * TM;
-  } else {
-    seq = t / g.seq_tiles;
-    m0 = (int64_t)(t - seq * g.seq_tiles) * TM;
-  }
-  const RowSeq rs = row_seq(a, seq);
+  RowSeq rs;
+  const int seq = tile_of(g, t, TM, m0, rs);
+  if (seq < 0) return;
   const int64_t M = (int64_t)(rs.end - rs.first) * G;
-  if (m0 >= M) return;
   const int cols = (int)min((int64_t)TM, M - m0), row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
   const int2 low = row_range(a, rs, row0), high = row_range(a, rs, row0 + (rem + cols - 1) / G);
   const int lo = low.x, hi = high.y;                         // what any column sees, and what all do
@@ -134,7 +144,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
   // columns: lane n of tile j
   int c_lo[NT], c_hi[NT];
   uint64_t c_set[NT];
-  uint4 q[NT][QP][QS];
+  ts_u32x4 q[NT][QP][QS];
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int m = rem + min(j * 16 + n, cols - 1), row = row0 + m / G, head = kvh * G + m % G;
@@ -161,9 +171,9 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
           for (int p = 0; p < QP; ++p) u[p][e] = __builtin_bit_cast(uint32_t, w[p]);
         }
 #pragma unroll
-        for (int p = 0; p < QP; ++p) q[j][p][c] = make_uint4(u[p][0], u[p][1], u[p][2], u[p][3]);
+        for (int p = 0; p < QP; ++p) q[j][p][c] = ts_u32x4{u[p][0], u[p][1], u[p][2], u[p][3]};
       } else {
-        q[j][0][c] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+        q[j][0][c] = ts_u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
       }
     }
   }
@@ -177,39 +187,30 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
     for (int d = 0; d < DT; ++d) o[j][d] = ts_f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int32_t* table = a.table + (int64_t)seq * a.table_stride;
+  const TS_CONSTANT int32_t* table = (const TS_CONSTANT int32_t*)(a.table + (int64_t)seq * a.table_stride);
   const char* kp = (const char*)pages.k;
   const char* vp = (const char*)pages.v;
   const int64_t head_bytes = (int64_t)16 * HD * sizeof(T), page_bytes = hkv * head_bytes;
 
-  struct Pages { int p[PG]; };
-  struct Block { uint4 k[KT][KC], v[F32 ? 2 : 1][DT], ks, vs; bool ok[PG]; };
-  auto pages_of = [&](int kb) {                              // the later ones may lie behind the last position
-    Pages p;
-#pragma unroll
-    for (int i = 0; i < PG; ++i) p.p[i] = kb + 16 * i < hi ? table[kb / 16 + i] : -1;
-    return p;
+  typedef typename std::conditional<E8, ts_u32x2, ts_u32x4>::type Vals;        // four (fp32) or eight consecutive keys of a dimension
+  struct Block { ts_u32x4 k[KT][KC]; Vals v[F32 ? 2 : 1][DT]; ts_u32x2 ks, vs; bool ok0, ok1; };
+  auto pages_of = [&](int kb) {                              // the second may lie behind the last position
+    return make_int2(kb < hi ? table[kb / 16] : -1, kb + 16 < hi ? table[kb / 16 + 1] : -1);
   };
-  auto fetch = [&](Block& f, const Pages& pg) {              // pages that do not exist: another is read, and masked
-    int64_t at[PG];
-    int some = 0;
-#pragma unroll
-    for (int i = 0; i < PG; ++i) {
-      f.ok[i] = pg.p[i] >= 0 && pg.p[i] < pages.n_pages;
-      some = f.ok[i] ? pg.p[i] : some;
-      at[i] = some * page_bytes + kvh * head_bytes;
-    }
-    auto pick = [&](int i) { return PG == 2 ? (i == 0 ? at[0] : at[1]) : (i < 2 ? (i == 0 ? at[0] : at[1]) : (i == 2 ? at[2] : at[PG - 1])); };
-    const int64_t mine = PG == 4 ? pick(n / 4) : pick(n / 8);          // bf16 and 8 bits: the page of this lane's key
+  auto fetch = [&](Block& f, int2 pg) __attribute__((always_inline)) {         // pages that do not exist: another is read, and masked
+    f.ok0 = pg.x >= 0 && pg.x < pages.n_pages;
+    f.ok1 = pg.y >= 0 && pg.y < pages.n_pages;
+    const int p0 = f.ok0 ? pg.x : 0, p1 = f.ok1 ? pg.y : p0;
+    const int64_t at0 = p0 * page_bytes + kvh * head_bytes, at1 = p1 * page_bytes + kvh * head_bytes;
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
       const int key = F32 ? 16 * t + n : KL * (n / 4) + 4 * t + n % 4;
-      const char* row = kp + (F32 ? at[t] : mine) + key % 16 * HD * (int)sizeof(T);
+      const char* row = kp + (key < 16 ? at0 : at1) + key % 16 * HD * (int)sizeof(T);
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
         const int b = (c * 4 + lg) * 16;
-        if (HD * (int)sizeof(T) % 64 == 0 || b < HD * (int)sizeof(T)) f.k[t][c] = *reinterpret_cast<const uint4*>(row + b);
-        else f.k[t][c] = make_uint4(0, 0, 0, 0);
+        if (HD * (int)sizeof(T) % 64 == 0 || b < HD * (int)sizeof(T)) f.k[t][c] = *reinterpret_cast<const ts_u32x4*>(row + b);
+        else f.k[t][c] = ts_u32x4{0, 0, 0, 0};
       }
     }
     if constexpr (F32) {
@@ -217,22 +218,21 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          if (HD % 16 == 0 || d * 16 + n < HD) f.v[t][d] = *reinterpret_cast<const uint4*>(vp + at[t] + (d * 16 + n) * 64 + lg * 16);
-          else f.v[t][d] = make_uint4(0, 0, 0, 0);
+          if (HD % 16 == 0 || d * 16 + n < HD) f.v[t][d] = *reinterpret_cast<const ts_u32x4*>(vp + (t ? at1 : at0) + (d * 16 + n) * 64 + lg * 16);
+          else f.v[t][d] = ts_u32x4{0, 0, 0, 0};
         }
-    } else if constexpr (E8) {
-      const int64_t own = pick(lg);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) f.v[0][d] = *reinterpret_cast<const uint4*>(vp + own + (d * 16 + n) * 16);
-      f.ks = *reinterpret_cast<const uint4*>(a.cache.k_scales + own / HD);      // 16 HD bytes of codes to 16 of scales
-      f.vs = *reinterpret_cast<const uint4*>(a.cache.v_scales + own / HD);
     } else {
-      const char* col = vp + pick(lg / 2) + (lg & 1) * 16;
+      constexpr int HALF = 8 * (int)sizeof(T);               // bytes of eight keys
+      const char* col = vp + (lg < 2 ? at0 : at1) + (lg & 1) * HALF;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) f.v[0][d] = *reinterpret_cast<const uint4*>(col + (d * 16 + n) * 32);
+      for (int d = 0; d < DT; ++d) f.v[0][d] = *reinterpret_cast<const Vals*>(col + (d * 16 + n) * 2 * HALF);
+      if constexpr (E8) {                                    // 16 HD bytes of codes to 16 of scales: of this lane's rows of K's tiles, of its keys
+        f.ks = *reinterpret_cast<const ts_u32x2*>(a.cache.k_scales + (n < 8 ? at0 : at1) / HD + (n / 4 & 1) * 8);
+        f.vs = *reinterpret_cast<const ts_u32x2*>(a.cache.v_scales + (lg < 2 ? at0 : at1) / HD + (lg & 1) * 8);
+      }
     }
   };
-  auto use = [&](Block& f, int kb) {
+  auto use = [&](Block& f, int kb) __attribute__((always_inline)) {
     ts_f32x4 s[NT][KT];
 #pragma unroll
     for (int t = 0; t < KT; ++t) {
@@ -249,8 +249,8 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
             for (int e = 0; e < 4; ++e) s[j][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kx[e], qx[e], s[j][t], 0, 0, 0);
           }
         } else {
-          uint4 kx;
-          if constexpr (E8) kx = c % 2 ? widen8(f.k[t][c / 2].z, f.k[t][c / 2].w) : widen8(f.k[t][c / 2].x, f.k[t][c / 2].y);
+          ts_u32x4 kx;
+          if constexpr (E8) kx = e4m3_to_bf16(f.k[t][c / 2][c % 2 * 2], f.k[t][c / 2][c % 2 * 2 + 1], __uint_as_float(f.ks[t] >> n % 4 * 8 << 23));
           else kx = f.k[t][c];
 #pragma unroll
           for (int j = 0; j < NT; ++j)
@@ -261,9 +261,9 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
       }
     }
     auto key_of = [&](int i) { return kb + (F32 ? 16 * (i / 4) + 4 * lg + i % 4 : KL * lg + i); };      // a lane's i-th key
-    bool whole = kb >= all_lo && kb + KB <= min(all_hi, k1);
-#pragma unroll
-    for (int i = 0; i < PG; ++i) whole = whole && f.ok[i];
+    const bool whole = kb >= all_lo && kb + KB <= min(all_hi, k1) && f.ok0 && f.ok1;
+    bool nans = false;
+    if constexpr (E8) nans = __ballot(nan_scale(f.vs[0]) || nan_scale(f.vs[1])) != 0;
     uint32_t keep[NT];
     uint32_t pk[NT][PP][KL / 2];                             // probabilities as pairs of bf16 terms
     float px[F32 ? NT : 1][F32 ? KL : 1];
@@ -272,20 +272,15 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
       float x[KL];
 #pragma unroll
       for (int i = 0; i < KL; ++i) {
-        float scale = g.scale_log2;
-        if constexpr (E8) scale *= scale_of((i < 8 ? (i < 4 ? f.ks.x : f.ks.y) : (i < 12 ? f.ks.z : f.ks.w)) >> i % 4 * 8 & 255);
-        x[i] = s[j][i / 4][i % 4] * scale;
+        x[i] = s[j][i / 4][i % 4] * g.scale_log2;
       }
       if (!whole) {
         keep[j] = 0;
 #pragma unroll
         for (int i = 0; i < KL; ++i) {
           const int key = key_of(i), own = key - rs.start;
-          bool in = key >= c_lo[j] && key < min(c_hi[j], k1);
-          if (F32) in = in && f.ok[i / 4];
-          else if (E8) in = in && (lg < 2 ? (lg == 0 ? f.ok[0] : f.ok[1]) : (lg == 2 ? f.ok[2 % PG] : f.ok[3 % PG]));
-          else in = in && (lg < 2 ? f.ok[0] : f.ok[1]);
-          if (a.ancestors) in = in && (own <= 0 || (own <= 64 && (c_set[j] >> (own - 1 & 63) & 1)));
+          bool in = (key >= c_lo[j]) & (key < min(c_hi[j], k1)) & (F32 ? (i < 4 ? f.ok0 : f.ok1) : (lg < 2 ? f.ok0 : f.ok1));
+          if (a.ancestors) in = in & ((own <= 0) | ((own <= 64) & ((int)(c_set[j] >> (own - 1 & 63)) & 1)));
           x[i] = in ? x[i] : -INFINITY;
           keep[j] |= in ? 1u << i : 0;
         }
@@ -306,10 +301,15 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
       for (int i = 0; i < KL; ++i) {
         x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
         l[j] += x[i];
-        if constexpr (E8) {
-          x[i] *= scale_of((i < 8 ? (i < 4 ? f.vs.x : f.vs.y) : (i < 12 ? f.vs.z : f.vs.w)) >> i % 4 * 8 & 255);
-          if (!whole) x[i] = keep[j] >> i & 1 ? x[i] : 0.f;            // the scale of what is not seen may be NaN
+      }
+      if constexpr (E8) {                                    // the scale of a value; of what is not seen it may be NaN
+        if (nans) {
+#pragma unroll
+          for (int i = 0; i < KL; ++i)
+            if ((f.vs[i / 4] >> i % 4 * 8 & 255) == 255) x[i] = whole || (keep[j] >> i & 1) ? NAN : 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < KL; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], (int)(f.vs[i / 4] >> i % 4 * 8 & 255) - 127);
       }
       if constexpr (F32) {
 #pragma unroll
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          uint32_t v[4] = {f.v[t][d].x, f.v[t][d].y, f.v[t][d].z, f.v[t][d].w};
+          ts_u32x4 v = f.v[t][d];
           if (!whole && __ballot((v[0] & 0x7f800000u) == 0x7f800000u || (v[1] & 0x7f800000u) == 0x7f800000u || (v[2] & 0x7f800000u) == 0x7f800000u ||
                                  (v[3] & 0x7f800000u) == 0x7f800000u)) {
             for (int cls = 0; cls < 3; ++cls)
@@ -353,39 +353,35 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
         }
     } else {
 #pragma unroll
-      for (int u = 0; u < KB / 32; ++u)
-#pragma unroll
         for (int d = 0; d < DT; ++d) {
-          uint4 v;
-          if constexpr (E8) v = u ? widen8(f.v[0][d].z, f.v[0][d].w) : widen8(f.v[0][d].x, f.v[0][d].y);
-          else v = f.v[0][d];
-          if (!whole && __ballot(not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w))) {
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          ts_u32x4 w;
+          if constexpr (E8) w = e4m3_to_bf16(f.v[0][d][0], f.v[0][d][1], 1.f);
+          else w = f.v[0][d];
+          if (!whole && __ballot(not_finite(w[0]) || not_finite(w[1]) || not_finite(w[2]) || not_finite(w[3]))) {
             for (int cls = 0; cls < 3; ++cls) {
-              uint32_t is[4];
+              ts_u32x4 is;
 #pragma unroll
               for (int e = 0; e < 4; ++e) is[e] = (of_class(w[e] << 16, cls) ? 0x3f80u : 0) | (of_class(w[e] & 0xffff0000u, cls) ? 0x3f800000u : 0);
 #pragma unroll
               for (int j = 0; j < NT; ++j) {
-                uint32_t in[4];
+                ts_u32x4 in;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) in[e] = (keep[j] >> (8 * u + 2 * e) & 1 ? 0x3f80u : 0) | (keep[j] >> (8 * u + 2 * e + 1) & 1 ? 0x3f800000u : 0);
-                const ts_f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, make_uint4(is[0], is[1], is[2], is[3])),
-                                                                              __builtin_bit_cast(ts_bf16x8, make_uint4(in[0], in[1], in[2], in[3])), ts_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                for (int e = 0; e < 4; ++e) in[e] = (keep[j] >> (2 * e) & 1 ? 0x3f80u : 0) | (keep[j] >> (2 * e + 1) & 1 ? 0x3f800000u : 0);
+                const ts_f32x4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, is),
+                                                                              __builtin_bit_cast(ts_bf16x8, in), ts_f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) o[j][d][r] += hit[r] > 0.f ? class_value(cls) : 0.f;
               }
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) w[e] &= ((w[e] & 0x7f80u) == 0x7f80u ? 0 : 0xffffu) | ((w[e] & 0x7f800000u) == 0x7f800000u ? 0 : 0xffff0000u);
-            v = make_uint4(w[0], w[1], w[2], w[3]);
           }
 #pragma unroll
           for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int p = PP - 1; p >= 0; --p)
-              o[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, v),
-                                                                __builtin_bit_cast(ts_bf16x8, make_uint4(pk[j][p][4 * u], pk[j][p][4 * u + 1], pk[j][p][4 * u + 2], pk[j][p][4 * u + 3])), o[j][d], 0, 0, 0);
+              o[j][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(ts_bf16x8, w),
+                                                                __builtin_bit_cast(ts_bf16x8, ts_u32x4{pk[j][p][0], pk[j][p][1], pk[j][p][2], pk[j][p][3]}), o[j][d], 0, 0, 0);
         }
     }
   };
@@ -403,7 +399,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
     const int last = kw + (k1 - 1 - kw) / STEP * STEP;
     Block fa, fb;
     fetch(fa, pages_of(kw));
-    Pages next = pages_of(kw + STEP);
+    int2 next = pages_of(kw + STEP);
     for (int kb = kw; kb < k1; kb += 2 * STEP) {
       fetch(fb, next);
       next = pages_of(min(kb + 2 * STEP, last));
@@ -414,7 +410,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
       use(fb, kb + STEP);
     }
   } else {
-    Pages next = pages_of(kw);
+    int2 next = pages_of(kw);
     for (int kb = kw; kb < k1; kb += STEP) {
       Block f;
       fetch(f, next);
@@ -466,7 +462,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
 // other multiplies.  The running maximum is a reference that moves only when a score passes it by more than 2^8, so that
 // sums are rarely rescaled.  The matrix layout is the one above in tiles of 32 x 32: row m of K's tile is key m with its bits 2 and 3
 // swapped.  Blocks go through registers (8-bit ones are widened there, times their scales, once for all waves) into two LDS slots: while
-// block b is used, b + 1 waits in registers and is written behind it, then b + 2 is requested; one barrier a block.
+// block b is used, b + 1 is written and b + 2 and b + 3 are on their way; one barrier a block.
 // ---------------------------------------------------------------------------------
 constexpr int RW_WAVES = 8, RW_TM = RW_WAVES * 32;
 typedef float ts_f32x16 __attribute__((ext_vector_type(16)));
@@ -486,20 +482,11 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   int id = gridDim.x - 1 - blockIdx.x;                       // the last tiles of a chunk see most
   const int hkv = pages.n_kv_heads, kvh = id % hkv; id /= hkv;
   const int split = id % g.splits, t = id / g.splits, G = g.group;
-  int seq;
   int64_t m0;
-  if (a.row_offsets) {
-    auto slot = [&](int s) { return ((int64_t)min(max(a.row_offsets[s], 0), a.n_rows) * G / RW_TM) + s; };
-    seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, slot));
-    if (seq < 0) return;
-    m0 = (t - slot(seq)) * RW_TM;
-  } else {
-    seq = t / g.seq_tiles;
-    m0 = (int64_t)(t - seq * g.seq_tiles) * RW_TM;
-  }
-  const RowSeq rs = row_seq(a, seq);
+  RowSeq rs;
+  const int seq = tile_of(g, t, RW_TM, m0, rs);
+  if (seq < 0) return;
   const int64_t M = (int64_t)(rs.end - rs.first) * G;
-  if (m0 >= M) return;
   const int cols = (int)min((int64_t)RW_TM, M - m0), row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
   const int lo = row_range(a, rs, row0).x, hi = row_range(a, rs, row0 + (rem + cols - 1) / G).y;
   const int64_t from = ((int64_t)(lo / g.chunk) + split) * g.chunk;
@@ -540,38 +527,33 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
   // ---- blocks: pages, registers, LDS
-  const int32_t* table = a.table + (int64_t)seq * a.table_stride;
-  typedef int32_t Pages __attribute__((ext_vector_type(4)));
-  auto pages_of = [&](int b) __attribute__((always_inline)) {
-    auto one = [&](int i) { return k0 + b * 64 + 16 * i < hi && b < blocks ? table[k0 / 16 + b * 4 + i] : -1; };
-    return Pages{one(0), one(1), one(2), one(3)};
+  const int32_t* table = a.table + (int64_t)seq * a.table_stride + k0 / 16 + lane % 4;
+  auto pages_of = [&](int b) __attribute__((always_inline)) {  // lane i: page i % 4 of the block, -1 behind the last position
+    return b < blocks && k0 + b * 64 + lane % 4 * 16 < hi ? table[b * 4] : -1;
   };
-  auto good = [&](int page) __attribute__((always_inline)) { return page >= 0 && page < pages.n_pages; };
-  auto good_bits = [&](Pages p) __attribute__((always_inline)) { return (good(p[0]) ? 1 : 0) | (good(p[1]) ? 2 : 0) | (good(p[2]) ? 4 : 0) | (good(p[3]) ? 8 : 0); };
-  ts_u32x4 st_k[LOADS], st_v[LOADS], st_vs[E8 ? LOADS : 1];
-  uint32_t st_ks[E8 ? LOADS : 1];
-  auto request = [&](Pages p) __attribute__((always_inline)) {
+  auto good_bits = [&](int pg) __attribute__((always_inline)) { return (int)__ballot((uint32_t)pg < (uint32_t)pages.n_pages) & 15; };
+  struct Stage { ts_u32x4 k[LOADS], v[LOADS], vs[E8 ? LOADS : 1]; uint32_t ks[E8 ? LOADS : 1]; };
+  const uint32_t piece_at = tid % PER_PAGE * 16;             // this thread's piece of a page
+  auto request = [&](Stage& st, int pg, int ok) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int piece = i * RW_WAVES * 64 + tid, pg = __builtin_amdgcn_readfirstlane(piece / PER_PAGE), in = piece % PER_PAGE;
-      const int which = pg == 0 ? p[0] : pg == 1 ? p[1] : pg == 2 ? p[2] : p[3];
-      const int64_t head = (int64_t)(good(which) ? which : 0) * hkv + kvh;
-      st_k[i] = *reinterpret_cast<const ts_u32x4*>((const char*)pages.k + head * PAGE * sizeof(T) + in * 16);
-      st_v[i] = *reinterpret_cast<const ts_u32x4*>((const char*)pages.v + head * PAGE * sizeof(T) + in * 16);
+      const int which = min(__builtin_amdgcn_readfirstlane((i * RW_WAVES * 64 + tid) / PER_PAGE), 3);
+      const int page = ok >> which & 1 ? __builtin_amdgcn_readlane(pg, which) : 0;
+      const int64_t head = (int64_t)page * hkv + kvh;
+      st.k[i] = *reinterpret_cast<const ts_u32x4*>((const char*)pages.k + head * (PAGE * (int)sizeof(T)) + piece_at);
+      st.v[i] = *reinterpret_cast<const ts_u32x4*>((const char*)pages.v + head * (PAGE * (int)sizeof(T)) + piece_at);
       if constexpr (E8) {
-        st_ks[i] = a.cache.k_scales[head * 16 + in * 16 / HD];
-        st_vs[i] = *reinterpret_cast<const ts_u32x4*>(a.cache.v_scales + head * 16);
+        st.ks[i] = (a.cache.k_scales + head * 16)[piece_at / HD];
+        st.vs[i] = *reinterpret_cast<const ts_u32x4*>(a.cache.v_scales + head * 16);
       }
     }
   };
-  // 16-byte pieces of a key lie where no two of 16 lanes that read the same piece of different keys meet on a bank
-  auto key_place = [&](int key, int piece) __attribute__((always_inline)) { return key * (HD / 8) + (HD == 128 ? piece ^ (key & 15) : piece ^ (key >> 1 & 7)); };
+  // 16-byte pieces of a key lie where no two of eight lanes that read the same piece of different keys (0 .. 3 and 8 .. 11, say) meet on a bank
+  auto key_place = [&](int key, int piece) __attribute__((always_inline)) { return key * (HD / 8) + (piece ^ ((key & 3) | (key >> 1 & 4))); };
   auto widen_values = [&](uint32_t lo4, uint32_t hi4, uint32_t s_lo, uint32_t s_hi) __attribute__((always_inline)) {      // eight keys of a dimension
     float x[4], y[4];
-    e4m3_to_f32(lo4, x);
-    e4m3_to_f32(hi4, y);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) { x[e] *= scale_of(s_lo >> 8 * e & 255); y[e] *= scale_of(s_hi >> 8 * e & 255); }
+    e4m3_to_f32(lo4, s_lo, x);
+    e4m3_to_f32(hi4, s_hi, y);
     return ts_u32x4{__builtin_bit_cast(uint32_t, to_bf16x2(x[0], x[1])), __builtin_bit_cast(uint32_t, to_bf16x2(x[2], x[3])),
                     __builtin_bit_cast(uint32_t, to_bf16x2(y[0], y[1])), __builtin_bit_cast(uint32_t, to_bf16x2(y[2], y[3]))};
   };
@@ -587,7 +569,7 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
     if (bad) dirty = 1;
     return v;
   };
-  auto write = [&](int slot, bool all_see) __attribute__((always_inline)) {
+  auto write = [&](Stage& st, int slot, bool all_see) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int piece = i * RW_WAVES * 64 + tid, pg = piece / PER_PAGE, in = piece % PER_PAGE;
@@ -595,22 +577,14 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
       ts_u32x4 v[E8 ? 2 : 1];
       if constexpr (E8) {
         const int key = pg * 16 + in * 16 / HD, c = in % (HD / 16) * 2;
-        const float ks = scale_of(st_ks[i]);
-        uint32_t u[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x[4];
-          e4m3_to_f32(st_k[i][e], x);
-          u[2 * e] = __builtin_bit_cast(uint32_t, to_bf16x2(x[0] * ks, x[1] * ks));
-          u[2 * e + 1] = __builtin_bit_cast(uint32_t, to_bf16x2(x[2] * ks, x[3] * ks));
-        }
-        sk[slot][key_place(key, c)] = ts_u32x4{u[0], u[1], u[2], u[3]};
-        sk[slot][key_place(key, c + 1)] = ts_u32x4{u[4], u[5], u[6], u[7]};
-        v[0] = widen_values(st_v[i][0], st_v[i][1], st_vs[i][0], st_vs[i][1]);
-        v[1] = widen_values(st_v[i][2], st_v[i][3], st_vs[i][2], st_vs[i][3]);
+        const float ks = scale_at<0>(st.ks[i]);
+        sk[slot][key_place(key, c)] = e4m3_to_bf16(st.k[i][0], st.k[i][1], ks);
+        sk[slot][key_place(key, c + 1)] = e4m3_to_bf16(st.k[i][2], st.k[i][3], ks);
+        v[0] = widen_values(st.v[i][0], st.v[i][1], st.vs[i][0], st.vs[i][1]);
+        v[1] = widen_values(st.v[i][2], st.v[i][3], st.vs[i][2], st.vs[i][3]);
       } else {
-        sk[slot][key_place(pg * 16 + in / (HD / 8), in % (HD / 8))] = st_k[i];
-        v[0] = st_v[i];
+        sk[slot][key_place(pg * 16 + in / (HD / 8), in % (HD / 8))] = st.k[i];
+        v[0] = st.v[i];
       }
 #pragma unroll
       for (int e = 0; e < (E8 ? 2 : 1); ++e) {
@@ -685,33 +659,34 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   if (tid == 0) dirty = 0;
   __syncthreads();
   if (blocks) {
-    Pages next = pages_of(0);
-    int ok = good_bits(next), ok_next;
-    request(next);
-    write(0, whole(0, ok));
+    // Block b + 1 is on its way or in registers while block b is used, and the pages of b + 2 are known.
+    int next = pages_of(0), ok = good_bits(next), ok_next;
+    Stage st;
+    request(st, next, ok);
     next = pages_of(1);
+    write(st, 0, whole(0, ok));
     ok_next = good_bits(next);
-    if (blocks > 1) request(next);
+    request(st, next, ok_next);
     next = pages_of(2);
     __syncthreads();
     for (int b = 0; b < blocks; ++b) {
       if (active) use(b & 1, k0 + b * 64, ok);
-      if (b + 1 < blocks) write(b + 1 & 1, whole(b + 1, ok_next));
-      if (b + 2 < blocks) request(next);
-      __syncthreads();
+      if (b + 1 < blocks) write(st, b + 1 & 1, whole(b + 1, ok_next));
       ok = ok_next;
       ok_next = good_bits(next);
+      request(st, next, ok_next);
       next = pages_of(b + 3);
+      wait_lds();
     }
   }
   // Values that are not finite, in blocks whose keys not every column sees, were left out: here they reach those that do.
   if (blocks && dirty) {
     for (int b = 0; b < blocks; ++b) {
-      const Pages pg = pages_of(b);
-      if (whole(b, good_bits(pg))) continue;
+      const int pg = pages_of(b), ok = good_bits(pg);
+      if (whole(b, ok)) continue;
       for (int u = 0; u < 4; ++u) {
-        const int page = u == 0 ? pg[0] : u == 1 ? pg[1] : u == 2 ? pg[2] : pg[3];
-        if (!good(page)) continue;
+        if (!(ok >> u & 1)) continue;
+        const int page = __builtin_amdgcn_readlane(pg, u);
         const int kb = k0 + b * 64 + u * 16 + 8 * h;
         const int64_t head = (int64_t)page * hkv + kvh;
         ts_u32x4 in;
@@ -775,8 +750,53 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   }
 }
 
-// The join of a row's splits: chunk c of the cache's positions lies at place c % splits.  A workgroup per (row, head), four
-// dimensions a thread, the splits dealt to the rows of threads.
+// The join of a row's splits: chunk c of the cache's positions lies at place c % splits.  Few splits: a wave per (row, head), four
+// dimensions a lane, the splits dealt to the lane groups of a head's length.
+template <typename TQ, int HD>
+__global__ __launch_bounds__(256) void k_kv_attend_rows_join_few(RowsArgs g) {
+  constexpr int COLS = HD / 4, GROUPS = 64 / COLS;
+  const ts_kv_attend_rows_args& a = g.a;
+  const int64_t at = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + threadIdx.x / 64);
+  const int lane = threadIdx.x % 64, row = (int)(at / a.n_q_heads), h = (int)(at % a.n_q_heads);
+  if (row >= a.n_rows) return;
+  int seq = row;
+  if (a.row_offsets) {
+    seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
+    if (seq < 0 || seq >= a.n_seqs || row >= a.row_offsets[seq + 1]) return;
+  } else if (row >= a.n_seqs) {
+    return;
+  }
+  const int2 range = row_range(a, row_seq(a, seq), row);
+  const int c0 = range.x / g.chunk, used = max(1, (range.y + g.chunk - 1) / g.chunk - c0);       // a row that sees nothing: one empty part
+  const float2* ml = reinterpret_cast<const float2*>(g.part_ml) + at * g.splits;
+  const float4* part = reinterpret_cast<const float4*>(g.part_o) + at * g.splits * COLS + lane % COLS;
+  float top = -INFINITY;
+  for (int i = lane; i < used; i += 64) top = fmaxf(top, ml[(c0 + i) % g.splits].x);
+  top = wave_max(top);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int i = lane / COLS; i < used; i += GROUPS) {
+    const int place = (c0 + i) % g.splits;
+    const float2 p = ml[place];
+    const float4 v = part[(int64_t)place * COLS];
+    const float f = __builtin_amdgcn_exp2f(p.x - ref);
+    sum += f * p.y;
+    x[0] += f * v.x; x[1] += f * v.y; x[2] += f * v.z; x[3] += f * v.w;
+  }
+#pragma unroll
+  for (int o = COLS; o < 64; o *= 2) {
+    sum += __shfl_xor(sum, o, 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], o, 64);
+  }
+  if (lane >= COLS) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = sum == 0.f ? 0.f : x[e] / sum;
+  store_n<4>((TQ*)a.out + (int64_t)row * a.out_stride + (int64_t)h * HD + lane * 4, x);
+  if (a.lse && lane == 0) a.lse[at] = sum == 0.f ? -INFINITY : (ref + log2f(sum)) * 0.69314718055994531f;
+}
+
+// Many splits: a workgroup per (row, head), four dimensions a thread, the splits dealt to the rows of threads.
 constexpr int RO_SPLITS = 512;                               // at most, see rows_cut
 template <typename TQ, int HD>
 __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
@@ -790,6 +810,8 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
   if (a.row_offsets) {
     seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
     if (seq < 0 || seq >= a.n_seqs || row >= a.row_offsets[seq + 1]) return;
+  } else if (row >= a.n_seqs) {
+    return;
   }
   const RowSeq rs = row_seq(a, seq);
   const int2 range = row_range(a, rs, row);
@@ -862,15 +884,14 @@ static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
   c.nt = rows_nt(a.n_seqs, a.n_rows, group, a.cache.pages.dtype == TS_DTYPE_F32 || a.dtype == TS_DTYPE_F32);
   const int tm = 16 * c.nt;
   c.slots = a.row_offsets ? (int64_t)a.n_rows * group / tm + a.n_seqs : (int64_t)a.n_seqs * ((group + tm - 1) / tm);
-  const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), unit = a.cache.pages.dtype == TS_DTYPE_E4M3 ? 2 : 1;
-  const int64_t units = (rows_units(a.max_len, a.window) + unit - 1) / unit;
+  const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), units = rows_units(a.max_len, a.window);
   int64_t per = 1;
   if (units * whole > 2 * RO_CUS) {
-    const int64_t want = std::max<int64_t>(1, RO_CUS / whole);
+    const int64_t want = std::max<int64_t>(1, (c.nt == 1 && a.cache.pages.dtype == TS_DTYPE_E4M3 ? 2 : 1) * RO_CUS / whole);
     per = (units + want - 1) / want;
   }
   if (units <= 2) per = units;
-  c.chunk = (int)(per * unit * RO_UNIT);
+  c.chunk = (int)(per * RO_UNIT);
   c.splits = (int)((units + per - 1) / per);
   if (c.splits == 1) c.chunk = 1 << 30;                      // one chunk, wherever a window lies
   else if (a.window > 0) ++c.splits;
@@ -902,6 +923,12 @@ extern "C" ts_status ts_kv_attend_rows_workspace(int32_t n_seqs, int32_t n_rows,
   return TS_OK;
 }
 
+template <typename TQ, int HD>
+static void launch_join(const RowsArgs& g, hipStream_t s) {
+  const int64_t n = (int64_t)g.a.n_rows * g.a.n_q_heads;
+  if (g.splits <= 16) k_kv_attend_rows_join_few<TQ, HD><<<(uint32_t)((n + 3) / 4), 256, 0, s>>>(g);
+  else k_kv_attend_rows_join<TQ, HD><<<(uint32_t)n, 256, 0, s>>>(g);
+}
 template <typename T, typename TQ, int HD>
 static void launch_rows(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
   constexpr int BIG = sizeof(T) == 4 || sizeof(TQ) == 4 ? 2 : 4;
@@ -909,13 +936,13 @@ static void launch_rows(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
   if constexpr (sizeof(T) != 4 && sizeof(TQ) == 2) {
     if (c.nt == 16) {
       k_kv_attend_wide<T, HD><<<grid, RW_WAVES * 64, 0, s>>>(g);
-      if (c.splits > 1) k_kv_attend_rows_join<TQ, HD><<<(uint32_t)(g.a.n_rows * g.a.n_q_heads), 256, 0, s>>>(g);
+      if (c.splits > 1) launch_join<TQ, HD>(g, s);
       return;
     }
   }
   if (c.nt == 1) k_kv_attend_rows<T, TQ, HD, 1><<<grid, RO_WAVES * 64, 0, s>>>(g);
   else k_kv_attend_rows<T, TQ, HD, BIG><<<grid, RO_WAVES * 64, 0, s>>>(g);
-  if (c.splits > 1) k_kv_attend_rows_join<TQ, HD><<<(uint32_t)(g.a.n_rows * g.a.n_q_heads), 256, 0, s>>>(g);
+  if (c.splits > 1) launch_join<TQ, HD>(g, s);
 }
 template <typename TQ>
 static void launch_rows_q(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
