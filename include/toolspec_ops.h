@@ -199,13 +199,13 @@ ts_status ts_kv_append_norm_rope(const ts_kv_append_norm_rope_args* args, ts_str
  * as it is stored (keys rotated), n_kv_heads heads of head_dim, in `dtype` (8-bit values and bf16 widen exactly to fp32 and 8-bit
  * values to bf16, a scale byte of 253 or more aside, whose values may be infinite; fp32 rounds to bf16 once).  starts null: from position 0 on; k_out or
  * v_out may be null.  Rows outside every sequence, and rows whose position is negative, beyond the table or on a page outside [0, n_pages),
- * stay as they were.
+ * stay as they were, or become zeros where zero_rest is not 0.
  * Errors: INVALID_ARG (as above; n_rows in [0, 2^23]), DEVICE. */
 typedef struct {
   ts_kv_pages_any cache;
   const int32_t* table; int64_t table_stride; int32_t table_width;
   const int32_t* starts; const int32_t* row_offsets;
-  int32_t n_seqs, n_rows, dtype;
+  int32_t n_seqs, n_rows, dtype, zero_rest;
   void* k_out; int64_t k_stride;
   void* v_out; int64_t v_stride;
 } ts_kv_read_args;

@@ -48,6 +48,16 @@ __device__ __forceinline__ void to_codes(const float (&x)[VE], uint32_t byte, ui
   for (int e = 0; e < VE; e += 4) w[e / 4] = byte == 255 ? 0x7f7f7f7fu : f32_to_e4m3(x[e] * inv, x[e + 1] * inv, x[e + 2] * inv, x[e + 3] * inv);
 }
 
+// the value of the lane half a row of LPV lanes away
+template <int LPV>
+__device__ __forceinline__ float other_half(float v) {
+  const int u = __float_as_int(v);
+  if constexpr (LPV == 16) return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0x128, 0xf, 0xf, true));         // rotated by 8 within 16
+  else if constexpr (LPV == 4) return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0x4e, 0xf, 0xf, true));      // lanes 2 3 0 1 of four
+  else if constexpr (LPV == 2) return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2 of four
+  else return __shfl_xor(v, LPV / 2, 64);
+}
+
 template <typename TI, typename TC, int HD>
 struct AppendAny {
   static constexpr int VE = sizeof(TI) == 2 ? 8 : 4, LPV = HD / VE, VECS = RA_THREADS / LPV, BATCH = 4, HALF = HD / 2;
@@ -60,16 +70,17 @@ struct AppendAny {
   };
 };
 
-// queries and keys
+// Queries and keys.  A thread keeps its row of the page and its place in the head and goes through the heads, so that its sines are
+// read once; several heads' pieces are requested before the first is worked on.
 template <typename TI, typename TC, int HD>
 __device__ __forceinline__ void any_turned(const AppendAnyArgs& g, const AppendPage& at, AppendAny<TI, TC, HD>& s) {
   typedef AppendAny<TI, TC, HD> S;
-  constexpr int VE = S::VE, LPV = S::LPV, HALF = S::HALF, BATCH = S::BATCH;
+  constexpr int VE = S::VE, LPV = S::LPV, HALF = S::HALF, BATCH = S::BATCH, VECS = S::VECS;
   const ts_kv_append_norm_rope_args& a = g.a;
-  const int tid = threadIdx.x, cnt = at.cnt, n = (min(at.head1, at.hq + at.hkv) - at.head0) * cnt;
-  const int c = tid % LPV, d0 = c * VE, rd = a.rope_dim, rh = rd / 2;
+  const int tid = threadIdx.x, cnt = at.cnt, n = min(at.head1, at.hq + at.hkv) - at.head0;
+  const int lane = tid % 64, c = tid % LPV, d0 = c * VE, rd = a.rope_dim, rh = rd / 2, vec = tid / LPV;
   const bool whole = rd % (2 * VE) == 0;                     // a lane's partners are one lane's
-  float* mine = s.x[tid / 64] + tid % 64 / LPV * HD;
+  float* mine = s.x[tid / 64] + lane / LPV * HD;
   auto gains = [&](const void* p, float (&v)[VE]) {
 #pragma unroll
     for (int e = 0; e < VE; ++e) v[e] = a.norm_dtype == TS_DTYPE_BF16 ? bf16_to_f32(((const bf16_t*)p)[d0 + e]) : ((const float*)p)[d0 + e];
@@ -77,97 +88,101 @@ __device__ __forceinline__ void any_turned(const AppendAnyArgs& g, const AppendP
   float gq[VE], gk[VE];
   if (a.q_norm && at.head0 < at.hq) gains(a.q_norm, gq);
   if (a.k_norm && at.head1 > at.hq) gains(a.k_norm, gk);
-  for (int i0 = 0; i0 < n; i0 += BATCH * S::VECS) {
-    float x[BATCH][VE];
-    int rr[BATCH], hh[BATCH];
+  const int row_step = min(cnt, VECS), head_step = VECS / row_step;                   // rows and heads at once
+  const int r0 = vec % row_step, h0 = vec / row_step;
+  bool first = true;
+  for (int rb = 0; rb < cnt; rb += row_step) {
+    const int r = min(rb + r0, cnt - 1);
+    const int64_t row = at.row + r;
+    float cs[VE], sn[VE];
+    for (int hb = 0; hb < n; hb += BATCH * head_step) {
+      float x[BATCH][VE];
 #pragma unroll
-    for (int b = 0; b < BATCH; ++b) {
-      if (i0 + b * S::VECS >= n) break;
-      const int i = min(i0 + b * S::VECS + tid / LPV, n - 1);
-      hh[b] = i / cnt;
-      rr[b] = i - hh[b] * cnt;
-      hh[b] += at.head0;
-      const int64_t row = at.row + rr[b];
-      load_n<VE>((hh[b] < at.hq ? (const TI*)a.q + row * a.q_stride + (int64_t)hh[b] * HD : (const TI*)a.k + row * a.k_stride + (int64_t)(hh[b] - at.hq) * HD) + d0, x[b]);
-    }
-    if (g.turn && i0 == 0) {
-      for (int i = tid; i < cnt * rh; i += RA_THREADS) {
-        const int r = i / rh, j = i - r * rh;
-        const int64_t p = a.positions ? a.positions[at.row + r] : at.pos + r;
-        const double t = s.freq[j] * (double)p, rest = t - rint(t);
-        float sn, cn;
-        sincospif(2.f * (float)rest, &sn, &cn);
-        s.cs[r * HALF + j] = make_float2(cn * a.rope_magnitude, sn * a.rope_magnitude);
+      for (int b = 0; b < BATCH; ++b) {
+        if (hb + b * head_step >= n) break;
+        const int h = at.head0 + min(hb + b * head_step + h0, n - 1);
+        load_n<VE>((h < at.hq ? (const TI*)a.q + row * a.q_stride + (int64_t)h * HD : (const TI*)a.k + row * a.k_stride + (int64_t)(h - at.hq) * HD) + d0, x[b]);
       }
-      __syncthreads();
-    }
-#pragma unroll
-    for (int b = 0; b < BATCH; ++b) {
-      if (i0 + b * S::VECS >= n) break;
-      const bool is_q = hh[b] < at.hq;
-      float (&v)[VE] = x[b];
-      if (is_q ? a.q_norm != nullptr : a.k_norm != nullptr) {      // all lanes of a row go one way
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < VE; ++e) ss += v[e] * v[e];
-        const float rs = 1.f / sqrtf(sum_over<LPV>(ss) * (1.f / HD) + a.norm_eps);
-#pragma unroll
-        for (int e = 0; e < VE; ++e) v[e] = v[e] * rs * (is_q ? gq[e] : gk[e]);
+      if (g.turn && first) {                                 // while the first pieces come
+        for (int i = tid; i < cnt * rh; i += RA_THREADS) {
+          const int ri = i / rh, j = i - ri * rh;
+          const int64_t p = a.positions ? a.positions[at.row + ri] : at.pos + ri;
+          const double t = s.freq[j] * (double)p, rest = t - rint(t);
+          float si, co;
+          sincospif(2.f * (float)rest, &si, &co);
+          s.cs[ri * HALF + j] = make_float2(co * a.rope_magnitude, si * a.rope_magnitude);
+        }
+        __syncthreads();
       }
-      if (g.turn) {
-        const float2* cs = s.cs + rr[b] * HALF;
-        if (a.rope_pairs) {
+      first = false;
+      if (g.turn && hb == 0) {                               // y = x cs + partner sn
 #pragma unroll
-          for (int e = 0; e < VE; e += 2) {
-            if (d0 + e >= rd) break;
-            const float2 w = cs[(d0 + e) / 2];
-            const float u = v[e] * w.x - v[e + 1] * w.y;
-            v[e + 1] = v[e + 1] * w.x + v[e] * w.y;
-            v[e] = u;
+        for (int e = 0; e < VE; ++e) {
+          const int d = d0 + e, j = a.rope_pairs ? d / 2 : d < rh ? d : d - rh;
+          const float2 w = d < rd ? s.cs[r * HALF + j] : make_float2(1.f, 0.f);
+          cs[e] = w.x;
+          sn[e] = (a.rope_pairs ? e % 2 == 0 : d < rh) ? -w.y : w.y;
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        if (hb + b * head_step >= n) break;
+        const int hi = hb + b * head_step + h0, h = at.head0 + min(hi, n - 1);
+        const bool is_q = h < at.hq, there = hi < n && rb + r0 < cnt && h0 < head_step;
+        float (&v)[VE] = x[b];
+        if (a.q_norm || a.k_norm) {
+          const bool normed = is_q ? a.q_norm != nullptr : a.k_norm != nullptr;      // all lanes of a row go one way
+          float ss = 0.f;
+#pragma unroll
+          for (int e = 0; e < VE; ++e) ss += v[e] * v[e];
+          const float rs = 1.f / sqrtf(sum_over<LPV>(ss) * (1.f / HD) + a.norm_eps);
+          if (normed) {
+#pragma unroll
+            for (int e = 0; e < VE; ++e) v[e] = v[e] * rs * (is_q ? gq[e] : gk[e]);
           }
-        } else {
-          // one wave writes and reads here, and its LDS accesses are done in order
+        }
+        if (g.turn) {
+          float o[VE];                                       // the partners
+          if (a.rope_pairs) {
 #pragma unroll
-          for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4*>(mine + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-          __builtin_amdgcn_wave_barrier();
-          asm volatile("" ::: "memory");
-          if (whole && d0 < rd) {
-            const bool low = d0 < rh;
-            const float* other = mine + (low ? d0 + rh : d0 - rh);
-            const float2* w = cs + (low ? d0 : d0 - rh);
+            for (int e = 0; e < VE; ++e) o[e] = v[e ^ 1];
+          } else if (whole && rd == HD && LPV > 1) {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) v[e] = v[e] * w[e].x + (low ? -other[e] : other[e]) * w[e].y;
-          } else if (!whole) {
+            for (int e = 0; e < VE; ++e) o[e] = other_half<LPV>(v[e]);
+          } else {
+            // one wave writes and reads here, and its LDS accesses are done in order
+#pragma unroll
+            for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4*>(mine + d0 + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
               const int d = d0 + e;
-              if (d >= rd) break;
-              const bool low = d < rh;
-              const float2 w = cs[low ? d : d - rh];
-              const float o = mine[low ? d + rh : d - rh];
-              v[e] = v[e] * w.x + (low ? -o : o) * w.y;
+              o[e] = d < rd ? mine[d < rh ? d + rh : d - rh] : 0.f;
             }
+            __builtin_amdgcn_wave_barrier();
+            asm volatile("" ::: "memory");
           }
-          __builtin_amdgcn_wave_barrier();
-          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int e = 0; e < VE; ++e)                       // beyond rope_dim the value itself, whatever lies in the other lane
+            v[e] = d0 + e < rd ? v[e] * cs[e] + o[e] * sn[e] : v[e];
         }
-      }
-      const bool there = i0 + b * S::VECS + tid / LPV < n;
-      if constexpr (S::E8) {
-        const uint32_t byte = scale_byte(top_bits<LPV>(v));
-        if (there && !is_q) {
-          const int64_t at16 = ((int64_t)at.page * at.hkv + (hh[b] - at.hq)) * 16 + at.slot + rr[b];
-          uint32_t w[VE / 4];
-          to_codes(v, byte, w);
-          uint8_t* dst = (uint8_t*)a.cache.pages.k + at16 * HD + d0;
-          if constexpr (VE == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-          else *reinterpret_cast<uint32_t*>(dst) = w[0];
-          if (c == 0) a.cache.k_scales[at16] = (uint8_t)byte;
+        if constexpr (S::E8) {
+          const uint32_t byte = scale_byte(top_bits<LPV>(v));
+          if (there && !is_q) {
+            const int64_t at16 = ((int64_t)at.page * at.hkv + (h - at.hq)) * 16 + at.slot + r;
+            uint32_t w[VE / 4];
+            to_codes(v, byte, w);
+            uint8_t* dst = (uint8_t*)a.cache.pages.k + at16 * HD + d0;
+            if constexpr (VE == 8) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t*>(dst) = w[0];
+            if (c == 0) a.cache.k_scales[at16] = (uint8_t)byte;
+          }
+        } else if (there && !is_q) {
+          store_n<VE>((TC*)a.cache.pages.k + (((int64_t)at.page * at.hkv + (h - at.hq)) * 16 + at.slot + r) * HD + d0, v);
         }
-      } else if (there && !is_q) {
-        store_n<VE>((TC*)a.cache.pages.k + (((int64_t)at.page * at.hkv + (hh[b] - at.hq)) * 16 + at.slot + rr[b]) * HD + d0, v);
+        if (there && is_q) store_n<VE>((TI*)a.q_out + row * a.q_out_stride + (int64_t)h * HD + d0, v);
       }
-      if (there && is_q) store_n<VE>((TI*)a.q_out + (int64_t)(at.row + rr[b]) * a.q_out_stride + (int64_t)hh[b] * HD + d0, v);
     }
   }
 }
@@ -298,18 +313,27 @@ __global__ __launch_bounds__(RA_THREADS) void k_kv_read(ReadArgs g) {
   const int tid = threadIdx.x, hkv = a.cache.pages.n_kv_heads;
   const int head0 = blockIdx.y * RA_HEADS, head1 = min(head0 + RA_HEADS, 2 * hkv);
   const int window1 = min((int)(blockIdx.x + 1) * g.window, a.n_rows);
+  auto none = [&](int row0, int rows) {                      // rows that are no position
+    if (!a.zero_rest) return;
+    for (int i = tid; i < rows * (head1 - head0) * HD; i += RA_THREADS) {
+      const int d = i % HD, hr = i / HD, h = head0 + hr % (head1 - head0), r = hr / (head1 - head0);
+      if (h < hkv) { if (a.k_out) st_from_f32((TO*)a.k_out + (int64_t)(row0 + r) * a.k_stride + (int64_t)h * HD + d, 0.f); }
+      else if (a.v_out) st_from_f32((TO*)a.v_out + (int64_t)(row0 + r) * a.v_stride + (int64_t)(h - hkv) * HD + d, 0.f);
+    }
+  };
   for (int row = blockIdx.x * g.window, cnt; row < window1; row += cnt) {
     cnt = 1;
     const int seq = seq_of_row(a.row_offsets, a.n_seqs + 1, row);
-    if (seq < 0 || seq >= a.n_seqs) continue;
+    if (seq < 0 || seq >= a.n_seqs) { none(row, 1); continue; }
     const int first = a.row_offsets[seq], end = min(a.row_offsets[seq + 1], a.n_rows);
     const int64_t pos = (a.starts ? (int64_t)a.starts[seq] : 0) + row - first;
-    if (pos < 0 || row >= end) continue;
+    if (pos < 0 || row >= end) { none(row, 1); continue; }
     const int slot = (int)(pos & 15);
     cnt = min(16 - slot, end - row);
-    if ((row != max(first, 0) && slot != 0) || pos >= (int64_t)a.table_width * 16) continue;
+    if (row != max(first, 0) && slot != 0) continue;         // another window's
+    if (pos >= (int64_t)a.table_width * 16) { none(row, cnt); continue; }
     const int page = a.table[(int64_t)seq * a.table_stride + pos / 16];
-    if (page < 0 || page >= a.cache.pages.n_pages) continue;
+    if (page < 0 || page >= a.cache.pages.n_pages) { none(row, cnt); continue; }
     if (a.k_out && head0 < hkv) {
       const int n = (min(head1, hkv) - head0) * cnt * PIECES;
       for (int i = tid; i < n; i += RA_THREADS) {

@@ -64,9 +64,9 @@ __device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int o
 __device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int seq) {
   return a.row_offsets ? row_seq(a, a.row_offsets[seq], a.row_offsets[seq + 1], a.lengths[seq]) : row_seq(a, seq, seq + 1, a.lengths[seq]);
 }
-// The sequence of a tile of `tm` columns and its first column, -1 if there is none.  Sequence s has tile slots [off group / tm + s, ...): as
+// The sequence of a tile of at most `tm` columns, its first column and their number; -1 if there is none.  Sequence s has tile slots [off group / tm + s, ...): as
 // many as its tiles or one more, without a sum over the others.
-__device__ __forceinline__ int tile_of(const RowsArgs& g, int t, int tm, int64_t& m0, RowSeq& rs) {
+__device__ __forceinline__ int tile_of(const RowsArgs& g, int t, int tm, int unit, int64_t& m0, int& cols, RowSeq& rs) {
   const ts_kv_attend_rows_args& a = g.a;
   int seq;
   if (!a.row_offsets) {
@@ -89,7 +89,14 @@ __device__ __forceinline__ int tile_of(const RowsArgs& g, int t, int tm, int64_t
       rs = row_seq(a, seq);
     }
   }
-  return m0 < (int64_t)(rs.end - rs.first) * g.group ? seq : -1;
+  // the columns go to as many tiles as they need, in units of `unit`, evenly
+  const int64_t M = (int64_t)(rs.end - rs.first) * g.group;
+  if (m0 >= M) return -1;
+  const int64_t tiles = (M + tm - 1) / tm;
+  const int step = (int)((M + tiles * unit - 1) / (tiles * unit)) * unit;
+  m0 = m0 / tm * step;
+  cols = (int)min((int64_t)step, M - m0);
+  return cols > 0 ? seq : -1;
 }
 // positions [lo, hi) that a row can see (with ancestors: some of them)
 __device__ __forceinline__ int2 row_range(const ts_kv_attend_rows_args& a, const RowSeq& s, int row) {
@@ -130,10 +137,10 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
   const int split = id % g.splits, t = id / g.splits, G = g.group;
   int64_t m0;
   RowSeq rs;
-  const int seq = tile_of(g, t, TM, m0, rs);
+  int cols;
+  const int seq = tile_of(g, t, TM, 16, m0, cols, rs);
   if (seq < 0) return;
-  const int64_t M = (int64_t)(rs.end - rs.first) * G;
-  const int cols = (int)min((int64_t)TM, M - m0), row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
+  const int row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
   const int2 low = row_range(a, rs, row0), high = row_range(a, rs, row0 + (rem + cols - 1) / G);
   const int lo = low.x, hi = high.y;                         // what any column sees, and what all do
   const int all_lo = high.x, all_hi = a.ancestors ? min(max(rs.start + 1, 0), low.y) : low.y;
@@ -464,12 +471,12 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
 // swapped.  Blocks go through registers (8-bit ones are widened there, times their scales, once for all waves) into two LDS slots: while
 // block b is used, b + 1 is written and b + 2 and b + 3 are on their way; one barrier a block.
 // ---------------------------------------------------------------------------------
-constexpr int RW_WAVES = 8, RW_TM = RW_WAVES * 32;
 typedef float ts_f32x16 __attribute__((ext_vector_type(16)));
 
-template <typename T, int HD>
+template <typename T, int HD, int RW_WAVES>
 __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g) {
   constexpr bool E8 = sizeof(T) == 1;
+  constexpr int RW_TM = RW_WAVES * 32;
   constexpr int DT = HD / 32, KS = HD / 16, PAGE = 16 * HD;               // tiles of 32 dimensions, steps of 16, elements of a page and head
   constexpr int RING = 2, LOADS = (4 * PAGE * (int)sizeof(T) + 16 * RW_WAVES * 64 - 1) / (16 * RW_WAVES * 64);      // 16-byte loads of a thread for keys, and for values
   constexpr int PER_PAGE = PAGE * (int)sizeof(T) / 16;                    // 16-byte pieces of a page
@@ -484,10 +491,10 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   const int split = id % g.splits, t = id / g.splits, G = g.group;
   int64_t m0;
   RowSeq rs;
-  const int seq = tile_of(g, t, RW_TM, m0, rs);
+  int cols;
+  const int seq = tile_of(g, t, RW_TM, 32, m0, cols, rs);
   if (seq < 0) return;
-  const int64_t M = (int64_t)(rs.end - rs.first) * G;
-  const int cols = (int)min((int64_t)RW_TM, M - m0), row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
+  const int row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
   const int lo = row_range(a, rs, row0).x, hi = row_range(a, rs, row0 + (rem + cols - 1) / G).y;
   const int64_t from = ((int64_t)(lo / g.chunk) + split) * g.chunk;
   if (split > 0 && from >= hi) return;
@@ -861,10 +868,10 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
 // ---------------------------------------------------------------------------------
 constexpr int RO_CUS = 256, RO_UNIT = 128;
 
-struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup (16: the wide kernel), keys of a split, splits, tile slots per KV head
+struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup (8 and 16: the wide kernel), keys of a split, splits, tile slots per KV head
 
 // Tiles of 16 columns where a sequence has no more, of 64 (fp32: 32) where it has.
-static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 128 ? 4 : 16; }
+static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 64 ? 4 : n_rows * group <= n_seqs * 512 ? 8 : 16; }
 static int64_t rows_units(int max_len, int window) {         // of 128 keys, in what one tile sees
   const int64_t span = window > 0 && (int64_t)window + 256 < max_len ? window + 256 : max_len;
   return std::max<int64_t>(1, (span + RO_UNIT - 1) / RO_UNIT);
@@ -875,7 +882,7 @@ static int64_t rows_whole(int64_t n_seqs, int64_t n_rows, int group, int hkv, in
 }
 static int64_t rows_room(int64_t n_seqs, int64_t n_rows, int group, int hkv, int max_len, int window) {
   int64_t room = 1;
-  for (int nt : {1, 2, 4, 16}) room = std::max(room, std::min(rows_units(max_len, window), 2 * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
+  for (int nt : {1, 2, 4, 8, 16}) room = std::max(room, std::min(rows_units(max_len, window), 2 * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
   return room > 1 && window > 0 ? room + 1 : room;
 }
 static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
@@ -887,7 +894,7 @@ static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
   const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), units = rows_units(a.max_len, a.window);
   int64_t per = 1;
   if (units * whole > 2 * RO_CUS) {
-    const int64_t want = std::max<int64_t>(1, (c.nt == 1 && a.cache.pages.dtype == TS_DTYPE_E4M3 ? 2 : 1) * RO_CUS / whole);
+    const int64_t want = std::max<int64_t>(1, ((c.nt == 1 && a.cache.pages.dtype == TS_DTYPE_E4M3) || c.nt == 8 ? 2 : 1) * RO_CUS / whole);
     per = (units + want - 1) / want;
   }
   if (units <= 2) per = units;
@@ -934,8 +941,9 @@ static void launch_rows(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
   constexpr int BIG = sizeof(T) == 4 || sizeof(TQ) == 4 ? 2 : 4;
   const uint32_t grid = (uint32_t)(c.slots * g.a.cache.pages.n_kv_heads * c.splits);
   if constexpr (sizeof(T) != 4 && sizeof(TQ) == 2) {
-    if (c.nt == 16) {
-      k_kv_attend_wide<T, HD><<<grid, RW_WAVES * 64, 0, s>>>(g);
+    if (c.nt >= 8) {
+      if (c.nt == 8) k_kv_attend_wide<T, HD, 4><<<grid, 256, 0, s>>>(g);
+      else k_kv_attend_wide<T, HD, 8><<<grid, 512, 0, s>>>(g);
       if (c.splits > 1) launch_join<TQ, HD>(g, s);
       return;
     }

@@ -60,7 +60,7 @@ class ts_kv_append_norm_rope_args(C.Structure):
 
 class ts_kv_read_args(C.Structure):
     _fields_ = [("cache", ts_kv_pages_any), ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int32),
-                ("starts", C.c_void_p), ("row_offsets", C.c_void_p), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("dtype", C.c_int32),
+                ("starts", C.c_void_p), ("row_offsets", C.c_void_p), ("n_seqs", C.c_int32), ("n_rows", C.c_int32), ("dtype", C.c_int32), ("zero_rest", C.c_int32),
                 ("k_out", C.c_void_p), ("k_stride", C.c_int64), ("v_out", C.c_void_p), ("v_stride", C.c_int64)]
 
 
@@ -477,9 +477,9 @@ def ts_kv_read(k_pages, v_pages, table, starts, row_offsets, n_rows, dtype=torch
     p_table, t_stride, t_width = _table(table, n)
     if n_rows < 0:
         _refuse("n_rows: %d", n_rows)
-    if k_out is None and v_out is None:
-        both = torch.zeros((2, n_rows, width), dtype=dtype, device=table.device)
-        k_out, v_out = both[0], both[1]
+    own = k_out is None and v_out is None
+    if own:
+        k_out, v_out = table.new_empty((2, n_rows, width), dtype=dtype).unbind()
     at = []
     for t, name in ((k_out, "k_out"), (v_out, "v_out")):
         if t is None:
@@ -490,7 +490,7 @@ def ts_kv_read(k_pages, v_pages, table, starts, row_offsets, n_rows, dtype=torch
             _refuse("%s: %d rows are needed, got %d", name, n_rows, t.shape[0])
     try:
         a = _pack_read(*pages, p_table, t_stride, t_width, 0 if starts is None else _ints(starts, "starts", n), _ints(row_offsets, "row_offsets", 2), n, n_rows,
-                       _DTYPES[dtype], *at)
+                       _DTYPES[dtype], own, *at)
     except struct.error as e:
         _out_of_range(e)
     binding._check(lib.ts_kv_read(a, _stream(table)))
