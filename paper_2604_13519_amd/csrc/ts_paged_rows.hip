@@ -19,6 +19,7 @@
 // so that they reach the rows that see them and no other.
 // ---------------------------------------------------------------------------------
 constexpr int RO_WAVES = 4;
+constexpr int RO_CUS = 256, RO_UNIT = 128, RO_MOST = 2;    // RO_MOST: workgroups a CU that a call is split into, at most
 
 struct RowsArgs {
   ts_kv_attend_rows_args a;
@@ -782,6 +783,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join_few(RowsArgs g) {
   top = wave_max(top);
   const float ref = top == -INFINITY ? 0.f : top;
   float sum = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int i = lane / COLS; i < used; i += GROUPS) {
     const int place = (c0 + i) % g.splits;
     const float2 p = ml[place];
@@ -804,7 +806,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join_few(RowsArgs g) {
 }
 
 // Many splits: a workgroup per (row, head), four dimensions a thread, the splits dealt to the rows of threads.
-constexpr int RO_SPLITS = 512;                               // at most, see rows_cut
+constexpr int RO_SPLITS = RO_MOST * RO_CUS;                  // at most, see rows_cut; a window may add one
 template <typename TQ, int HD>
 __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
   constexpr int COLS = HD / 4, ROWS = 256 / COLS;
@@ -866,12 +868,11 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
 // ---------------------------------------------------------------------------------
 // entry points
 // ---------------------------------------------------------------------------------
-constexpr int RO_CUS = 256, RO_UNIT = 128;
 
 struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup (8 and 16: the wide kernel), keys of a split, splits, tile slots per KV head
 
 // Tiles of 16 columns where a sequence has no more, of 64 (fp32: 32) where it has.
-static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 64 ? 4 : n_rows * group <= n_seqs * 512 ? 8 : 16; }
+static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 512 ? 8 : 16; }
 static int64_t rows_units(int max_len, int window) {         // of 128 keys, in what one tile sees
   const int64_t span = window > 0 && (int64_t)window + 256 < max_len ? window + 256 : max_len;
   return std::max<int64_t>(1, (span + RO_UNIT - 1) / RO_UNIT);
@@ -882,7 +883,7 @@ static int64_t rows_whole(int64_t n_seqs, int64_t n_rows, int group, int hkv, in
 }
 static int64_t rows_room(int64_t n_seqs, int64_t n_rows, int group, int hkv, int max_len, int window) {
   int64_t room = 1;
-  for (int nt : {1, 2, 4, 8, 16}) room = std::max(room, std::min(rows_units(max_len, window), 2 * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
+  for (int nt : {1, 2, 8, 16}) room = std::max(room, std::min(rows_units(max_len, window), RO_MOST * RO_CUS / std::max<int64_t>(1, rows_whole(n_seqs, n_rows, group, hkv, nt))));
   return room > 1 && window > 0 ? room + 1 : room;
 }
 static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
@@ -893,8 +894,9 @@ static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
   c.slots = a.row_offsets ? (int64_t)a.n_rows * group / tm + a.n_seqs : (int64_t)a.n_seqs * ((group + tm - 1) / tm);
   const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), units = rows_units(a.max_len, a.window);
   int64_t per = 1;
-  if (units * whole > 2 * RO_CUS) {
-    const int64_t want = std::max<int64_t>(1, ((c.nt == 1 && a.cache.pages.dtype == TS_DTYPE_E4M3) || c.nt == 8 ? 2 : 1) * RO_CUS / whole);
+  const int a_cu = (c.nt == 1 && a.cache.pages.dtype == TS_DTYPE_E4M3) || c.nt == 8 ? 2 : 1;
+  if (units * whole > RO_MOST * RO_CUS) {
+    const int64_t want = std::max<int64_t>(1, std::min(a_cu, RO_MOST) * RO_CUS / whole);
     per = (units + want - 1) / want;
   }
   if (units <= 2) per = units;
@@ -933,23 +935,16 @@ extern "C" ts_status ts_kv_attend_rows_workspace(int32_t n_seqs, int32_t n_rows,
 template <typename TQ, int HD>
 static void launch_join(const RowsArgs& g, hipStream_t s) {
   const int64_t n = (int64_t)g.a.n_rows * g.a.n_q_heads;
-  if (g.splits <= 16) k_kv_attend_rows_join_few<TQ, HD><<<(uint32_t)((n + 3) / 4), 256, 0, s>>>(g);
+  if (g.splits <= (n >= 1024 ? 64 : 16)) k_kv_attend_rows_join_few<TQ, HD><<<(uint32_t)((n + 3) / 4), 256, 0, s>>>(g);
   else k_kv_attend_rows_join<TQ, HD><<<(uint32_t)n, 256, 0, s>>>(g);
 }
 template <typename T, typename TQ, int HD>
 static void launch_rows(const RowsArgs& g, const RowsCut& c, hipStream_t s) {
-  constexpr int BIG = sizeof(T) == 4 || sizeof(TQ) == 4 ? 2 : 4;
   const uint32_t grid = (uint32_t)(c.slots * g.a.cache.pages.n_kv_heads * c.splits);
-  if constexpr (sizeof(T) != 4 && sizeof(TQ) == 2) {
-    if (c.nt >= 8) {
-      if (c.nt == 8) k_kv_attend_wide<T, HD, 4><<<grid, 256, 0, s>>>(g);
-      else k_kv_attend_wide<T, HD, 8><<<grid, 512, 0, s>>>(g);
-      if (c.splits > 1) launch_join<TQ, HD>(g, s);
-      return;
-    }
-  }
   if (c.nt == 1) k_kv_attend_rows<T, TQ, HD, 1><<<grid, RO_WAVES * 64, 0, s>>>(g);
-  else k_kv_attend_rows<T, TQ, HD, BIG><<<grid, RO_WAVES * 64, 0, s>>>(g);
+  else if constexpr (sizeof(T) == 4 || sizeof(TQ) == 4) k_kv_attend_rows<T, TQ, HD, 2><<<grid, RO_WAVES * 64, 0, s>>>(g);
+  else if (c.nt == 8) k_kv_attend_wide<T, HD, 4><<<grid, 256, 0, s>>>(g);
+  else k_kv_attend_wide<T, HD, 8><<<grid, 512, 0, s>>>(g);
   if (c.splits > 1) launch_join<TQ, HD>(g, s);
 }
 template <typename TQ>
@@ -985,6 +980,7 @@ extern "C" ts_status ts_kv_attend_rows(const ts_kv_attend_rows_args* args, ts_st
   if (c.splits > 1) {
     uint64_t need = 0;
     if ((st = ts_kv_attend_rows_workspace(a.n_seqs, a.n_rows, a.n_q_heads, p.n_kv_heads, p.head_dim, a.max_len, a.window, &need))) return st;
+    need = std::max(need, (uint64_t)a.n_rows * a.n_q_heads * c.splits * (p.head_dim + 2) * 4);           // what the kernels write: never beyond the bytes given
     if (!a.workspace || a.workspace_bytes < need || !aligned_to(a.workspace, 16))
       return ts_fail(TS_ERR_INVALID_ARG, "%s: needs a 16-byte aligned workspace of %llu bytes, got %llu", call, (unsigned long long)need, (unsigned long long)a.workspace_bytes);
   }
