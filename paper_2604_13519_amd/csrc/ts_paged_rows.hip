@@ -65,39 +65,58 @@ __device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int o
 __device__ __forceinline__ RowSeq row_seq(const ts_kv_attend_rows_args& a, int seq) {
   return a.row_offsets ? row_seq(a, a.row_offsets[seq], a.row_offsets[seq + 1], a.lengths[seq]) : row_seq(a, seq, seq + 1, a.lengths[seq]);
 }
-// The sequence of a tile of at most `tm` columns, its first column and their number; -1 if there is none.  Sequence s has tile slots [off group / tm + s, ...): as
-// many as its tiles or one more, without a sum over the others.
-__device__ __forceinline__ int tile_of(const RowsArgs& g, int t, int tm, int unit, int64_t& m0, int& cols, RowSeq& rs) {
+// The sequence of the t-th tile of at most TM columns, its first column and their number; -1 if there is none.  A sequence's columns go
+// to as many tiles as they need, evenly in units of UNIT, its last rows first, and the sequences with the highest positions
+// come first (up to 16 of them): what takes longest starts first.  (rows x heads of a call are below 2^24.)
+template <int TM, int UNIT>
+__device__ __forceinline__ int tile_of(const RowsArgs& g, int t, int& m0, int& cols, RowSeq& rs) {
   const ts_kv_attend_rows_args& a = g.a;
-  int seq;
+  const int G = g.group;
+  int seq, tile;                                             // the tile of the sequence
   if (!a.row_offsets) {
     seq = t / g.seq_tiles;
-    m0 = (int64_t)(t - seq * g.seq_tiles) * tm;
+    tile = t - seq * g.seq_tiles;
     rs = row_seq(a, seq);
-  } else {
-    auto slot = [&](int off, int s) { return (int64_t)min(max(off, 0), a.n_rows) * g.group / tm + s; };
-    if (a.n_seqs < 64) {                                     // offsets and lengths in one trip to memory
-      const int lane = threadIdx.x % 64, off = a.row_offsets[min(lane, a.n_seqs)], len = a.lengths[min(lane, a.n_seqs - 1)];
-      seq = __popcll(__ballot(lane < a.n_seqs && slot(off, lane) <= t)) - 1;
-      if (seq < 0) return -1;
-      const int first = __builtin_amdgcn_readlane(off, seq);
-      m0 = (t - slot(first, seq)) * tm;
-      rs = row_seq(a, first, __builtin_amdgcn_readlane(off, seq + 1), __builtin_amdgcn_readlane(len, seq));
+  } else if (a.n_seqs < 64) {                                // offsets and lengths in one trip to memory
+    const int lane = threadIdx.x % 64, off = a.row_offsets[min(lane, a.n_seqs)], len = a.lengths[min(lane, a.n_seqs - 1)];
+    const int end = __shfl_down(off, 1, 64);
+    const int rows = lane < a.n_seqs ? max(0, max(min(end, a.n_rows), 0) - min(max(off, 0), a.n_rows)) : 0, tiles = (rows * G + TM - 1) / TM;
+    int before = 0;                                          // tiles of the sequences that come first
+    if (a.n_seqs <= 16) {
+      const int64_t top = (int64_t)len + rows;
+      const int key = (int)max((int64_t)0, min(top, (int64_t)1 << 30));
+      for (int i = 0; i < a.n_seqs; ++i) {
+        const int k = __builtin_amdgcn_readlane(key, i), n = __builtin_amdgcn_readlane(tiles, i);
+        before += k > key || (k == key && i < lane) ? n : 0;
+      }
     } else {
-      seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, [&](int s) { return slot(a.row_offsets[s], s); }));
-      if (seq < 0) return -1;
-      m0 = (t - slot(a.row_offsets[seq], seq)) * tm;
-      rs = row_seq(a, seq);
+      before = tiles;
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) {
+        const int x = __shfl_up(before, o, 64);
+        before += lane >= o ? x : 0;
+      }
+      before -= tiles;
     }
+    const uint64_t in = __ballot(t >= before && t - before < tiles);
+    if (!in) return -1;
+    seq = __builtin_ctzll(in);
+    tile = t - __builtin_amdgcn_readlane(before, seq);
+    rs = row_seq(a, __builtin_amdgcn_readlane(off, seq), __builtin_amdgcn_readlane(end, seq), __builtin_amdgcn_readlane(len, seq));
+  } else {
+    // sequence s has places [off group / TM + s, ...): as many as its tiles or one more, without a sum over the others
+    auto place = [&](int s) { return min(max(a.row_offsets[s], 0), a.n_rows) * G / TM + s; };
+    seq = __builtin_amdgcn_readfirstlane(last_at_most(a.n_seqs, t, place));
+    if (seq < 0) return -1;
+    tile = t - place(seq);
+    rs = row_seq(a, seq);
   }
-  // the columns go to as many tiles as they need, in units of `unit`, evenly
-  const int64_t M = (int64_t)(rs.end - rs.first) * g.group;
-  if (m0 >= M) return -1;
-  const int64_t tiles = (M + tm - 1) / tm;
-  const int step = (int)((M + tiles * unit - 1) / (tiles * unit)) * unit;
-  m0 = m0 / tm * step;
-  cols = (int)min((int64_t)step, M - m0);
-  return cols > 0 ? seq : -1;
+  const int M = (rs.end - rs.first) * G, tiles = (M + TM - 1) / TM;
+  if (tile >= tiles) return -1;
+  const int step = (M + tiles * UNIT - 1) / (tiles * UNIT) * UNIT;
+  m0 = (tiles - 1 - tile) * step;
+  cols = min(step, M - m0);
+  return seq;
 }
 // positions [lo, hi) that a row can see (with ancestors: some of them)
 __device__ __forceinline__ int2 row_range(const ts_kv_attend_rows_args& a, const RowSeq& s, int row) {
@@ -136,12 +155,11 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
   int id = blockIdx.x;
   const int hkv = pages.n_kv_heads, kvh = id % hkv; id /= hkv;
   const int split = id % g.splits, t = id / g.splits, G = g.group;
-  int64_t m0;
+  int m0, cols;
   RowSeq rs;
-  int cols;
-  const int seq = tile_of(g, t, TM, 16, m0, cols, rs);
+  const int seq = tile_of<TM, 16>(g, t, m0, cols, rs);
   if (seq < 0) return;
-  const int row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
+  const int row0 = rs.first + m0 / G, rem = m0 % G;
   const int2 low = row_range(a, rs, row0), high = row_range(a, rs, row0 + (rem + cols - 1) / G);
   const int lo = low.x, hi = high.y;                         // what any column sees, and what all do
   const int all_lo = high.x, all_hi = a.ancestors ? min(max(rs.start + 1, 0), low.y) : low.y;
@@ -487,15 +505,14 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   const ts_kv_attend_rows_args& a = g.a;
   const ts_kv_pages& pages = a.cache.pages;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 32, h = lane / 32;
-  int id = gridDim.x - 1 - blockIdx.x;                       // the last tiles of a chunk see most
+  int id = blockIdx.x;
   const int hkv = pages.n_kv_heads, kvh = id % hkv; id /= hkv;
   const int split = id % g.splits, t = id / g.splits, G = g.group;
-  int64_t m0;
+  int m0, cols;
   RowSeq rs;
-  int cols;
-  const int seq = tile_of(g, t, RW_TM, 32, m0, cols, rs);
+  const int seq = tile_of<RW_TM, 32>(g, t, m0, cols, rs);
   if (seq < 0) return;
-  const int row0 = rs.first + (int)(m0 / G), rem = (int)(m0 % G);
+  const int row0 = rs.first + m0 / G, rem = m0 % G;
   const int lo = row_range(a, rs, row0).x, hi = row_range(a, rs, row0 + (rem + cols - 1) / G).y;
   const int64_t from = ((int64_t)(lo / g.chunk) + split) * g.chunk;
   if (split > 0 && from >= hi) return;
