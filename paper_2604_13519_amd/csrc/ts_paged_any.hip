@@ -21,17 +21,28 @@ struct AppendAnyArgs {
   bool turn;                             // rope_dim > 0 and frequencies that are not all zero
 };
 
-template <int LPV>
-__device__ __forceinline__ float sum_over(float v) {
-#pragma unroll
-  for (int o = LPV / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+// Rows of LPV lanes (2 .. 32) are reduced without the LDS: within four lanes, within 8 and 16 by their mirrors, and 32 by a swap.
+template <int CTRL> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ uint32_t other_16(uint32_t v) {    // of lane l ^ 16
+  const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return threadIdx.x & 16 ? x[0] : x[1];
+}
+template <int LPV, typename F>
+__device__ __forceinline__ uint32_t over(uint32_t v, F join) {
+  if constexpr (LPV > 1) v = join(v, moved<0xb1>(v));
+  if constexpr (LPV > 2) v = join(v, moved<0x4e>(v));
+  if constexpr (LPV > 4) v = join(v, moved<0x141>(v));
+  if constexpr (LPV > 8) v = join(v, moved<0x140>(v));
+  if constexpr (LPV > 16) v = join(v, other_16(v));
   return v;
 }
 template <int LPV>
+__device__ __forceinline__ float sum_over(float v) {
+  return __uint_as_float(over<LPV>(__float_as_uint(v), [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); }));
+}
+template <int LPV>
 __device__ __forceinline__ uint32_t max_over(uint32_t v) {
-#pragma unroll
-  for (int o = LPV / 2; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-  return v;
+  return over<LPV>(v, [](uint32_t x, uint32_t y) { return max(x, y); });
 }
 // the bits of the largest magnitude of a row: magnitudes order like their bits, NaN above infinity
 template <int LPV, int VE>
@@ -51,11 +62,12 @@ __device__ __forceinline__ void to_codes(const float (&x)[VE], uint32_t byte, ui
 // the value of the lane half a row of LPV lanes away
 template <int LPV>
 __device__ __forceinline__ float other_half(float v) {
-  const int u = __float_as_int(v);
-  if constexpr (LPV == 16) return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0x128, 0xf, 0xf, true));         // rotated by 8 within 16
-  else if constexpr (LPV == 4) return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0x4e, 0xf, 0xf, true));      // lanes 2 3 0 1 of four
-  else if constexpr (LPV == 2) return __int_as_float(__builtin_amdgcn_update_dpp(u, u, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2 of four
-  else return __shfl_xor(v, LPV / 2, 64);
+  const uint32_t u = __float_as_uint(v);
+  if constexpr (LPV == 32) return __uint_as_float(other_16(u));
+  else if constexpr (LPV == 16) return __uint_as_float(moved<0x128>(u));             // rotated by 8 within 16
+  else if constexpr (LPV == 8) return __uint_as_float(moved<0x1b>(moved<0x141>(u))); // mirrored within 8, and back within 4
+  else if constexpr (LPV == 4) return __uint_as_float(moved<0x4e>(u));
+  else return __uint_as_float(moved<0xb1>(u));
 }
 
 template <typename TI, typename TC, int HD>
@@ -135,7 +147,7 @@ __device__ __forceinline__ void any_turned(const AppendAnyArgs& g, const AppendP
           float ss = 0.f;
 #pragma unroll
           for (int e = 0; e < VE; ++e) ss += v[e] * v[e];
-          const float rs = 1.f / sqrtf(sum_over<LPV>(ss) * (1.f / HD) + a.norm_eps);
+          const float rs = rsqrtf(sum_over<LPV>(ss) * (1.f / HD) + a.norm_eps);
           if (normed) {
 #pragma unroll
             for (int e = 0; e < VE; ++e) v[e] = v[e] * rs * (is_q ? gq[e] : gk[e]);

@@ -149,6 +149,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
   constexpr int TM = 16 * NT, OS = DT * 16 + 4;
   __shared__ float so[RO_WAVES * 16 * OS];
   __shared__ float sm[RO_WAVES][16], sl[RO_WAVES][16];
+  __shared__ int2 where[TM];                                  // row and head of a column
   const ts_kv_attend_rows_args& a = g.a;
   const ts_kv_pages& pages = a.cache.pages;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, n = lane % 16, lg = lane / 16;
@@ -174,6 +175,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     const int m = rem + min(j * 16 + n, cols - 1), row = row0 + m / G, head = kvh * G + m % G;
+    if (tid < 16) where[j * 16 + n] = make_int2(row, head);
     const int2 range = row_range(a, rs, row);
     c_lo[j] = range.x; c_hi[j] = range.y;
     c_set[j] = a.ancestors ? a.ancestors[row] : 0;
@@ -457,7 +459,7 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
     for (int d = 0; d < DT; ++d) *reinterpret_cast<ts_f32x4*>(&so[(wave * 16 + n) * OS + d * 16 + lg * 4]) = o[j][d];
     __syncthreads();
     for (int i = tid; i < min(16, cols - j * 16) * HD; i += RO_WAVES * 64) {
-      const int c = i / HD, d = i % HD, mc = rem + j * 16 + c, row = row0 + mc / G, head = kvh * G + mc % G;
+      const int c = i / HD, d = i % HD, row = where[j * 16 + c].x, head = where[j * 16 + c].y;
       float top = sm[0][c];
 #pragma unroll
       for (int w = 1; w < RO_WAVES; ++w) top = fmaxf(top, sm[w][c]);
