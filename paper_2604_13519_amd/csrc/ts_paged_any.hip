@@ -400,10 +400,10 @@ __global__ __launch_bounds__(RA_THREADS) void k_kv_read(ReadArgs g) {
 // ---------------------------------------------------------------------------------
 // entry points
 // ---------------------------------------------------------------------------------
-// rows of a window, as ts_kv_append takes them
+// Rows of a window.  One sequence of 512 rows, 8 + 32 heads of 128: windows of 8 10.1 us, of 16 8.7; of 2048 rows the same.
 static int window_of(int n_rows, int n_seqs) {
   const int each = n_rows / n_seqs;
-  return each < 2 ? 1 : each < 8 ? 2 : each < 256 ? 4 : each < 1024 ? 8 : 16;
+  return each < 2 ? 1 : each < 8 ? 2 : each < 256 ? 4 : 16;
 }
 
 template <typename TI>

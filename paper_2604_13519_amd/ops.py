@@ -466,6 +466,15 @@ def ts_kv_append_norm_rope(k_pages, v_pages, table, lengths, row_offsets, q, k, 
     return q_out
 
 
+def _read_into(t, name, n_rows, width, dtype):
+    if t is None:
+        return 0, 0
+    at = _rows(t, name, width, dtype)
+    if t.shape[0] != n_rows:
+        _refuse("%s: %d rows are needed, got %d", name, n_rows, t.shape[0])
+    return at
+
+
 def ts_kv_read(k_pages, v_pages, table, starts, row_offsets, n_rows, dtype=torch.bfloat16, scales=None, k_out=None, v_out=None):
     """Positions starts[s], starts[s] + 1, ... of each sequence as rows row_offsets[s], ...: (k, v), [n_rows][heads * head_dim] of `dtype`, zeros where a
     row is no position.  starts None: from 0 on.  With k_out and / or v_out (of `dtype`) only those are written.  See the header."""
@@ -479,15 +488,10 @@ def ts_kv_read(k_pages, v_pages, table, starts, row_offsets, n_rows, dtype=torch
         _refuse("n_rows: %d", n_rows)
     own = k_out is None and v_out is None
     if own:
-        k_out, v_out = table.new_empty((2, n_rows, width), dtype=dtype).unbind()
-    at = []
-    for t, name in ((k_out, "k_out"), (v_out, "v_out")):
-        if t is None:
-            at += (0, 0)
-            continue
-        at += _rows(t, name, width, dtype)
-        if t.shape[0] != n_rows:
-            _refuse("%s: %d rows are needed, got %d", name, n_rows, t.shape[0])
+        k_out, v_out = table.new_empty((n_rows, width), dtype=dtype), table.new_empty((n_rows, width), dtype=dtype)
+        at = (k_out.data_ptr(), width, v_out.data_ptr(), width)
+    else:
+        at = _read_into(k_out, "k_out", n_rows, width, dtype) + _read_into(v_out, "v_out", n_rows, width, dtype)
     try:
         a = _pack_read(*pages, p_table, t_stride, t_width, 0 if starts is None else _ints(starts, "starts", n), _ints(row_offsets, "row_offsets", 2), n, n_rows,
                        _DTYPES[dtype], own, *at)
