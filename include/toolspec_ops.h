@@ -156,8 +156,9 @@ ts_status ts_kv_attend_workspace(int32_t n_seqs, int32_t n_q_heads, int32_t n_kv
  * significant bits, largest 448.  k_scales and v_scales, [n_pages][n_kv_heads][16] bytes each, 16-byte aligned, hold e + 127
  * for each position's row of a head, and a value stands for its e4m3 value times 2^e: e is the least that keeps the row's
  * largest magnitude at or below 448 * 2^e, and at least -127 (all zeros: -127); values are rounded to nearest, ties to
- * even.  A row with an infinity or NaN has scale byte 255 and all its values are NaN.  For pages of other types the two are
- * null.  (A program that writes pages by itself may use other scales; 255 is NaN there too.) */
+ * even.  A row with an infinity or NaN has scale byte 255 and all its values are NaN.  Values whose magnitude 2^e takes to 2^128 and
+ * beyond (rows with magnitudes above 31/32 of 2^128, or scales that a program wrote itself) are infinite; in products and as bf16 bits
+ * below 2^-133 are lost.  For pages of other types the two are null. */
 enum { TS_DTYPE_E4M3 = 3 };
 typedef struct {
   ts_kv_pages pages;
@@ -196,8 +197,8 @@ typedef struct {
 ts_status ts_kv_append_norm_rope(const ts_kv_append_norm_rope_args* args, ts_stream stream);
 
 /* Positions of a cache given back as rows: row row_offsets[s] + i of k_out and v_out is position starts[s] + i of sequence s,
- * as it is stored (keys rotated), n_kv_heads heads of head_dim, in `dtype` (8-bit values and bf16 widen exactly to fp32 and 8-bit
- * values to bf16, a scale byte of 253 or more aside, whose values may be infinite; fp32 rounds to bf16 once).  starts null: from position 0 on; k_out or
+ * as it is stored (keys rotated), n_kv_heads heads of head_dim, in `dtype` (8-bit values and bf16 widen exactly to fp32, 8-bit
+ * values to bf16 as said above; fp32 rounds to bf16 once).  starts null: from position 0 on; k_out or
  * v_out may be null.  Rows outside every sequence, and rows whose position is negative, beyond the table or on a page outside [0, n_pages),
  * stay as they were, or become zeros where zero_rest is not 0.
  * Errors: INVALID_ARG (as above; n_rows in [0, 2^23]), DEVICE. */
@@ -219,9 +220,10 @@ ts_status ts_kv_read(const ts_kv_read_args* args, ts_stream stream);
  * bit is set like any other; window has to be 0).  out, lse, scale, heads, pages out of range, max_len (here: no position of
  * a row is at or above it), contents of what is not seen, and rows that see nothing: as ts_kv_attend; rows outside every sequence
  * stay as they were in out and lse.  A seen infinite value makes its dimension infinite, or NaN where its probability is zero.
- * Scores, sums and outputs are fp32; queries and probabilities of fp32 rows enter the products over bf16 and 8-bit pages with 24 bits;
- * probabilities of bf16 rows are rounded to bf16, once, for the product with the values, not for their sum, where a chunk has
- * more rows x heads per KV head than one tile (16), and have 24 bits too where it has not.
+ * Scores, sums and outputs are fp32; queries and probabilities of fp32 rows enter the products over bf16 and 8-bit pages with 24 bits.
+ * Probabilities of bf16 rows have 24 bits too where the chunks have up to 16 rows x heads per KV head on average; where they have more they are
+ * rounded to bf16, once, for the product with the values (not for their sum): as much as the rounding of the output.  The order of
+ * the sums depends on the sizes (n_seqs, n_rows, heads, max_len, window) and a chunk's own rows, never on contents.
  *   q, out    : [n_rows] rows of n_q_heads * head_dim, in `dtype`
  *   lse       : [n_rows][n_q_heads] fp32, or null
  *   ancestors : [n_rows] 64-bit sets, or null

@@ -794,7 +794,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join_few(RowsArgs g) {
     return;
   }
   const int2 range = row_range(a, row_seq(a, seq), row);
-  const int c0 = range.x / g.chunk, used = max(1, (range.y + g.chunk - 1) / g.chunk - c0);       // a row that sees nothing: one empty part
+  const int c0 = range.x / g.chunk, used = range.y > range.x ? (range.y + g.chunk - 1) / g.chunk - c0 : 0;      // a row that sees nothing has no parts
   const float2* ml = reinterpret_cast<const float2*>(g.part_ml) + at * g.splits;
   const float4* part = reinterpret_cast<const float4*>(g.part_o) + at * g.splits * COLS + lane % COLS;
   float top = -INFINITY;
@@ -843,7 +843,7 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
   }
   const RowSeq rs = row_seq(a, seq);
   const int2 range = row_range(a, rs, row);
-  const int c0 = range.x / g.chunk, used = max(1, (range.y + g.chunk - 1) / g.chunk - c0);       // a row that sees nothing: one empty part
+  const int c0 = range.x / g.chunk, used = range.y > range.x ? (range.y + g.chunk - 1) / g.chunk - c0 : 0;      // a row that sees nothing has no parts
   const int64_t at = (int64_t)row * a.n_q_heads + h;
   const float2* ml = reinterpret_cast<const float2*>(g.part_ml) + at * g.splits;
   float top = -INFINITY;

@@ -280,6 +280,26 @@ def test_bad_pages_lengths_and_offsets_are_not_followed():
         assert bool((call(table, off=(5, 3), out=torch.full((rows, hq * hd), 7.0, dtype=BF16, device="cuda"))[0] == 7).all())
 
 
+@pytest.mark.parametrize("dtype,qdtype", TYPES)
+def test_windows_that_end_behind_max_len(dtype, qdtype):
+    """The window counts from a row's position; rows whose window lies at max_len and beyond see nothing, beside rows of the same tile that do."""
+    hq, hkv, hd, n, top = 8, 2, 64, 2100, 2048
+    for rows in (1, 3, 80):
+        for window in (100, 128, 60):
+            pages, table, K, V = cache_of([n + rows], hkv, hd, dtype, 3)
+            q = torch.randn((rows, hq * hd), generator=torch.Generator().manual_seed(4)).to(qdtype)
+            ws = ops.ts_kv_attend_rows_workspace(1, rows, hq, hkv, hd, top, window)
+            if ws is not None:
+                ws.fill_(255)                                  # NaN: a part that nobody wrote shows
+            out, lse = ops.ts_kv_attend_rows(*pages.pages, table, ints([n]), ints([0, rows]), q.cuda(), top, window=window, scales=pages.scales, workspace=ws)
+            seen = seen_of(n, rows, window)
+            seen[:, top:] = False
+            want, want_lse, rough, d = plain(q.view(rows, hq, hd), K[0], V[0], seen, hd ** -0.5)
+            none = ~seen.any(1)
+            assert bool((out.cpu()[none] == 0).all()) and bool((lse.cpu()[none] == -math.inf).all())
+            assert bool(((out.double().cpu().view(rows, hq, hd) - want).abs() <= tolerance(want, rough, d, window, dtype, qdtype, rows * 4)).all()), (rows, window)
+
+
 def test_strided_rows():
     pages, table, K, V = cache_of([60], 2, 64, BF16, 8)
     wide = torch.full((20, 4 * 64 + 9), math.nan, dtype=BF16, device="cuda")
