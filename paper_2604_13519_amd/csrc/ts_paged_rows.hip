@@ -575,8 +575,11 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
       }
     }
   };
-  // 16-byte pieces of a key lie where no two of eight lanes that read the same piece of different keys (0 .. 3 and 8 .. 11, say) meet on a bank
-  auto key_place = [&](int key, int piece) __attribute__((always_inline)) { return key * (HD / 8) + (piece ^ ((key & 3) | (key >> 1 & 4))); };
+  // LDS places of 16-byte pieces: of sixteen lanes that read or write together, each meets a sixteenth of 256 bytes of its own.  Sixteen
+  // lanes read one piece of sixteen keys, or one half (eight keys) of sixteen dimensions; they write the pieces of one or two
+  // keys (widened: every other one of two or four), or both halves of eight dimensions (widened: one of sixteen).
+  auto key_place = [&](int key, int piece) __attribute__((always_inline)) { return key * (HD / 8) + (piece ^ (HD == 128 ? key & 15 : key >> 1 & 7)); };
+  auto value_place = [&](int page, int dim, int half) __attribute__((always_inline)) { return ((page * DT + dim / 32) * 2 + half) * 32 + (dim % 32 ^ half * 8); };
   auto widen_values = [&](uint32_t lo4, uint32_t hi4, uint32_t s_lo, uint32_t s_hi) __attribute__((always_inline)) {      // eight keys of a dimension
     float x[4], y[4];
     e4m3_to_f32(lo4, s_lo, x);
@@ -616,7 +619,7 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
 #pragma unroll
       for (int e = 0; e < (E8 ? 2 : 1); ++e) {
         if (!all_see) v[e] = clean(v[e]);
-        sv[slot][piece * (E8 ? 2 : 1) + e] = v[e];
+        sv[slot][E8 ? value_place(pg, in, e) : value_place(pg, in / 2, in % 2)] = v[e];
       }
     }
   };
@@ -678,7 +681,7 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
       for (int v = 0; v < 2; ++v)
 #pragma unroll
         for (int d = 0; d < DT; ++d)
-          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ts_bf16x8, sv[slot][((t * 2 + v) * HD + d * 32 + n) * 2 + h]), __builtin_bit_cast(ts_bf16x8, p[v]), o[d], 0, 0, 0);
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(ts_bf16x8, sv[slot][value_place(t * 2 + v, d * 32 + n, h)]), __builtin_bit_cast(ts_bf16x8, p[v]), o[d], 0, 0, 0);
     }
   };
   auto whole = [&](int b, int ok) { return k0 + b * 64 >= tile_lo && k0 + b * 64 + 64 <= tile_hi && ok == 15; };
