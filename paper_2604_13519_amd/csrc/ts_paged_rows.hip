@@ -5,18 +5,26 @@
 
 // ---------------------------------------------------------------------------------
 // The rows of a chunk and the query heads that share a KV head are the columns of one problem: column m of (sequence, KV head) is
-// row m / group, head m % group, and all columns go over the same keys and values.  Tiles of 16 NT columns, one pass with a
-// running maximum and sum, four waves that take blocks of KB keys in turn, the cache's length split over workgroups
-// and joined where the tiles alone do not fill the card.
+// row m / group, head m % group, and all columns go over the same keys and values.  One pass with a running maximum and sum, the
+// cache's length split over workgroups and joined where the tiles of columns alone do not fill the card.
+//
+// This kernel: few columns (single tokens), and fp32 rows or pages.  Tiles of 16 NT columns, four waves that take blocks of 32 keys in
+// turn, straight from memory: bound by the bytes of the cache, each read once for a tile.
 //
 // Matrix instructions without any exchange between lanes: S^T = K Q^T puts 16 columns on the lanes (lane l: column l % 16) and four keys
 // of a tile in a lane's registers; O^T = V^T P^T wants eight (fp32: one) consecutive keys of a column in a lane.
-// Which key is which row of K's tile is free: row m of tile t takes key KB / 4 (m / 4) + 4 t + m % 4, and the probabilities that a
-// lane has computed are, in place, the operand it needs next.
+// Which key is which row of K's tile is free: row m of tile t takes key 8 (m / 4) + 4 t + m % 4, and the probabilities that a
+// lane has computed are, in place, the operand it needs next.  8-bit keys are widened to bf16 times their scales (exact), 8-bit values
+// without, their scales go onto the probabilities: eight keys of a lane are eight scales.
 //
 // Where rows see different keys of a block, probabilities of unseen ones are zero, and zero times an infinite or NaN value
 // is not: such blocks are looked through, and values that are not finite are replaced by zeros and counted by indicator products,
 // so that they reach the rows that see them and no other.
+//
+// 8-bit pages, 8 KV heads of 128, 64 query heads: a token for each of 8 sequences up to 32768 (387 MB) 82 us in a kernel trace, 4.7 TB/s.
+// 32 query heads over 8, one token over 8192 positions, in a captured graph with its join: bf16 12.5 us (ts_kv_attend 10.6), 8-bit 12.0.
+// fp32 pages, 32 query heads over 8 of 128, 300 rows over 4000: 356 us, 57 TFLOP/s of the 157 that fp32 matrix
+// instructions have.
 // ---------------------------------------------------------------------------------
 constexpr int RO_WAVES = 4;
 constexpr int RO_CUS = 256, RO_UNIT = 128, RO_MOST = 2;    // RO_MOST: workgroups a CU that a call is split into, at most
@@ -485,12 +493,22 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
 }
 
 // ---------------------------------------------------------------------------------
-// Many columns over bf16 and 8-bit pages, bf16 rows: bound by the matrix pipes and by the soft-max beside them.  Eight waves of 32
-// columns share the keys and values of a block of 64 through the LDS; two waves a SIMD, so that one's soft-max runs while the
-// other multiplies.  The running maximum is a reference that moves only when a score passes it by more than 2^8, so that
-// sums are rarely rescaled.  The matrix layout is the one above in tiles of 32 x 32: row m of K's tile is key m with its bits 2 and 3
-// swapped.  Blocks go through registers (8-bit ones are widened there, times their scales, once for all waves) into two LDS slots: while
-// block b is used, b + 1 is written and b + 2 and b + 3 are on their way; one barrier a block.
+// Many columns over bf16 and 8-bit pages, bf16 rows: bound by the matrix pipes and by the soft-max beside them.  W waves of 32
+// columns share the keys and values of a block of 64 through the LDS.  The running maximum is a reference that moves only when a
+// score passes it by more than 2^8, so that sums are rarely rescaled.  The matrix layout is the one above in tiles of 32 x 32: row m of K's
+// tile is key m with its bits 2 and 3 swapped.  Blocks go through registers (8-bit ones are widened there, times their scales,
+// once for all waves) into two LDS slots: while block b is used, b + 1 waits in registers and is written behind it, then b + 2 is
+// requested; one barrier a block.  Probabilities are rounded to bf16 for the product with the values: a second term would be half as
+// many matrix instructions again, for a rounding as large as the output's own.
+//
+// bf16, 32 query heads over 8 of 128: three prompts, 9012 rows (237 GFLOP as counted) 290 - 305 us, 0.80 PFLOP/s, matrix pipes busy 40 %;
+// a tree of 65 rows over 8192 positions 28 us and 7 of the join; 16 x 33 rows over up to 4096 66 and 12.  8-bit, 64 heads over 8:
+// 4 x 512 rows over up to 16384 (881 GFLOP) 975 - 985 us, 0.90 PFLOP/s.  What a block's time goes into, by leaving pieces out (the last
+// case, 1193 us then): products alone 531, without staging 872, without staging and LDS reads 640, without staging and soft-max 730.
+// Measured and not kept (prompts and last case, microseconds, beside this kernel of the same day): four waves of 64 columns, half the
+// LDS reads, a phase's soft-max between its neighbours' products by hand, one wave a SIMD: 406 and 2247 : 332 and 1261.  Two groups of
+// waves half a step apart, one multiplying while the other works out probabilities: 319 - 356 and 1365 - 1895.  Two blocks on their way, a
+// barrier for 128 keys, wave priorities, fragments read ahead: no gain.
 // ---------------------------------------------------------------------------------
 typedef float ts_f32x16 __attribute__((ext_vector_type(16)));
 
@@ -893,7 +911,10 @@ __global__ __launch_bounds__(256) void k_kv_attend_rows_join(RowsArgs g) {
 
 struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a workgroup (8 and 16: the wide kernel), keys of a split, splits, tile slots per KV head
 
-// Tiles of 16 columns where a sequence has no more, of 64 (fp32: 32) where it has.
+// Columns of a workgroup, from those a sequence has on average: 16; then, of fp32 rows or pages, 32; of others 128 and, from 512 on, 256.
+// bf16, 32 query heads over 8, microseconds: 8 rows over 8192 (32 columns) 128 a workgroup 20.3, tiles of 64 straight from memory 29.3;
+// 16 x 12 rows over 4096 (48) 57 and 157; 16 x 33 over up to 4096 (132) 76, and 256 a workgroup 88; 8-bit chunks of 4 x 512 rows
+// (4096) 1217 and 1127.
 static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 512 ? 8 : 16; }
 static int64_t rows_units(int max_len, int window) {         // of 128 keys, in what one tile sees
   const int64_t span = window > 0 && (int64_t)window + 256 < max_len ? window + 256 : max_len;
@@ -916,6 +937,8 @@ static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
   c.slots = a.row_offsets ? (int64_t)a.n_rows * group / tm + a.n_seqs : (int64_t)a.n_seqs * ((group + tm - 1) / tm);
   const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), units = rows_units(a.max_len, a.window);
   int64_t per = 1;
+  // Workgroups a CU: two of the smaller wide ones (16 x 33 rows 105 -> 86 us, 8 x 33 rows over 16384 8-bit positions 237 -> 143; three or four
+  // no faster) and of single tokens over 8-bit pages (8 sequences up to 32768 133 -> 88, four 93).
   const int a_cu = (c.nt == 1 && a.cache.pages.dtype == TS_DTYPE_E4M3) || c.nt == 8 ? 2 : 1;
   if (units * whole > RO_MOST * RO_CUS) {
     const int64_t want = std::max<int64_t>(1, std::min(a_cu, RO_MOST) * RO_CUS / whole);
