@@ -166,7 +166,7 @@ typedef struct {
 } ts_kv_pages_any;
 
 /* ts_kv_append for decoder blocks that norm the heads of queries and keys, turn them otherwise, or keep 8-bit pages.  Rows, offsets,
- * lengths, tables and places as there.  A head of a query or key is, in fp32 and in this order
+ * lengths, tables and places as there (q_out may be q).  A head of a query or key is, in fp32 and in this order
  *   normed  : x / sqrt(mean of x^2 + norm_eps) * gain, where there is a gain: q_norm, k_norm, [head_dim] of norm_dtype, each
  *             may be null
  *   rotated : its first rope_dim values (even, at most head_dim; 0: none) in pairs - (j, j + rope_dim / 2), or (2 j, 2 j + 1)
