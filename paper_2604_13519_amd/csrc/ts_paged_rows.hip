@@ -801,7 +801,7 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
 // The join of a row's splits: chunk c of the cache's positions lies at place c % splits.  Few splits: a wave per (row, head), four
 // dimensions a lane, the splits dealt to the lane groups of a head's length.  Bound by trips to memory in turn: the sequence, its length, the parts.
 // One token over 8192 positions (33 splits, the kernel below) 5.0 - 5.6 us in a trace, 65 rows x 32 heads of 17 splits (18 MB) 6.8 - 7.0.  Weights and
-// parts asked for before the row's sequence is known gained 0.3 us at most in a call (17.1 : 16.6, 35.6 : 35.3, 75.6 : 75.4): not kept.
+// parts asked for before the row's sequence is known gained 0.2 - 0.5 us of a call (17.1 : 16.6, 35.6 : 35.3, 75.6 : 75.4): not kept.
 template <typename TQ, int HD>
 __global__ __launch_bounds__(256) void k_kv_attend_rows_join_few(RowsArgs g) {
   constexpr int COLS = HD / 4, GROUPS = 64 / COLS;
