@@ -1,14 +1,56 @@
-"""Attention of chunks over batches of 63 to 200 sequences with different numbers of rows: what the plan of such calls can come across, against the plain
+"""Attention of chunks over batches of 40 to 200 sequences with different numbers of rows: what the plan of such calls can come across, against the plain
 64-bit implementation and with the tolerances of test_gpu_paged_rows."""
+import numpy as np
 import pytest
 import torch
 
 from paged_any import BF16, E4M3, F32, cache_of, ints
 from paper_2604_13519_amd import ops
-from test_gpu_paged_rows import seen_of, tolerance
+from test_gpu_paged_rows import TYPES, check, random_tree, seen_of, tolerance
 from test_gpu_paged_rows import plain as plain_rows
 
 pytestmark = pytest.mark.gpu
+
+
+def ragged(n, most_rows, most_before, seed, empty=0.3):
+    """Rows and earlier positions of n sequences: some without rows, the first and last among them."""
+    rng = np.random.default_rng(seed)
+    new = [int(x) for x in rng.integers(0, most_rows + 1, n)]
+    new = [0 if rng.random() < empty or i in (0, n - 1) else r for i, r in enumerate(new)]
+    new[n // 2] = most_rows
+    return [int(x) for x in rng.integers(0, most_before + 1, n)], new
+
+
+@pytest.mark.parametrize("dtype,qdtype", TYPES)
+@pytest.mark.parametrize("n", [40, 63, 64, 65, 200])
+def test_ragged_batches(dtype, qdtype, n):
+    """Few rows each (tiles of 16), some more (128; fp32 32), many (256: more than 512 columns a sequence on average)."""
+    before, new = ragged(n, 6, 300, n)
+    check(before, new, 4, 2, 64, dtype, qdtype, seed=n, spare=2, tag="few")
+    before, new = ragged(n, 60 if n == 200 else 150, 200, n + 1)
+    check(before, new, 8, 2, 64 if n % 2 else 128, dtype, qdtype, seed=n + 1, tag="some")
+    before, new = ragged(n, 30 if n == 200 else 100, 100, n + 2, empty=0.1)
+    check(before, new, 34, 1, 64, dtype, qdtype, seed=n + 2, spare=1, tag="many")
+    before, new = ragged(n, 300, 50, n + 3, empty=0.97)                             # one long chunk and little else
+    check(before, new, 4, 1, 64, dtype, qdtype, seed=n + 3, tag="one")
+
+
+@pytest.mark.parametrize("dtype,qdtype", TYPES)
+@pytest.mark.parametrize("n", [64, 130])
+def test_ragged_batches_with_splits_windows_and_trees(dtype, qdtype, n):
+    """One KV head: contexts of some thousand positions are split over workgroups."""
+    before, new = ragged(n, 3, 200, n)
+    before[3], before[n // 2] = 3000, 2500
+    check(before, new, 4, 1, 64, dtype, qdtype, seed=n, spare=3, tag="splits")
+    check(before, new, 4, 1, 64, dtype, qdtype, window=700, seed=n, tag="splits of a window")
+    before, new = ragged(n, 70, 200, n + 1)
+    before[3], before[n // 2], new[3] = 3000, 2500, 5
+    check(before, new, 4, 1, 128, dtype, qdtype, seed=n + 1, tag="splits, more rows")
+    check(before, new, 4, 1, 64, dtype, qdtype, window=45, seed=n + 1, tag="window")
+    new = [min(r, 65) for r in new]
+    rng = np.random.default_rng(n)
+    for rows in (new, [min(r, 4) for r in new]):
+        check(before, rows, 4, 1, 64, dtype, qdtype, trees=[random_tree(rng, r) if r else [] for r in rows], seed=n + 2, spare=1, tag="tree")
 
 
 def test_offsets_that_decrease_stay_in_bounds():
