@@ -136,6 +136,14 @@ __device__ __forceinline__ ts_u32x4 e4m3_to_bf16(uint32_t a, uint32_t b, float s
   return ts_u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
                   __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};
 }
+// eight values of one scale each: the bytes of two dwords, their scales those of two others
+__device__ __forceinline__ ts_u32x4 e4m3_to_bf16(uint32_t a, uint32_t b, uint32_t s_a, uint32_t s_b) {
+  float x[4], y[4];
+  e4m3_to_f32(a, s_a, x);
+  e4m3_to_f32(b, s_b, y);
+  return ts_u32x4{__builtin_bit_cast(uint32_t, to_bf16x2(x[0], x[1])), __builtin_bit_cast(uint32_t, to_bf16x2(x[2], x[3])),
+                  __builtin_bit_cast(uint32_t, to_bf16x2(y[0], y[1])), __builtin_bit_cast(uint32_t, to_bf16x2(y[2], y[3]))};
+}
 __device__ __forceinline__ uint32_t f32_to_e4m3(float a, float b, float c, float d) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }

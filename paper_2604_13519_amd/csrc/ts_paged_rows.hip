@@ -16,7 +16,8 @@
 // of a tile in a lane's registers; O^T = V^T P^T wants eight (fp32: one) consecutive keys of a column in a lane.
 // Which key is which row of K's tile is free: row m of tile t takes key 8 (m / 4) + 4 t + m % 4, and the probabilities that a
 // lane has computed are, in place, the operand it needs next.  8-bit keys are widened to bf16 times their scales (exact), 8-bit values
-// without, their scales go onto the probabilities: eight keys of a lane are eight scales.
+// without, their scales go onto the probabilities: eight keys of a lane are eight scales.  In blocks with a scale below 2^-63 or from 2^113 on
+// the values are widened times theirs: an infinite one is so whatever its probability, a tiny one costs no bits of it.
 //
 // Where rows see different keys of a block, probabilities of unseen ones are zero, and zero times an infinite or NaN value
 // is not: such blocks are looked through, and values that are not finite are replaced by zeros and counted by indicator products,
@@ -47,8 +48,8 @@ __device__ __forceinline__ int2 row_range(const ts_kv_attend_rows_args& a, const
   return make_int2(lo, hi);
 }
 
-// whether one of four scales is NaN
-__device__ __forceinline__ bool nan_scale(uint32_t w) { return (((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u) != 0; }
+// whether one of four scales is below 2^-63, or from 2^113 on (NaN too)
+__device__ __forceinline__ bool far_scale(uint32_t w) { return (((((w & 0x7f7f7f7fu) + 0x10101010u) & w) | ~(w | w << 1)) & 0x80808080u) != 0; }
 __device__ __forceinline__ bool not_finite(uint32_t bf16_pair) {
   return (bf16_pair & 0x7f80u) == 0x7f80u || (bf16_pair & 0x7f800000u) == 0x7f800000u;
 }
@@ -211,8 +212,8 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
     }
     auto key_of = [&](int i) { return kb + (F32 ? 16 * (i / 4) + 4 * lg + i % 4 : KL * lg + i); };      // a lane's i-th key
     const bool whole = kb >= all_lo && kb + KB <= min(all_hi, k1) && f.ok0 && f.ok1;
-    bool nans = false;
-    if constexpr (E8) nans = __ballot(nan_scale(f.vs[0]) || nan_scale(f.vs[1])) != 0;
+    bool far = false;                                        // a value's scale goes onto its probability where that neither overflows nor loses bits
+    if constexpr (E8) far = __ballot(far_scale(f.vs[0]) || far_scale(f.vs[1])) != 0;
     uint32_t keep[NT];
     uint32_t pk[NT][PP][KL / 2];                             // probabilities as pairs of bf16 terms
     float px[F32 ? NT : 1][F32 ? KL : 1];
@@ -251,14 +252,11 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
         x[i] = __builtin_amdgcn_exp2f(x[i] - ref);
         l[j] += x[i];
       }
-      if constexpr (E8) {                                    // the scale of a value; of what is not seen it may be NaN
-        if (nans) {
+      if constexpr (E8) {
+        if (!far) {
 #pragma unroll
-          for (int i = 0; i < KL; ++i)
-            if ((f.vs[i / 4] >> i % 4 * 8 & 255) == 255) x[i] = whole || (keep[j] >> i & 1) ? NAN : 0.f;
+          for (int i = 0; i < KL; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], (int)(f.vs[i / 4] >> i % 4 * 8 & 255) - 127);
         }
-#pragma unroll
-        for (int i = 0; i < KL; ++i) x[i] = __builtin_amdgcn_ldexpf(x[i], (int)(f.vs[i / 4] >> i % 4 * 8 & 255) - 127);
       }
       if constexpr (F32) {
 #pragma unroll
@@ -304,8 +302,12 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
           ts_u32x4 w;
-          if constexpr (E8) w = e4m3_to_bf16(f.v[0][d][0], f.v[0][d][1], 1.f);
-          else w = f.v[0][d];
+          if constexpr (E8) {
+            if (far) w = e4m3_to_bf16(f.v[0][d][0], f.v[0][d][1], f.vs[0], f.vs[1]);
+            else w = e4m3_to_bf16(f.v[0][d][0], f.v[0][d][1], 1.f);
+          } else {
+            w = f.v[0][d];
+          }
           if (!whole && __ballot(not_finite(w[0]) || not_finite(w[1]) || not_finite(w[2]) || not_finite(w[3]))) {
             for (int cls = 0; cls < 3; ++cls) {
               ts_u32x4 is;
@@ -511,13 +513,6 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   // keys (widened: every other one of two or four), or both halves of eight dimensions (widened: one of sixteen).
   auto key_place = [&](int key, int piece) __attribute__((always_inline)) { return key * (HD / 8) + (piece ^ (HD == 128 ? key & 15 : key >> 1 & 7)); };
   auto value_place = [&](int page, int dim, int half) __attribute__((always_inline)) { return ((page * DT + dim / 32) * 2 + half) * 32 + (dim % 32 ^ half * 8); };
-  auto widen_values = [&](uint32_t lo4, uint32_t hi4, uint32_t s_lo, uint32_t s_hi) __attribute__((always_inline)) {      // eight keys of a dimension
-    float x[4], y[4];
-    e4m3_to_f32(lo4, s_lo, x);
-    e4m3_to_f32(hi4, s_hi, y);
-    return ts_u32x4{__builtin_bit_cast(uint32_t, to_bf16x2(x[0], x[1])), __builtin_bit_cast(uint32_t, to_bf16x2(x[2], x[3])),
-                    __builtin_bit_cast(uint32_t, to_bf16x2(y[0], y[1])), __builtin_bit_cast(uint32_t, to_bf16x2(y[2], y[3]))};
-  };
   // values that are not finite become zeros where not every column sees them
   auto clean = [&](ts_u32x4 v) __attribute__((always_inline)) {
     bool bad = false;
@@ -541,8 +536,8 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
         const float ks = scale_at<0>(st.ks[i]);
         sk[slot][key_place(key, c)] = e4m3_to_bf16(st.k[i][0], st.k[i][1], ks);
         sk[slot][key_place(key, c + 1)] = e4m3_to_bf16(st.k[i][2], st.k[i][3], ks);
-        v[0] = widen_values(st.v[i][0], st.v[i][1], st.vs[i][0], st.vs[i][1]);
-        v[1] = widen_values(st.v[i][2], st.v[i][3], st.vs[i][2], st.vs[i][3]);
+        v[0] = e4m3_to_bf16(st.v[i][0], st.v[i][1], st.vs[i][0], st.vs[i][1]);
+        v[1] = e4m3_to_bf16(st.v[i][2], st.v[i][3], st.vs[i][2], st.vs[i][3]);
       } else {
         sk[slot][key_place(pg * 16 + in / (HD / 8), in % (HD / 8))] = st.k[i];
         v[0] = st.v[i];
@@ -661,7 +656,7 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
           ts_u32x4 v;
           if constexpr (E8) {
             const uint2 w = *reinterpret_cast<const uint2*>((const char*)pages.v + (head * HD + d * 32 + n) * 16 + 8 * h), sc = *reinterpret_cast<const uint2*>(a.cache.v_scales + head * 16 + 8 * h);
-            v = widen_values(w.x, w.y, sc.x, sc.y);
+            v = e4m3_to_bf16(w.x, w.y, sc.x, sc.y);
           } else {
             v = *reinterpret_cast<const ts_u32x4*>((const char*)pages.v + (head * HD + d * 32 + n) * 32 + 16 * h);
           }
