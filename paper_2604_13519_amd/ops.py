@@ -345,6 +345,13 @@ def ts_kv_attend_workspace(n_seqs, n_q_heads, n_kv_heads, head_dim, max_len, win
     return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
 
 
+def _given_lse(t, n, heads):
+    if t.shape != (n, heads) or t.dtype is not torch.float32 or not t.is_contiguous() or not t.is_cuda:
+        _refuse("lse: a contiguous fp32 [%d][%d] tensor on a GPU is needed, got %s %s", n, heads, t.dtype, tuple(t.shape))
+    if t.requires_grad:
+        _no_gradient("lse")
+
+
 def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=None, workspace=None, out=None, lse=None):
     """Attention of one token per sequence, q [n_seqs][heads * head_dim]: (out like q, lse fp32 [n_seqs][heads]).  scale None:
     1 / sqrt(head_dim).  workspace: of ts_kv_attend_workspace; without one the call allocates it.  See the header."""
@@ -364,8 +371,8 @@ def ts_kv_attend(k_pages, v_pages, table, lengths, q, max_len, window=0, scale=N
         po, o_stride = _rows(out, "out", width, dtype)
     if lse is None:
         lse = q.new_empty((n, heads), dtype=torch.float32)
-    elif lse.shape != (n, heads) or lse.dtype is not torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
-        _refuse("lse: a contiguous fp32 [%d][%d] tensor on a GPU is needed, got %s %s", n, heads, lse.dtype, tuple(lse.shape))
+    else:
+        _given_lse(lse, n, heads)
     if out.shape[0] != n:
         _refuse("out: %d rows are needed, got %d", n, out.shape[0])
     if workspace is None:
@@ -395,6 +402,8 @@ def _any_pages(k_pages, v_pages, scales):
         _refuse("v_pages: shape %s is needed, got %s", (n, h, hd, TS_PAGE_SIZE), tuple(v_pages.shape))
     if v_pages.dtype is not torch.float8_e4m3fn:
         raise TypeError("pages: two of one type are needed, got %s and %s" % (k_pages.dtype, v_pages.dtype))
+    if k_pages.requires_grad or v_pages.requires_grad:
+        _no_gradient("pages")
     if scales is None or len(scales) != 2:
         _refuse("scales: (k_scales, v_scales) are needed with float8_e4m3fn pages")
     shape = (n, h, TS_PAGE_SIZE)
@@ -533,8 +542,8 @@ def ts_kv_attend_rows(k_pages, v_pages, table, lengths, row_offsets, q, max_len,
         _refuse("out: %d rows are needed, got %d", rows, out.shape[0])
     if lse is None:
         lse = q.new_empty((rows, heads), dtype=torch.float32) if row_offsets is None else q.new_zeros((rows, heads), dtype=torch.float32)
-    elif lse.shape != (rows, heads) or lse.dtype is not torch.float32 or not lse.is_contiguous() or not lse.is_cuda:
-        _refuse("lse: a contiguous fp32 [%d][%d] tensor on a GPU is needed, got %s %s", rows, heads, lse.dtype, tuple(lse.shape))
+    else:
+        _given_lse(lse, rows, heads)
     sets = 0
     if ancestors is not None:
         if ancestors.dtype is not torch.int64 or not ancestors.is_cuda or ancestors.dim() != 1 or not ancestors.is_contiguous() or ancestors.shape[0] < rows:

@@ -151,6 +151,39 @@ def test_tensors_are_looked_at(lib):
         ops._gain(t(64), "k_norm", 64, torch.bfloat16)
 
 
+class OnGpu(torch.Tensor):
+    """A tensor that says it is on a GPU: what is looked at before a call."""
+    is_cuda = True
+
+
+def on_gpu(*shape, dtype=torch.float32, grad=False):
+    t = torch.zeros(shape).to(dtype)
+    return (t.requires_grad_() if grad else t).as_subclass(OnGpu)
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_gradients_of_8_bit_pages_are_refused(lib, which):
+    e4m3, byte, i32 = torch.float8_e4m3fn, torch.uint8, torch.int32
+    k, v = on_gpu(3, 2, 16, 64, dtype=e4m3, grad=which == 0), on_gpu(3, 2, 64, 16, dtype=e4m3, grad=which == 1)
+    scales = (on_gpu(3, 2, 16, dtype=byte), on_gpu(3, 2, 16, dtype=byte))
+    table, one, off, rows = on_gpu(1, 3, dtype=i32), on_gpu(1, dtype=i32), on_gpu(2, dtype=i32), on_gpu(4, 128)
+    for call in (lambda: ops.ts_kv_append_norm_rope(k, v, table, one, off, rows, rows, rows, scales=scales), lambda: ops.ts_kv_read(k, v, table, one, off, 4, scales=scales),
+                 lambda: ops.ts_kv_attend_rows(k, v, table, one, off, rows, 40, scales=scales)):
+        with pytest.raises(ValueError, match="pages requires a gradient"):
+            call()
+    with torch.no_grad():
+        ops._any_pages(k, v, scales)
+
+
+def test_a_gradient_of_lse_is_refused(lib):
+    k, v, table, one, off = on_gpu(3, 2, 16, 64), on_gpu(3, 2, 64, 16), on_gpu(4, 3, dtype=torch.int32), on_gpu(4, dtype=torch.int32), on_gpu(2, dtype=torch.int32)
+    q, out, lse = on_gpu(4, 128), on_gpu(4, 128), on_gpu(4, 2, grad=True)
+    with pytest.raises(ValueError, match="lse requires a gradient"):
+        ops.ts_kv_attend_rows(k, v, table, one, off, q, 40, out=out, lse=lse)
+    with pytest.raises(ValueError, match="lse requires a gradient"):
+        ops.ts_kv_attend(k, v, table, one, q, 40, out=out, lse=lse)
+
+
 def test_numbers_beyond_32_bits_are_refused(lib):
     for at in range(7):
         sizes = [1, 1, 8, 8, 128, 100, 0]
