@@ -4,9 +4,11 @@
 ts_status ops_device(const char* call, std::initializer_list<const void*> pointers, ts_stream stream, int* device) {
   int dev = -1;
   // A lookup is 0.2 us of a call's 4 to 6 in the library.  Small tensors of a program mostly lie in a few allocations: what lies in one
-  // that this call has met needs none (append of 15 pointers 12.0 -> 11.4 us a call, through the binding).
+  // that this call has met needs none (append of 15 pointers 12.0 -> 11.4 us a call, through the binding).  An allocation's bounds cost about as
+  // much as half a lookup, so calls of few pointers do without (product with 4-bit weights, three allocations: 6.2 us, with bounds 6.4).
   struct { uintptr_t from, to; } met[4];
   int n_met = 0;
+  const bool bounds = pointers.size() > 8;
   for (const void* p : pointers) {
     if (!p) continue;
     bool inside = false;
@@ -22,7 +24,7 @@ ts_status ops_device(const char* call, std::initializer_list<const void*> pointe
     dev = a.device;
     hipDeviceptr_t base = nullptr;
     size_t size = 0;
-    if (n_met < 4) {
+    if (bounds && n_met < 4) {
       if (hipMemGetAddressRange(&base, &size, (hipDeviceptr_t)p) == hipSuccess) met[n_met++] = {(uintptr_t)base, (uintptr_t)base + size};
       else (void)hipGetLastError();
     }
