@@ -462,7 +462,7 @@ __global__ __launch_bounds__(RW_WAVES * 64, 2) void k_kv_attend_wide(RowsArgs g)
   const int tile_lo = row_range(a, rs, row0 + (rem + cols - 1) / G).x;
   const int tile_hi = min(a.ancestors ? min(max(rs.start + 1, 0), row_range(a, rs, row0).y) : row_range(a, rs, row0).y, k1);
 
-  const float scale = g.scale_log2 == 0.f ? 0x1p-149f : fabsf(g.scale_log2);       // never zero: times -infinity
+  const float scale = g.scale_log2 == 0.f ? 0x1p-149f : fabsf(g.scale_log2);       // zero only where the host flushes subnormal numbers, see rows_cut
   int c_lo, c_hi;
   uint64_t c_set;
   ts_u32x4 q[KS];
@@ -842,7 +842,9 @@ static int64_t rows_room(int64_t n_seqs, int64_t n_rows, int group, int hkv, int
 static RowsCut rows_cut(const ts_kv_attend_rows_args& a) {
   const int group = a.n_q_heads / a.cache.pages.n_kv_heads, hkv = a.cache.pages.n_kv_heads;
   RowsCut c;
-  c.nt = rows_nt(a.n_seqs, a.n_rows, group, a.cache.pages.dtype == TS_DTYPE_F32 || a.dtype == TS_DTYPE_F32);
+  // The wide kernel masks products before it scales them, and zero times the -infinity of what is not seen is not -infinity: a scale of zero is
+  // the other kernel's, where a seen infinite product makes its head NaN.
+  c.nt = a.scale == 0.f ? 1 : rows_nt(a.n_seqs, a.n_rows, group, a.cache.pages.dtype == TS_DTYPE_F32 || a.dtype == TS_DTYPE_F32);
   const int tm = 16 * c.nt;
   c.slots = a.row_offsets ? (int64_t)a.n_rows * group / tm + a.n_seqs : (int64_t)a.n_seqs * ((group + tm - 1) / tm);
   const int64_t whole = rows_whole(a.n_seqs, a.n_rows, group, hkv, c.nt), units = rows_units(a.max_len, a.window);

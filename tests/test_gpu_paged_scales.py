@@ -1,4 +1,4 @@
-"""Attention over 8-bit pages whose value scales a program wrote itself, at both ends of their range: a value stands for its e4m3 value times 2^e, infinite
+"""Attention of chunks with a scale of zero; and over 8-bit pages whose value scales a program wrote itself, at both ends of their range: a value stands for its e4m3 value times 2^e, infinite
 from 2^128 on, whatever its probability, in calls of few columns and of many; against 64 bits with the tolerances of test_gpu_paged_rows."""
 import math
 
@@ -65,3 +65,26 @@ def test_scales_at_their_ends(qdtype, rows, n, byte, at):
         i = inf[h // 2]
         assert bool((out[:, h, i] == V[at, h // 2, i]).all()), "infinite values: %s" % out[0, h, i]
         assert float(off[:, h, ~i].max() if bool((~i).any()) else 0) <= 1.0, off[:, h, ~i].max()
+
+
+@pytest.mark.parametrize("dtype,qdtype", [(BF16, BF16), (BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("rows", [1, 20])
+def test_an_infinite_product_with_a_scale_of_zero(dtype, qdtype, rows):
+    """Zero times either infinity is no number: the heads that see such a score are NaN, the others the mean of what they see."""
+    hq, hkv, hd, n = 4, 2, 64, 50
+    pages, table, K, V = cache_of([n + rows], hkv, hd, dtype, 4)
+    q = (torch.rand((rows, hq * hd), generator=torch.Generator().manual_seed(3)) + 0.01).to(qdtype).cuda()
+    for at, bad in ((7, -math.inf), (7, math.inf), (n + rows - 1, -math.inf), (n + rows // 2, -math.inf)):
+        other = pages.clone()
+        other.pages[0][int(table[0, at // 16]), 1, at % 16] = bad
+        for scale in (0.0, -0.0):
+            out, lse = ops.ts_kv_attend_rows(*other.pages, table, ints([n]), ints([0, rows]), q, n + rows, scale=scale)
+            out, lse = out.double().cpu().view(rows, hq, hd), lse.cpu()
+            for r in range(rows):
+                sees = n + r >= at
+                assert bool(out[r, 2:].isnan().all()) == sees and bool(lse[r, 2:].isnan().all()) == sees, (at, bad, r)
+                want = V[0][:n + r + 1].double().mean(0)
+                for h in range(2 if sees else 4):
+                    # equal weights: their sum, the values' sum and its rounding
+                    tol = (2.0 ** -8 if qdtype == BF16 and rows > 8 else 2.0 ** -20) * V[0][:n + r + 1, h // 2].double().abs().mean(0) + torch.finfo(qdtype).eps / 2 * want[h // 2].abs() + 1e-6
+                    assert bool(((out[r, h] - want[h // 2]).abs() <= tol).all()), (at, bad, r, h)
