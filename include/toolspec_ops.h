@@ -93,7 +93,7 @@ ts_status ts_kv_extend(ts_kv* kv, int32_t n_pos, ts_stream stream);
 /* Appends new rows to the cache.  Rows [row_offsets[s], row_offsets[s + 1]) belong to sequence s
  * and get positions lengths[s], lengths[s] + 1, ... .  Keys are stored rotated (pair
  * (j, j + head_dim / 2) by position * rope_theta^(-2 j / head_dim), an angle that is good to 1e-7
- * radians at any position; rope_theta 0: not rotated),
+ * radians up to position 2^25, and to 5e-7 at any; rope_theta 0: not rotated),
  * values as they are, both in the cache's dtype; with q, the rotated queries go to q_out (which
  * may be q).  Rows outside every sequence, and rows whose position is negative, beyond the table
  * or on a page outside [0, n_pages), leave cache and q_out as they were.  Lengths are not
@@ -176,7 +176,8 @@ typedef struct {
  *             (a table's entries are taken as exact).
  * and then rounded once, to its place.  The position of the angle is that of the row, or positions[row] where that is not null
  * (a draft tree's rows lie one behind the other and are turned by their depths); the row's place is not changed by it.
- * A head whose squares overflow fp32 is normed to zeros, NaN stays NaN.
+ * A head whose squares overflow fp32 is normed to zeros; with norm_eps 0 one whose squares all vanish in fp32 becomes infinite, or NaN where it is
+ * zero; NaN stays NaN.  Where nothing of this is asked for, ts_kv_append does the same in less time.
  * Errors: INVALID_ARG (as ts_kv_append; scales missing or misaligned, rope_dim, norm_eps negative or not finite, rope_magnitude not finite,
  * misaligned gains, frequencies or positions), DEVICE. */
 typedef struct {
@@ -222,8 +223,12 @@ ts_status ts_kv_read(const ts_kv_read_args* args, ts_stream stream);
  * stay as they were in out and lse.  A seen infinite value makes its dimension infinite, or NaN where its probability is zero.
  * Scores, sums and outputs are fp32; queries and probabilities of fp32 rows enter the products over bf16 and 8-bit pages with 24 bits.
  * Probabilities of bf16 rows have 24 bits too where the chunks have up to 16 rows x heads per KV head on average; where they have more they are
- * rounded to bf16, once, for the product with the values (not for their sum): as much as the rounding of the output.  The order of
+ * rounded to bf16, once, for the product with the values (not for their sum): as much as the rounding of the output.  The average is that of the
+ * call, n_rows * n_q_heads / (n_seqs * n_kv_heads): a row's bits go by the sizes of the call that it is in, and a program that wants 24 bits for chunks of
+ * many rows gives them in fp32.  The order of
  * the sums depends on the sizes (n_seqs, n_rows, heads, max_len, window) and a chunk's own rows, never on contents.
+ * The same averages choose how the work is cut: sequences of one or a few rows and chunks of many, or one long sequence and many short ones, take less
+ * time in calls of their own than in one together.  One token per sequence over fp32 and bf16 pages takes as long or less by ts_kv_attend.
  *   q, out    : [n_rows] rows of n_q_heads * head_dim, in `dtype`
  *   lse       : [n_rows][n_q_heads] fp32, or null
  *   ancestors : [n_rows] 64-bit sets, or null

@@ -12,7 +12,7 @@
 // rounded to 2^-26 of a turn there, 9e-8 radians, as much as a step of fp32 sines.
 //
 // Bound by the start of a launch for a step's rows (one row, 8 + 32 heads of 128: 3.9 us, of which starting a launch is 2 to 3) and by HBM
-// for contexts: 2040 rows of 8 + 64 heads move 80 MB (as counted) in 21.2 us, 3.8 TB/s; 2048 rows of 8 + 32 heads on whole pages 50 MB
+// for contexts: 1938 rows of 8 + 64 heads move 80 MB (as counted) in 21.2 us, 3.8 TB/s; 2048 rows of 8 + 32 heads on whole pages 50 MB
 // in 10.2 us, 4.9 TB/s.
 // ---------------------------------------------------------------------------------
 struct AppendArgs {
@@ -537,7 +537,7 @@ extern "C" ts_status ts_kv_append(const ts_kv_append_args* args, ts_stream strea
   g.window = each < 2 ? 1 : each < 8 ? 2 : each < 256 ? 4 : each < 1024 ? 8 : 16;
   // Its heads: many sequences with a few rows each are many pages with little on them, and where a page's rows go and their
   // sines are the work: 8 / 32 heads, 64 sequences of 1 row 4.8 / 5.3 us, 128 5.8 / 6.0, 256 9.2 / 7.6, 1024 29 / 20; 64 of 4
-  // rows 9.7 / 10.3, 128 17 / 14, 512 43 / 32; contexts 2040 rows of 5 21 / 23, 2048 of 1 12 / 18.
+  // rows 9.7 / 10.3, 128 17 / 14, 512 43 / 32; contexts 1938 rows of 5 21 / 23, 2048 of 1 12 / 18.
   g.heads = a.n_seqs >= 128 && each < 16 ? APPEND_HEADS : 8;
   const dim3 grid((a.n_rows + g.window - 1) / g.window, (heads + g.heads - 1) / g.heads);
   hipStream_t s = (hipStream_t)stream;

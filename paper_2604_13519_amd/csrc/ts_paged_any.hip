@@ -13,9 +13,11 @@
 // before its first byte.
 //
 // 8 + 32 heads of 128, bf16: a token's row 4.5 us, with norms 5.1, into 8-bit pages 4.9 (ts_kv_append 3.9): the launch and three dependent trips to
-// memory; 2048 rows on whole pages 13.0, 16.1 and 16.0 (10.4): 50 MB at 3.1 TB/s.  2040 rows of 5 sequences, 8 + 64 heads, 8-bit: 32.5 us for
-// 76 MB, 2.3 TB/s: pages begun and ended by parts, and 122 x 10 workgroups that each wait for offsets, length, page and rows in
-// turn.  Four, eight and sixteen heads a workgroup, with the reading back:
+// memory; 2048 rows on whole pages 13.0, 16.1 and 16.0 (10.4): 50 MB at 3.1 TB/s.  1938 rows of 5 sequences, 8 + 64 heads, 8-bit: 32.5 us for
+// 76 MB, 2.3 TB/s.  ts_kv_append moves 79 MB of the same rows in 21.2, with the same pages begun and ended by parts and the same trips for offsets, length,
+// page and rows, so these are not what makes the difference.  What it has beside them: pieces of at most four heads on their way in place of all,
+// a pair's sines read one by one (conflicts are half of the LDS cycles), and for 8 bits two barriers and a pass through the
+// LDS.  Their shares were not measured.  Four, eight and sixteen heads a workgroup, with the reading back:
 // 49.7, 40.8 and 45.0; rows reduced through the LDS 37 for 33.
 // ---------------------------------------------------------------------------------
 constexpr int RA_THREADS = 256, RA_HEADS = 8;

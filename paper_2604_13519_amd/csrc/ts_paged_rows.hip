@@ -413,8 +413,10 @@ __global__ __launch_bounds__(RO_WAVES * 64, NT == 1 ? 2 : 1) void k_kv_attend_ro
 // score passes it by more than 2^8, so that sums are rarely rescaled.  The matrix layout is the one above in tiles of 32 x 32: row m of K's
 // tile is key m with its bits 2 and 3 swapped.  Blocks go through registers (8-bit ones are widened there, times their scales,
 // once for all waves) into two LDS slots: while block b is used, b + 1 waits in registers and is written behind it, then b + 2 is
-// requested; one barrier a block.  Probabilities are rounded to bf16 for the product with the values: a second term would be half as
-// many matrix instructions again, for a rounding as large as the output's own.
+// requested; one barrier a block.  Probabilities are rounded to bf16 for the product with the values, a rounding as large as the output's own:
+// 0.0023 of the outputs' norm from 64 bits, where the output's alone is 0.0017.  A second term, which takes that away, is half as many matrix
+// instructions again: prompts 286 -> 367 us, 8-bit chunks below 972 -> 1244, the tree 36.2 -> 40.1; 412, 1463 and 44.6 where the second term may not be zero, so that
+// an infinite value stays so.
 //
 // bf16, 32 query heads over 8 of 128: three prompts, 9012 rows (237 GFLOP as counted) 290 - 305 us, 0.80 PFLOP/s, matrix pipes busy 40 %;
 // a tree of 65 rows over 8192 positions 28 us and 7 of the join; 16 x 33 rows over up to 4096 66 and 12.  8-bit, 64 heads over 8:
@@ -824,7 +826,8 @@ struct RowsCut { int nt, chunk, splits; int64_t slots; };    // tiles of 16 a wo
 // Columns of a workgroup, from those a sequence has on average: 16; then, of fp32 rows or pages, 32; of others 128 and, from 512 on, 256.
 // bf16, 32 query heads over 8, microseconds: 8 rows over 8192 (32 columns) 128 a workgroup 20.3, tiles of 64 straight from memory 29.3;
 // 16 x 12 rows over 4096 (48) 57 and 157; 16 x 33 over up to 4096 (132) 76, and 256 a workgroup 88; 8-bit chunks of 4 x 512 rows
-// (4096) 1217 and 1127.
+// (4096) 1217 and 1127.  All of these have about as many rows a sequence.  Where they differ the average serves neither kind: 7 tokens over 32768 positions and a chunk
+// of 512 rows over 8192, bf16, 64 heads over 8, 674 in one call and 166 + 168 in two; a token over 32768 beside 63 over 200, 32 heads, 284 and 30 + 16.
 static int rows_nt(int64_t n_seqs, int64_t n_rows, int group, bool f32) { return n_rows * group <= n_seqs * 16 ? 1 : f32 ? 2 : n_rows * group <= n_seqs * 512 ? 8 : 16; }
 static int64_t rows_units(int max_len, int window) {         // of 128 keys, in what one tile sees
   const int64_t span = window > 0 && (int64_t)window + 256 < max_len ? window + 256 : max_len;
