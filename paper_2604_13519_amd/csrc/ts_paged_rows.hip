@@ -9,7 +9,7 @@
 // row m / group, head m % group, and all columns go over the same keys and values.  One pass with a running maximum and sum, the
 // cache's length split over workgroups and joined where the tiles of columns alone do not fill the card.
 //
-// This kernel: few columns (single tokens), and fp32 rows or pages.  Tiles of 16 NT columns, four waves that take blocks of 32 keys in
+// This kernel: few columns (single tokens), fp32 rows or pages, a scale of zero.  Tiles of 16 NT columns, four waves that take blocks of 32 keys in
 // turn, straight from memory: bound by the bytes of the cache, each read once for a tile.
 //
 // Matrix instructions without any exchange between lanes: S^T = K Q^T puts 16 columns on the lanes (lane l: column l % 16) and four keys
